@@ -363,6 +363,94 @@ int psc_imi_search(const psc_index *idx, const float *q_dev, int64_t nq, int max
                    int k, int64_t *ids_dev, float *dists_dev, int32_t *cells_out_dev, uint8_t *qcodes_out_dev,
                    void *workspace_dev, size_t workspace_bytes, psc_stream stream);
 
+/* ------------------------------------------------------------------ attention memory in 4 bits */
+/* A language model's cached keys and values, compressed as they arrive and compared with queries in full precision: the
+ * asymmetric comparison of the scan above, on coordinates in 4-bit floating point.
+ *
+ * The cache is a pool of pages, each with `page` slots for every kv head; a sequence's slot s lies on page
+ * table_dev[b][s / page] at s % page.  Buffers, all the caller's: codes [pages][kv_heads][page][head_dim / 2], scales
+ * [pages][kv_heads][page][head_dim / 32] (uint8), for keys and for values; 16-byte aligned.  Two coordinates to a byte,
+ * the even one in the low half, each a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6; 32 consecutive coordinates share the
+ * scale 2^(byte - 127).  psc_kv_append rounds to it: with a the largest magnitude of the 32, the exponent is
+ * floor(log2 a) - 2, one more where a exceeds 7 times that power, and lies in -23 .. 13 (held values are then exact in
+ * float16 and bfloat16; larger magnitudes become 6 * 2^13); a coordinate becomes the nearest value, ties to the even
+ * code, magnitudes over 6 become 6.  A token whose key or value has a coordinate that is not finite keeps no value, and
+ * 255 (NaN) as the scales of its key: rows that see the token come out NaN, other rows do not change.
+ *   head_dim  64, 128 or 256        page   16, 32, 64, 128 or 256        pages, kv_heads, batch >= 1
+ *   table_dev [batch][table_width] (int32), entries outside 0 .. pages - 1: no page -- slots there are never written,
+ *             read as zeros and are seen by no row.  No page may stand twice among those written by one call.
+ *   lengths_dev [batch] (int32): tokens of each sequence; what exceeds table_width * page does not exist.
+ * Arrays "per slot" are dense: [batch][kv_heads][table_width * page], 16-byte aligned.
+ * batch * kv_heads <= 65535, table_width * page < 2^30. */
+#define PSC_BF16 0
+#define PSC_F16 1
+#define PSC_F32 2
+typedef struct psc_kv_cache {
+    uint8_t *k_codes_dev, *k_scales_dev, *v_codes_dev, *v_scales_dev;
+    int64_t pages;
+    int kv_heads, head_dim, page;
+    const int32_t *table_dev;
+    int batch, table_width;
+    const int32_t *lengths_dev;
+} psc_kv_cache;
+
+/* Rows of several sequences lie one after another: sequence b has the rows offsets_dev[b] .. offsets_dev[b + 1] - 1
+ * (int32 [batch + 1], ascending, from 0 to nrows), or, offsets_dev NULL, nrows / batch each (nrows a multiple of batch).
+ * Coordinates of a head are contiguous; the strides, in elements, lead from row to row and from head to head (a
+ * product's output that holds queries, keys and values side by side is taken as it is).  Rows and heads start at
+ * multiples of 16 bytes.  dtype: PSC_BF16, PSC_F16 or PSC_F32.
+ *
+ * psc_kv_append: row r of sequence b (counted from its first) is written to slot lengths_dev[b] + r; lengths_dev is not
+ * changed.  positions_dev (may be NULL), per slot: receives first_dev[b] + r (first_dev NULL: the slot).  weights_dev
+ * (may be NULL), per slot: receives 0. */
+int psc_kv_append(const psc_kv_cache *cache, int dtype, const void *k_dev, int64_t k_row_stride, int64_t k_head_stride,
+                  const void *v_dev, int64_t v_row_stride, int64_t v_head_stride, int nrows, const int32_t *offsets_dev,
+                  const int32_t *first_dev, int32_t *positions_dev, float *weights_dev, psc_stream stream);
+
+/* The values that the cache holds in the slots lengths_dev[b] + r: k_dev, v_dev [nrows][kv_heads][head_dim]. */
+int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *offsets_dev, void *k_dev, void *v_dev,
+                psc_stream stream);
+
+/* Attention of nrows rows of q_heads heads (a multiple of kv_heads: query head h looks at kv head h / (q_heads /
+ * kv_heads)); no sequence has more than max_rows rows (offsets_dev NULL: not used).
+ *   scores s = scale * q . k (scale > 0) over the tokens that a row sees, p = softmax(s), out = sum p v.
+ * Row r of sequence b stands at position first_dev[b] + r (first_dev NULL: its rows are its last tokens); a token at
+ * positions_dev (per slot, >= 0; NULL: its slot).  A row sees the tokens of its sequence
+ *   - at its own position and before it, if `causal`;
+ *   - of those, if window > 0, the ones fewer than `window` positions back and the ones at positions below `sinks`.
+ * out_dev [nrows][q_heads][head_dim] (dtype), lse_dev (may be NULL) [nrows][q_heads] float32: log of the sum of exp s.
+ * A row that sees nothing: zeros and -infinity.  window > 0 needs causal.
+ * weights_out_dev (may be NULL), per slot: weights_in_dev (NULL: 0) + the sum of p over the sequence's rows and the kv
+ * head's query heads; 0 is added in slots that no row sees, rows that come out NaN add nothing.  The two may be the same.
+ * Held values enter the products exactly, rows as they are; scores, sums and softmax are float32; probabilities are
+ * rounded to float16 for the second product (float32 rows: to 22 bits).  Results do not depend on timing: nothing is
+ * added atomically.  Where slots are positions (positions_dev NULL), tokens that a window hides are not read.
+ * Workspace: psc_kv_attention_workspace_bytes (may be 0: workspace_dev may then be NULL). */
+size_t psc_kv_attention_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
+                                        int window, int sinks, int has_positions, int has_weights);
+int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,
+                     int64_t q_head_stride, int nrows, int max_rows, int q_heads, const int32_t *offsets_dev,
+                     const int32_t *first_dev, const int32_t *positions_dev, float scale, int causal, int window,
+                     int sinks, void *out_dev, float *lse_dev, const float *weights_in_dev, float *weights_out_dev,
+                     void *workspace_dev, size_t workspace_bytes, psc_stream stream);
+
+/* Cuts every (sequence, kv head) with more than `budget` tokens down to the budget.  Kept are the tokens at positions
+ * below `sinks` and at seen_dev[b] - recent and later (seen_dev NULL: lengths_dev; sinks + recent <= budget), then
+ * those of the largest weights_dev (per slot; NaN counts as the smallest); the lower slot on equal weight.  The slots
+ * below the budget that fall free take, in ascending order, the kept tokens of the slots behind it, in ascending order;
+ * nothing else moves, and slots behind the budget stay as they are until they are written again.
+ *   kept_dev [batch][kv_heads][budget] (int32): the slot that the token now in this slot had; -1 past the length
+ *   lengths_out_dev [batch]: min(length, budget)
+ *   positions_out_dev (may be NULL), weights_out_dev [batch][kv_heads][out_stride], out_stride >= budget: positions
+ *     (positions_dev NULL: the slots that they had) and weights of the kept tokens; -1 and 0 past the length
+ * lengths_out_dev may be lengths_dev, positions_out_dev positions_dev and weights_out_dev weights_dev, the last two with
+ * out_stride = table_width * page.  Workspace: psc_kv_evict_workspace_bytes. */
+size_t psc_kv_evict_workspace_bytes(const psc_kv_cache *cache, int budget);
+int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int32_t *positions_dev,
+                 const int32_t *seen_dev, int budget, int sinks, int recent, int32_t *kept_dev,
+                 int32_t *lengths_out_dev, int32_t *positions_out_dev, float *weights_out_dev, int64_t out_stride,
+                 void *workspace_dev, size_t workspace_bytes, psc_stream stream);
+
 /* Synchronise `stream` and report whether any scan that used this workspace since
  * the last call gave up on an internal wait (never expected; results of such a
  * scan are marked with id -2).  Returns 0 if clean, PSC_EHIP otherwise. */

@@ -21,3 +21,4 @@ from .binding import (  # noqa: F401
     version,
     workspace_status,
 )
+from .kv import KvCache  # noqa: F401

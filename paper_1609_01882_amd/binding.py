@@ -79,6 +79,12 @@ def _load():
         "psc_imi_search_workspace_bytes": (sz, [vp, i64, i32]),
         "psc_imi_search": (i32, [vp, vp, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
         "psc_workspace_status": (i32, [vp, vp]),
+        "psc_kv_append": (i32, [vp, i32, vp, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp]),
+        "psc_kv_read": (i32, [vp, i32, i32, vp, vp, vp, vp]),
+        "psc_kv_attention_workspace_bytes": (sz, [vp, i32, i32, i32, i32, i32, i32, i32, i32]),
+        "psc_kv_attention": (i32, [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, C.c_float, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
+        "psc_kv_evict_workspace_bytes": (sz, [vp, i32]),
+        "psc_kv_evict": (i32, [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, i64, vp, sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -100,7 +106,9 @@ def exported_symbols():
             "psc_knn_graph", "psc_ivf_train_coarse", "psc_ivf_set_coarse", "psc_ivf_get_coarse",
             "psc_ivf_assign_encode", "psc_ivf_set_lists", "psc_ivf_search_workspace_bytes",
             "psc_ivf_search", "psc_imi_set_coarse", "psc_imi_assign_workspace_bytes", "psc_imi_assign_encode",
-            "psc_imi_set_lists", "psc_imi_search_workspace_bytes", "psc_imi_search", "psc_workspace_status"]
+            "psc_imi_set_lists", "psc_imi_search_workspace_bytes", "psc_imi_search", "psc_workspace_status",
+            "psc_kv_append", "psc_kv_read", "psc_kv_attention_workspace_bytes", "psc_kv_attention",
+            "psc_kv_evict_workspace_bytes", "psc_kv_evict"]
 
 
 def _check(rc: int):

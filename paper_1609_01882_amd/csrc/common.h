@@ -318,6 +318,62 @@ int launch_coarse_refill(const float *x_dev, int64_t n, int dim, int big, int c,
 // Row ncent of cent_dev [ncent + 1][dim] := the mean of rows 0 .. ncent-1.
 int launch_mean_centroid(float *cent_dev, int ncent, int dim, hipStream_t s);
 
+// ---- attention memory in 4 bits (kernels_kv.hip)
+// What psc_kv_cache says, checked; page = 1 << page_shift slots.
+struct KvView {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int64_t pages;
+    int heads, dim, page_shift;
+    const int32_t *table, *lengths;
+    int batch, width;
+};
+// Rows that are written or read: row r of sequence b (offsets, or `each` rows a sequence) has slot lengths[b] + r.
+struct KvRows {
+    const void *k, *v;
+    int64_t k_stride, k_head_stride, v_stride, v_head_stride;
+    int nrows, each;
+    const int32_t *offsets, *first;
+    int32_t *positions;
+    float *weights;
+};
+int launch_kv_append(const KvView &c, int dtype, const KvRows &r, hipStream_t s);
+int launch_kv_read(const KvView &c, int dtype, const KvRows &r, void *k_out, void *v_out, hipStream_t s);
+struct KvQueries {
+    const void *q;
+    int64_t row_stride, head_stride;
+    int nrows, each, max_rows, q_heads, group;
+    const int32_t *offsets, *first, *positions;
+    float factor;  // scale / log 2
+    int causal, window, sinks;
+    void *out;
+    float *lse;
+    int splits, split_blocks;
+    float *part_stat, *part_acc;  // [splits][nrows][q_heads][2], [...][dim]
+    float *stat;                  // [nrows][q_heads][2]: maximum (units of log 2), 1 / sum
+};
+struct KvPlan {
+    bool split_tokens = false;  // the waves of a workgroup share rows and split tokens
+    int row_tiles = 0;          // of 16, to a wave
+    int64_t row_groups = 0, splits = 0, split_blocks = 0;
+    size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0;
+    size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes; }
+};
+KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered,
+                         bool weights);
+// received (or null): given (or 0) + the weight each token received.
+int launch_kv_attention(const KvView &c, int dtype, const KvQueries &q, const KvPlan &p, const float *given, float *received,
+                        hipStream_t s);
+struct KvEvict {
+    const float *weights;
+    const int32_t *positions, *seen;
+    int budget, sinks, recent;
+    int64_t out_stride;
+    int32_t *kept, *lengths_out, *positions_out;
+    float *weights_out;
+    int32_t *holes, *later;  // scratch [batch][heads][budget] each
+};
+int launch_kv_evict(const KvView &c, const KvEvict &e, hipStream_t s);
+
 }  // namespace psc
 
 struct psc_index {

@@ -1,0 +1,1052 @@
+// Attention memory in 4 bits: writing it, attending over it, cutting it to a budget.
+//
+// Format.  A token's head has head_dim coordinates, two to a byte (even coordinates in the low half), as E2M1
+// floats: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign.  32 consecutive coordinates share the scale 2^e, e + 127 in a byte.
+// With a the largest of the 32 magnitudes, e = floor(log2 a) - 2, one more where a > 7 * 2^e (there the error of
+// cutting a to 6 and that of the coarser grid are the same; on normal, Laplace and heavy-tailed data this rule has
+// the smallest mean square error of all thresholds on a's mantissa, 1.25 % of the normal data's), clamped to
+// -23 .. 13: every held value is then exact in float16 as well as in bfloat16, which the products rely on.
+// A token with a value that is not finite gets 255 in all scale bytes of its key, and a value of zeros: its scores
+// are NaN, so every row that sees it comes out NaN, and no other row does (a NaN in the value would reach masked
+// rows too, as 0 * NaN).
+#include <algorithm>
+#include <cmath>
+
+#include "common.h"
+#include "entry.h"
+
+namespace psc {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+
+constexpr uint32_t kNanScale = 255u;
+constexpr int kMinScale = 127 - 23, kMaxScale = 127 + 13;
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLn2 = 0.693147180559945f;
+
+template <int DT>
+struct Element;  // what a row's coordinates are stored as
+template <>
+struct Element<PSC_BF16> {
+    typedef uint16_t type;
+    static __device__ float load(type x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ type store(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+};
+template <>
+struct Element<PSC_F16> {
+    typedef uint16_t type;
+    static __device__ float load(type x) { return (float)__builtin_bit_cast(_Float16, x); }
+    static __device__ type store(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+};
+template <>
+struct Element<PSC_F32> {
+    typedef float type;
+    static __device__ float load(type x) { return x; }
+    static __device__ type store(float x) { return x; }
+};
+
+// N consecutive coordinates (16-byte aligned for N * size >= 16) as floats, and back.
+template <int DT, int N>
+__device__ __forceinline__ void load_row(const void *p, float (&x)[N])
+{
+    typedef typename Element<DT>::type T;
+    T t[N];
+    __builtin_memcpy(t, __builtin_assume_aligned(p, N * sizeof(T) < 16 ? N * sizeof(T) : 16), sizeof t);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = Element<DT>::load(t[i]);
+}
+template <int DT, int N>
+__device__ __forceinline__ void store_row(void *p, const float (&x)[N])
+{
+    typedef typename Element<DT>::type T;
+    T t[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = Element<DT>::store(x[i]);
+    __builtin_memcpy(__builtin_assume_aligned(p, N * sizeof(T) < 16 ? N * sizeof(T) : 16), t, sizeof t);
+}
+
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Two held values: byte B of `codes`.
+template <int B>
+__device__ __forceinline__ uint32_t two_b16(uint32_t codes, float scale)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, B));
+}
+template <int B>
+__device__ __forceinline__ uint32_t two_h16(uint32_t codes, float scale)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, B));
+}
+
+// The sequence a row belongs to: offsets [batch + 1] ascending, or `each` rows for every sequence.
+__device__ __forceinline__ int sequence_of_row(const int32_t *offsets, int batch, int each, int row)
+{
+    if (!offsets) return row / each;
+    int lo = 0, hi = batch;  // offsets[lo] <= row < offsets[hi], where offsets are as they should be
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (offsets[mid] <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// The page of a slot, -1 where the table has none.
+__device__ __forceinline__ int page_of(const KvView &c, int b, int64_t slot)
+{
+    if (slot < 0 || slot >= (int64_t)c.width << c.page_shift) return -1;
+    const int p = c.table[(int64_t)b * c.width + (int)(slot >> c.page_shift)];
+    return p >= 0 && p < c.pages ? p : -1;
+}
+
+// ------------------------------------------------------------------------------------------- append, read
+// D / 8 lanes to a (row, head), 8 coordinates of its key and of its value to a lane; four lanes share a scale.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRows r)
+{
+    constexpr int L = D / 8;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int part = (int)(threadIdx.x % L);
+    if (item >= (int64_t)r.nrows * c.heads) return;
+    const int row = (int)(item / c.heads), head = (int)(item % c.heads);
+    const int b = sequence_of_row(r.offsets, c.batch, r.each, row);
+    const int place = row - (r.offsets ? r.offsets[b] : b * r.each);
+    const int64_t slot = (int64_t)c.lengths[b] + place;
+    const int page = place < 0 ? -1 : page_of(c, b, slot);
+    typedef typename Element<DT>::type T;
+    float x[2][8];
+    load_row<DT, 8>((const T *)r.k + row * r.k_stride + head * r.k_head_stride + part * 8, x[0]);
+    load_row<DT, 8>((const T *)r.v + row * r.v_stride + head * r.v_head_stride + part * 8, x[1]);
+    float top[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        top[t] = 0.f;
+        uint32_t bits = 0u;  // the largest magnitude as an integer: NaN and infinity are above all others
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[t][i]) & 0x7fffffffu);
+        bits = max(bits, (uint32_t)__shfl_xor((int)bits, 1));
+        bits = max(bits, (uint32_t)__shfl_xor((int)bits, 2));
+        top[t] = __uint_as_float(bits);
+    }
+    uint32_t odd = max(__float_as_uint(top[0]), __float_as_uint(top[1]));
+#pragma unroll
+    for (int d = 4; d < L; d *= 2) odd = max(odd, (uint32_t)__shfl_xor((int)odd, d));
+    const bool finite = odd < 0x7f800000u;
+    if (page < 0) return;
+    const int64_t at = ((int64_t)page * c.heads + head) << c.page_shift | (slot & ((1 << c.page_shift) - 1));
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const uint32_t bits = __float_as_uint(top[t]);
+        int e = (int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+        e = min(max(e, kMinScale), kMaxScale);
+        uint32_t codes = 0u;
+        if (finite) {
+            const float s = scale_of((uint32_t)e);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[t][0], x[t][1], s, 0);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[t][2], x[t][3], s, 1);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[t][4], x[t][5], s, 2);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[t][6], x[t][7], s, 3);
+        } else {
+            e = t == 0 ? (int)kNanScale : kMinScale;
+        }
+        uint8_t *to = t == 0 ? c.k_codes : c.v_codes, *scales = t == 0 ? c.k_scales : c.v_scales;
+        *(uint32_t *)(to + at * (D / 2) + part * 4) = codes;
+        if (part % 4 == 0) scales[at * (D / 32) + part / 4] = (uint8_t)e;
+    }
+    if (part == 0) {
+        const int64_t dense = ((int64_t)b * c.heads + head) * ((int64_t)c.width << c.page_shift) + slot;
+        if (r.positions) r.positions[dense] = (r.first ? r.first[b] : c.lengths[b]) + place;
+        if (r.weights) r.weights[dense] = 0.f;
+    }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(256) void kv_read_kernel(KvView c, KvRows r, void *k_out, void *v_out)
+{
+    constexpr int L = D / 8;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int part = (int)(threadIdx.x % L);
+    if (item >= (int64_t)r.nrows * c.heads) return;
+    const int row = (int)(item / c.heads), head = (int)(item % c.heads);
+    const int b = sequence_of_row(r.offsets, c.batch, r.each, row);
+    const int place = row - (r.offsets ? r.offsets[b] : b * r.each);
+    const int64_t slot = (int64_t)c.lengths[b] + place;
+    const int page = place < 0 ? -1 : page_of(c, b, slot);
+    typedef typename Element<DT>::type T;
+    const int64_t at = page < 0 ? 0 : ((int64_t)page * c.heads + head) << c.page_shift | (slot & ((1 << c.page_shift) - 1));
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const uint8_t *from = t == 0 ? c.k_codes : c.v_codes, *scales = t == 0 ? c.k_scales : c.v_scales;
+        uint32_t codes = 0u, e = kMinScale;
+        if (page >= 0) {
+            codes = *(const uint32_t *)(from + at * (D / 2) + part * 4);
+            e = scales[at * (D / 32) + part / 4];
+        }
+        const float s = scale_of(e);
+        const uint32_t two[4] = {two_b16<0>(codes, s), two_b16<1>(codes, s), two_b16<2>(codes, s), two_b16<3>(codes, s)};
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(two[i] << 16);
+            x[2 * i + 1] = __uint_as_float(two[i] & 0xffff0000u);
+        }
+        store_row<DT, 8>((T *)(t == 0 ? k_out : v_out) + item * D + part * 8, x);
+    }
+}
+
+// ------------------------------------------------------------------------------------------- attention
+// The rows of a (sequence, kv head): row m of it is query head m % group of the sequence's row m / group.
+struct RowSet {
+    int first_row, rows;  // the sequence's rows, in the caller's array
+    int first_pos;        // position of its first row
+    int n;                // tokens of the sequence
+};
+__device__ __forceinline__ RowSet rows_of(const KvView &c, const KvQueries &q, int b)
+{
+    RowSet s;
+    s.first_row = q.offsets ? q.offsets[b] : b * q.each;
+    s.rows = q.offsets ? q.offsets[b + 1] - s.first_row : q.each;
+    if (s.first_row < 0 || s.first_row > q.nrows) s.rows = 0;
+    s.rows = max(0, min(min(s.rows, q.max_rows), q.nrows - s.first_row));
+    s.n = (int)max((int64_t)0, min((int64_t)c.lengths[b], (int64_t)c.width << c.page_shift));
+    s.first_pos = q.first ? q.first[b] : s.n - s.rows;
+    return s;
+}
+
+// Blocks of 32 slots that some row at positions lo_pos .. hi_pos can see: those below `sink_blocks`, then
+// `main` ... end.  With positions of their own the slots are in no order: all blocks.
+struct Blocks {
+    int sink_blocks, main, end;
+    __device__ int count() const { return sink_blocks + end - main; }
+    __device__ int block(int i) const { return i < sink_blocks ? i : i - sink_blocks + main; }
+};
+__device__ __forceinline__ Blocks blocks_of(const KvQueries &q, int n, int lo_pos, int hi_pos)
+{
+    Blocks k;
+    k.sink_blocks = 0;
+    k.main = 0;
+    int end = n;
+    if (!q.positions && q.causal) end = (int)max((int64_t)0, min((int64_t)n, (int64_t)hi_pos + 1));
+    k.end = (end + 31) / 32;
+    if (!q.positions && q.window > 0) {
+        const int from = (int)max((int64_t)0, min((int64_t)end, (int64_t)lo_pos - q.window + 1));
+        k.sink_blocks = (min(q.sinks, end) + 31) / 32;
+        k.main = max(k.sink_blocks, from / 32);
+        if (k.main > k.end) k.main = k.end;
+    }
+    return k;
+}
+
+// What a lane holds of a block of 32 tokens as it lies in memory.  With i = lane % 16 and g = lane / 16:
+// keys of the tokens i and 16 + i, coordinates g D/4 ... (a run of D/8 bytes; whole scale blocks or halves of one);
+// values of the tokens 4 g + r and 16 + 4 g + r (r = 0..3), coordinates i D/16 ... (a run of D/32 bytes).
+template <int D>
+struct Raw {
+    uint32_t k[2][D / 32], ks[2];
+    uint32_t v[8][D == 256 ? 2 : 1], vs[8];
+    int pos[8];  // positions of the value tokens, where they have some of their own
+};
+
+template <int D>
+__device__ __forceinline__ void load_keys(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (&k)[D / 32], uint32_t &ks)
+{
+    const int64_t at = (((int64_t)page * c.heads + head) << c.page_shift) + in_page;  // uniform
+    const uint8_t *p = c.k_codes + at * (D / 2), *s = c.k_scales + at * (D / 32);
+    const uint32_t off = (uint32_t)(i * (D / 2) + g * (D / 8));
+    if constexpr (D == 64) {
+        const u32x2 t = *(const u32x2 *)(p + off);
+        k[0] = t.x;
+        k[1] = t.y;
+        ks = s[(uint32_t)(i * 2 + (g >> 1))];
+    } else {
+#pragma unroll
+        for (int j = 0; j < D / 128; ++j) {
+            const u32x4 t = *(const u32x4 *)(p + off + j * 16);
+            k[j * 4 + 0] = t.x;
+            k[j * 4 + 1] = t.y;
+            k[j * 4 + 2] = t.z;
+            k[j * 4 + 3] = t.w;
+        }
+        if constexpr (D == 128) ks = s[(uint32_t)(i * 4 + g)];
+        else ks = *(const uint16_t *)(s + (uint32_t)(i * 8 + g * 2));
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void load_values(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (*v)[D == 256 ? 2 : 1], uint32_t *vs)
+{
+    const int64_t at = (((int64_t)page * c.heads + head) << c.page_shift) + in_page;
+    const uint8_t *p = c.v_codes + at * (D / 2), *s = c.v_scales + at * (D / 32);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t off = (uint32_t)((g * 4 + r) * (D / 2) + i * (D / 32));
+        if constexpr (D == 64) v[r][0] = *(const uint16_t *)(p + off);
+        else if constexpr (D == 128) v[r][0] = *(const uint32_t *)(p + off);
+        else {
+            const u32x2 t = *(const u32x2 *)(p + off);
+            v[r][0] = t.x;
+            v[r][1] = t.y;
+        }
+        vs[r] = s[(uint32_t)((g * 4 + r) * (D / 32) + i * (D / 16) / 32)];
+    }
+}
+
+// Keys of 16 tokens as operands of D / 32 products (bfloat16, or float16 for float16 rows): both exact.
+template <int D, int DT>
+__device__ __forceinline__ void expand_keys(const uint32_t (&k)[D / 32], uint32_t ks, u32x4 (&a)[D / 32])
+{
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        const float s = scale_of(D == 256 ? (j < 4 ? ks & 255u : ks >> 8) : ks);
+        if constexpr (DT == PSC_F16) a[j] = u32x4{two_h16<0>(k[j], s), two_h16<1>(k[j], s), two_h16<2>(k[j], s), two_h16<3>(k[j], s)};
+        else a[j] = u32x4{two_b16<0>(k[j], s), two_b16<1>(k[j], s), two_b16<2>(k[j], s), two_b16<3>(k[j], s)};
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ f32x4 mfma_scores(u32x4 a, u32x4 b, f32x4 acc)
+{
+    if constexpr (DT == PSC_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), acc, 0, 0, 0);
+}
+
+// Sixteen rows as operands: lane (i, g) holds of row i the coordinates g D/4 ..., 8 to a product.  float32 rows are the
+// sum of three bfloat16 (24 bits of mantissa): three products each.
+template <int D, int DT>
+struct Rows {
+    static constexpr int kTerms = DT == PSC_F32 ? 3 : 1;
+    u32x4 x[kTerms][D / 32];
+};
+template <int D, int DT>
+__device__ __forceinline__ void load_rows(const KvQueries &q, const RowSet &s, int head, int m, int g, Rows<D, DT> &rows)
+{
+    typedef typename Element<DT>::type T;
+    const int mm = max(0, min(m, s.rows * q.group - 1));
+    const int t = mm / q.group, h = head * q.group + mm % q.group;
+    const T *p = (const T *)q.q + (int64_t)(s.first_row + t) * q.row_stride + (int64_t)h * q.head_stride + g * (D / 4);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        if constexpr (DT != PSC_F32) rows.x[0][j] = *(const u32x4 *)(p + j * 8);
+        else {
+            float x[8];
+            load_row<DT, 8>(p + j * 8, x);
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __bf16 a = (__bf16)x[2 * i], b = (__bf16)x[2 * i + 1];
+                    w[i] = (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+                    x[2 * i] -= (float)a;
+                    x[2 * i + 1] -= (float)b;
+                }
+                rows.x[term][j] = u32x4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+}
+
+// Scores of 16 tokens x 16 rows: token 4 g + r in register r, row i.
+template <int D, int DT>
+__device__ __forceinline__ f32x4 scores_of(const u32x4 (&a)[D / 32], const Rows<D, DT> &rows)
+{
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int term = Rows<D, DT>::kTerms - 1; term >= 0; --term)  // the smallest first
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) s = mfma_scores<DT>(a[j], rows.x[term][j], s);
+    return s;
+}
+
+// Which of a lane's 8 tokens (16 h + 4 g + r of the block) its row sees.
+struct RowMask {
+    int pos, after;  // position; tokens must lie after this one (or be among the first)
+};
+__device__ __forceinline__ RowMask row_mask(const KvQueries &q, int pos)
+{
+    RowMask m;
+    m.pos = q.causal ? pos : 0x7fffffff;
+    m.after = q.window > 0 ? (int)max((int64_t)pos - q.window, (int64_t)-0x80000000ll) : (int)-0x80000000ll;
+    return m;
+}
+__device__ __forceinline__ bool sees(const KvQueries &q, const RowMask &m, int pos_k)
+{
+    return pos_k <= m.pos && (q.window <= 0 || pos_k > m.after || pos_k < q.sinks);
+}
+
+// exp2 of the probability's exponent; values below 2^-126 come out as 0 or denormal, nothing depends on which.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// One wave attends with 16 RT rows over every nwaves-th block of the workgroup's part of the blocks.
+//
+// The transposed products keep everything of a row in the lanes of its column: scores K Q^T have the tokens in rows and
+// the rows in columns, so a lane holds 8 scores of one row; they are the operand of V^T P^T as they are, since the
+// order of the tokens inside a product is free as long as both sides agree; and the running maximum, which rescales
+// a column of the output, is the lane's own.  Values have to be transposed for that: a lane takes a run of
+// coordinates of 8 tokens and pairs up the tokens' values of one coordinate with one permutation each.
+// Scores, maximum, sum and output are 32-bit floats.  Probabilities are rounded to float16 (at most 2^-11 of each, an
+// eighth of what the output's own rounding to bfloat16 may add); for float32 rows two float16 hold 22 bits.
+template <int D, int DT, int RT>
+struct Attention {
+    f32x4 acc[RT][D / 16];
+    float top[RT], sum[RT];  // of the scaled scores in units of log 2; the sum is the lane's own share
+    Rows<D, DT> rows[RT];
+
+    __device__ void block(const KvView &c, const KvQueries &q, const Raw<D> &raw, const RowMask (&mask)[RT], int slot, int lim0,
+                          int lim1, bool whole, float factor, int g)
+    {
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u32x4 a[D / 32];
+            expand_keys<D, DT>(raw.k[h], raw.ks[h], a);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) s[t][h] = scores_of<D, DT>(a, rows[t]);
+        }
+        if (!whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = slot + 16 * h + 4 * g + r;
+                    const bool there = at < (h ? lim1 : lim0);
+                    const int pos = q.positions ? raw.pos[4 * h + r] : at;
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+                        if (!(there && sees(q, mask[t], pos))) s[t][h][r] = kNegInf;
+                }
+        }
+        uint32_t p[RT][2][4];  // float16 pairs (the second array: what the first leaves of float32 rows' probabilities)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            float m = kNegInf;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) m = fmaxf(m, s[t][h][r]);
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            m *= factor;
+            if (__any(m > top[t])) {
+                const float now = fmaxf(top[t], m);
+                const float shrink = now == kNegInf ? 1.f : exp2_fast(top[t] - now);
+                top[t] = now;
+                sum[t] *= shrink;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) acc[t][j] *= shrink;
+            }
+            const float base = top[t] == kNegInf ? 0.f : top[t];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const float e0 = exp2_fast(__builtin_fmaf(s[t][h][r], factor, -base));
+                    const float e1 = exp2_fast(__builtin_fmaf(s[t][h][r + 1], factor, -base));
+                    sum[t] += e0 + e1;
+                    const h16x2 hi = {(_Float16)e0, (_Float16)e1};
+                    p[t][0][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, hi);
+                    if constexpr (DT == PSC_F32) {
+                        const h16x2 lo = {(_Float16)(e0 - (float)hi.x), (_Float16)(e1 - (float)hi.y)};
+                        p[t][1][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, lo);
+                    }
+                }
+        }
+        // tokens 0..7 of the lane: 4 g + r, then 16 + 4 g + r
+        uint32_t held[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const int at = slot + (t < 4 ? 4 * g + t : 12 + 4 * g + t);
+            held[t] = whole || at < (t < 4 ? lim0 : lim1) ? raw.vs[t] : 0u;  // what lies past the end may be NaN: scale 2^-127, zeros in float16
+        }
+        constexpr int kBytes = D / 32;  // code bytes of a token in this lane
+#pragma unroll
+        for (int y = 0; y < kBytes; ++y) {
+            uint32_t w[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const float sc = scale_of(held[t]);
+                const uint32_t x = raw.v[t][y / 4];
+                w[t] = y % 4 == 0 ? two_h16<0>(x, sc) : y % 4 == 1 ? two_h16<1>(x, sc) : y % 4 == 2 ? two_h16<2>(x, sc) : two_h16<3>(x, sc);
+            }
+            u32x4 lo, hi;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                lo[t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x05040100u);
+                hi[t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x07060302u);
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+#pragma unroll
+                for (int term = DT == PSC_F32 ? 1 : 0; term >= 0; --term) {
+                    const h16x8 pr = __builtin_bit_cast(h16x8, (u32x4){p[t][term][0], p[t][term][1], p[t][term][2], p[t][term][3]});
+                    acc[t][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, lo), pr, acc[t][2 * y], 0, 0, 0);
+                    acc[t][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, hi), pr, acc[t][2 * y + 1], 0, 0, 0);
+                }
+            }
+        }
+    }
+};
+
+// kSplitTokens: the workgroup's four waves share 16 RT rows, every fourth block each, and are joined in LDS; otherwise
+// each wave has 16 RT rows of its own and all blocks.
+template <int D, int DT, int RT, bool kSplitTokens>
+__global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q)
+{
+    const int lane = lane_id(), i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads;
+    const RowSet s = rows_of(c, q, b);
+    const int m_all = s.rows * q.group;
+    const int m0 = ((int)blockIdx.y * (kSplitTokens ? 1 : 4) + (kSplitTokens ? 0 : wave)) * 16 * RT;
+    if ((int)blockIdx.y * (kSplitTokens ? 1 : 4) * 16 * RT >= m_all) return;  // (the whole workgroup)
+    const int m_end = min(m0 + 16 * RT, m_all);
+    const int lo_pos = s.first_pos + m0 / q.group, hi_pos = s.first_pos + (max(m_end, 1) - 1) / q.group;
+    const Blocks blocks = blocks_of(q, s.n, lo_pos, hi_pos);
+    const int count = m0 < m_all ? blocks.count() : 0;
+    const int begin = (int)blockIdx.x * q.split_blocks, end = min(count, begin + q.split_blocks);
+    const int step = kSplitTokens ? 4 : 1;
+
+    Attention<D, DT, RT> a;
+    RowMask mask[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        load_rows<D, DT>(q, s, head, m0 + t * 16 + i, g, a.rows[t]);
+        mask[t] = row_mask(q, s.first_pos + (m0 + t * 16 + i) / q.group);
+        a.top[t] = kNegInf;
+        a.sum[t] = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) a.acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int64_t dense = ((int64_t)b * c.heads + head) * ((int64_t)c.width << c.page_shift);
+
+    // the block that is being worked on, the one whose codes are on their way, the one whose pages are
+    Raw<D> raw;
+    int pages[2] = {-1, -1}, slot = 0, lim[2] = {0, 0};
+    auto find_pages = [&](int at, int (&pg)[2]) {
+        if (at >= end) return;
+        const int sl = blocks.block(at) * 32;
+        pg[0] = page_of(c, b, sl);
+        pg[1] = sl + 16 < s.n ? page_of(c, b, sl + 16) : -1;
+    };
+    auto load = [&](int at, const int (&pg)[2], Raw<D> &r) {
+        if (at >= end) return;
+        const int sl = blocks.block(at) * 32, mask_page = (1 << c.page_shift) - 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int page = max(pg[h], 0);
+            load_keys<D>(c, head, page, (sl + 16 * h) & mask_page, i, g, r.k[h], r.ks[h]);
+            load_values<D>(c, head, page, (sl + 16 * h) & mask_page, i, g, &r.v[4 * h], &r.vs[4 * h]);
+            if (q.positions && sl + 16 * h < s.n) {
+                const int4 x = *(const int4 *)(q.positions + dense + sl + 16 * h + 4 * g);
+                r.pos[4 * h] = x.x;
+                r.pos[4 * h + 1] = x.y;
+                r.pos[4 * h + 2] = x.z;
+                r.pos[4 * h + 3] = x.w;
+            }
+        }
+    };
+    int at = begin + (kSplitTokens ? wave : 0);
+    find_pages(at, pages);
+    load(at, pages, raw);
+    int next_pages[2] = {-1, -1};
+    find_pages(at + step, next_pages);
+    for (; at < end; at += step) {
+        Raw<D> next = raw;
+        load(at + step, next_pages, next);
+        int then[2] = {-1, -1};
+        find_pages(at + 2 * step, then);
+        slot = blocks.block(at) * 32;
+        lim[0] = pages[0] >= 0 ? s.n : 0;
+        lim[1] = pages[1] >= 0 ? s.n : 0;
+        const bool there = slot + 32 <= s.n && pages[0] >= 0 && pages[1] >= 0 && !q.positions;
+        const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
+                           (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
+        a.block(c, q, raw, mask, slot, lim[0], lim[1], whole, q.factor, g);
+        raw = next;
+        pages[0] = next_pages[0];
+        pages[1] = next_pages[1];
+        next_pages[0] = then[0];
+        next_pages[1] = then[1];
+    }
+    const bool parts = q.splits > 1;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        a.sum[t] += __shfl_xor(a.sum[t], 16);
+        a.sum[t] += __shfl_xor(a.sum[t], 32);
+    }
+
+    if constexpr (!kSplitTokens) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int m = m0 + t * 16 + i;
+            if (m >= m_all) continue;
+            const int64_t row = (int64_t)(s.first_row + m / q.group) * q.q_heads + head * q.group + m % q.group;
+            if (parts) {
+                const int64_t at_part = (int64_t)blockIdx.x * q.nrows * q.q_heads + row;
+                if (g == 0) *(float2 *)(q.part_stat + at_part * 2) = make_float2(a.top[t], a.sum[t]);
+                if (a.sum[t] == 0.f) continue;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x[D / 16];
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r];
+                    store_row<PSC_F32, D / 16>(q.part_acc + at_part * D + (g * 4 + r) * (D / 16), x);
+                }
+            } else {
+                const float inv = a.sum[t] == 0.f ? 0.f : 1.f / a.sum[t];
+                if (g == 0) {
+                    if (q.lse) q.lse[row] = a.sum[t] == 0.f ? kNegInf : (a.top[t] + __log2f(a.sum[t])) * kLn2;
+                    if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(a.top[t] == kNegInf ? 0.f : a.top[t], inv);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x[D / 16];
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r] * inv;
+                    store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + (g * 4 + r) * (D / 16), x);
+                }
+            }
+        }
+    } else {
+        constexpr int kStride = D + 4;
+        __shared__ float joined[4][16 * kStride];
+        __shared__ float tops[4][16 * RT], sums[4][16 * RT];
+        if (g == 0) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                tops[wave][t * 16 + i] = a.top[t];
+                sums[wave][t * 16 + i] = a.sum[t];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            float top = kNegInf;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, tops[w][t * 16 + i]);
+            const float shrink = top == kNegInf ? 1.f : exp2_fast(a.top[t] - top);
+            if (t) __syncthreads();
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x[D / 16];
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r] * shrink;
+                store_row<PSC_F32, D / 16>(&joined[wave][i * kStride + (g * 4 + r) * (D / 16)], x);
+            }
+            __syncthreads();
+            const int local = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, m = m0 + t * 16 + local;
+            if (m < m_all) {
+                float best = kNegInf, sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) best = fmaxf(best, tops[w][t * 16 + local]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sum += sums[w][t * 16 + local] * (best == kNegInf ? 1.f : exp2_fast(tops[w][t * 16 + local] - best));
+                float x[D / 16];
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    x[j] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x[j] += joined[w][local * kStride + part * (D / 16) + j];
+                }
+                const int64_t row = (int64_t)(s.first_row + m / q.group) * q.q_heads + head * q.group + m % q.group;
+                if (parts) {
+                    const int64_t at_part = (int64_t)blockIdx.x * q.nrows * q.q_heads + row;
+                    if (part == 0) *(float2 *)(q.part_stat + at_part * 2) = make_float2(best, sum);
+                    if (sum != 0.f) store_row<PSC_F32, D / 16>(q.part_acc + at_part * D + part * (D / 16), x);
+                } else {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    if (part == 0) {
+                        if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (best + __log2f(sum)) * kLn2;
+                        if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(best == kNegInf ? 0.f : best, inv);
+                    }
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) x[j] *= inv;
+                    store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
+                }
+            }
+        }
+    }
+}
+
+// Joins a row's parts: 16 lanes to a row.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
+{
+    const int64_t all = (int64_t)q.nrows * q.q_heads, row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int part = (int)threadIdx.x & 15;
+    if (row >= all) return;
+    float top = kNegInf, sum = 0.f, x[D / 16];
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) x[j] = 0.f;
+    for (int p = 0; p < q.splits; ++p) {
+        const float2 st = *(const float2 *)(q.part_stat + (p * all + row) * 2);
+        if (st.y == 0.f) continue;  // nothing seen there
+        const float now = fmaxf(top, st.x);
+        const float mine = now == kNegInf ? 1.f : exp2_fast(top - now), theirs = now == kNegInf ? 1.f : exp2_fast(st.x - now);
+        float y[D / 16];
+        load_row<PSC_F32, D / 16>(q.part_acc + (p * all + row) * D + part * (D / 16), y);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) x[j] = __builtin_fmaf(x[j], mine, y[j] * theirs);
+        sum = __builtin_fmaf(sum, mine, st.y * theirs);
+        top = now;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (part == 0) {
+        if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (top + __log2f(sum)) * kLn2;
+        if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(top == kNegInf ? 0.f : top, inv);
+    }
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) x[j] *= inv;
+    store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
+}
+
+// The weight that every token received: scores once more, from the same products as in the attention itself, so that
+// with the row's maximum and sum each probability is the one that was used.  A wave has 32 tokens and goes through all
+// rows that can see one; the rows' shares are added in one order.  Rows that came out NaN add nothing.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
+{
+    const int lane = lane_id(), i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads;
+    const RowSet s = rows_of(c, q, b);
+    const int64_t stride = (int64_t)c.width << c.page_shift, dense = ((int64_t)b * c.heads + head) * stride;
+    const int64_t block = (int64_t)blockIdx.x * 4 + wave;
+    if (block * 32 >= stride) return;
+    const int slot = (int)(block * 32), m_all = s.rows * q.group;
+
+    float total[2][4] = {};
+    if (slot < s.n && m_all > 0) {
+        const int pages[2] = {page_of(c, b, slot), slot + 16 < s.n ? page_of(c, b, slot + 16) : -1};
+        u32x4 a[2][D / 32];
+        int pos[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t k[D / 32], ks;
+            load_keys<D>(c, head, max(pages[h], 0), (slot + 16 * h) & ((1 << c.page_shift) - 1), i, g, k, ks);
+            expand_keys<D, DT>(k, ks, a[h]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at = slot + 16 * h + 4 * g + r;
+                pos[h][r] = q.positions && at < s.n ? q.positions[dense + at] : at;
+            }
+        }
+        int64_t m_begin = 0, m_end = m_all;
+        if (!q.positions) {
+            if (q.causal) m_begin = max((int64_t)0, (int64_t)slot - s.first_pos) * q.group / 16 * 16;
+            if (q.window > 0 && slot >= q.sinks)
+                m_end = min(m_end, max((int64_t)0, (int64_t)slot + 31 + q.window - s.first_pos) * q.group);
+        }
+        for (int64_t m0 = m_begin; m0 < m_end; m0 += 16) {
+            const int m = (int)m0 + i;
+            Rows<D, DT> rows;
+            load_rows<D, DT>(q, s, head, m, g, rows);
+            const bool valid = m < m_all;
+            const int mm = min(m, m_all - 1);
+            const int64_t row = (int64_t)(s.first_row + mm / q.group) * q.q_heads + head * q.group + mm % q.group;
+            const float2 st = *(const float2 *)(q.stat + row * 2);
+            const RowMask mask = row_mask(q, s.first_pos + mm / q.group);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 x = scores_of<D, DT>(a[h], rows);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = exp2_fast(__builtin_fmaf(x[r], q.factor, -st.x)) * st.y;
+                    const bool adds = valid && pages[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]) && p == p;
+                    total[h][r] += adds ? p : 0.f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int d = 1; d < 16; d *= 2) total[h][r] += __shfl_xor(total[h][r], d);
+    float mine = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mine = i == j ? total[j >> 2][j & 3] : mine;
+    const int at = slot + (i & 4) * 4 + 4 * g + (i & 3);
+    if (i < 8 && at < stride) received[dense + at] = (given ? given[dense + at] : 0.f) + mine;
+}
+
+// ------------------------------------------------------------------------------------------- eviction
+constexpr int kEvictThreads = 1024;
+
+// Order of a token's claim to stay: the first and the most recent above all, then the weight; NaN below all.
+__device__ __forceinline__ uint32_t claim_of(const KvEvict &e, int seen, float weight, int pos)
+{
+    if (pos < e.sinks || (int64_t)pos >= (int64_t)seen - e.recent) return 0xffffffffu;
+    return weight == weight ? dist_key(weight) : 0u;
+}
+
+// One workgroup to a (sequence, kv head).  The budget-th largest claim is found digit by digit (11, 11, 10 bits) from
+// counts in LDS; each wave then lists, in order, the slots below the budget that fall free and the kept ones behind it.
+__global__ __launch_bounds__(kEvictThreads) void kv_select_kernel(KvView c, KvEvict e)
+{
+    const int b = (int)blockIdx.x / c.heads;
+    const int tid = (int)threadIdx.x, lane = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t stride = (int64_t)c.width << c.page_shift, dense = (int64_t)blockIdx.x * stride;
+    const int n = (int)max((int64_t)0, min((int64_t)c.lengths[b], stride));
+    const int seen = e.seen ? e.seen[b] : n;
+    int32_t *kept = e.kept + (int64_t)blockIdx.x * e.budget;
+    const int budget = e.budget;
+    if (n <= budget) {
+        for (int s = tid; s < budget; s += kEvictThreads) kept[s] = s < n ? s : -1;
+        return;
+    }
+    __shared__ uint32_t counts[2048];
+    __shared__ uint32_t wave_sum[16][2];
+    __shared__ uint32_t found[2];
+    auto claim = [&](int s) { return claim_of(e, seen, e.weights[dense + s], e.positions ? e.positions[dense + s] : s); };
+
+    uint32_t prefix = 0u, known = 0u, wanted = (uint32_t)budget;  // claims whose `known` bits are `prefix`: the wanted-th of them
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+        for (int t = tid; t < 2048; t += kEvictThreads) counts[t] = 0u;
+        __syncthreads();
+        for (int s = tid; s < n; s += kEvictThreads) {
+            const uint32_t x = claim(s);
+            if ((x & known) == prefix) atomicAdd(&counts[(x >> shift) & (bins - 1)], 1u);
+        }
+        __syncthreads();
+        // the bins from the largest down, two to a thread
+        const uint32_t hi = counts[2047 - 2 * tid], lo = counts[2046 - 2 * tid];
+        uint32_t upto = hi + lo;
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t y = (uint32_t)__shfl_up((int)upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 63) wave_sum[wave][0] = upto;
+        __syncthreads();
+        uint32_t before = 0u;
+        for (int w = 0; w < wave; ++w) before += wave_sum[w][0];
+        upto += before;
+        const uint32_t from = upto - hi - lo;
+        if (from < wanted && wanted <= upto) {
+            const bool first = wanted <= from + hi;
+            found[0] = (uint32_t)(first ? 2047 - 2 * tid : 2046 - 2 * tid);
+            found[1] = wanted - (first ? from : from + hi);
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        known |= (uint32_t)(bins - 1) << shift;
+        wanted = found[1];
+        __syncthreads();
+    }
+    // kept: claims above `prefix`, and the first `wanted` of those equal to it.  Each wave has a run of slots.
+    const int run = (n + 1023) / 1024 * 64, begin = min(n, wave * run), end = min(n, begin + run);
+    uint32_t equal = 0u;
+    for (int s = begin + lane; s - lane < end; s += 64) equal += (uint32_t)__popcll(ballot64(s < end && claim(s) == prefix));
+    if (lane == 0) wave_sum[wave][0] = equal;
+    __syncthreads();
+    uint32_t equal_before = 0u;
+    for (int w = 0; w < wave; ++w) equal_before += wave_sum[w][0];
+    __syncthreads();
+    int32_t *holes = e.holes + (int64_t)blockIdx.x * budget, *later = e.later + (int64_t)blockIdx.x * budget;
+    for (int write = 0; write < 2; ++write) {  // first the numbers of either kind, then the lists
+        uint32_t eq = equal_before, nh = 0u, nl = 0u;
+        if (write) {
+            for (int w = 0; w < wave; ++w) {
+                nh += wave_sum[w][0];
+                nl += wave_sum[w][1];
+            }
+        }
+        for (int s = begin + lane; s - lane < end; s += 64) {
+            const uint32_t x = s < end ? claim(s) : 0u;
+            const bool same = s < end && x == prefix;
+            const uint64_t sames = ballot64(same);
+            const bool stays = s < end && (x > prefix || (same && eq + (uint32_t)prefix_count(sames) < wanted));
+            eq += (uint32_t)__popcll(sames);
+            const bool is_hole = s < end && s < budget && !stays, is_later = stays && s >= budget;
+            const uint64_t hs = ballot64(is_hole), ls = ballot64(is_later);
+            if (write) {
+                if (s < budget && s < end && stays) kept[s] = s;
+                if (is_hole) holes[nh + (uint32_t)prefix_count(hs)] = s;
+                if (is_later) later[nl + (uint32_t)prefix_count(ls)] = s;
+            }
+            nh += (uint32_t)__popcll(hs);
+            nl += (uint32_t)__popcll(ls);
+        }
+        if (!write) {
+            if (lane == 0) {
+                wave_sum[wave][0] = nh;
+                wave_sum[wave][1] = nl;
+            }
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+    uint32_t all = 0u;
+    for (int w = 0; w < 16; ++w) all += wave_sum[w][0];
+    for (uint32_t j = (uint32_t)tid; j < all; j += kEvictThreads) kept[holes[j]] = later[j];
+}
+
+// Sixteen lanes to a kept slot: its position and weight, and, where it comes from behind the budget, its codes.
+// Sources lie at and behind the budget, targets below it: no order is needed.
+__global__ __launch_bounds__(256) void kv_move_kernel(KvView c, KvEvict e)
+{
+    const int64_t all = (int64_t)c.batch * c.heads * e.budget;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int part = (int)threadIdx.x & 15;
+    if (item >= all) return;
+    const int64_t bh = item / e.budget, stride = (int64_t)c.width << c.page_shift;
+    const int to = (int)(item % e.budget), from = e.kept[item];
+    const int b = (int)(bh / c.heads), head = (int)(bh % c.heads);
+    if (part == 0) {
+        const int pos = from < 0 ? -1 : e.positions ? e.positions[bh * stride + from] : from;
+        const float weight = from < 0 ? 0.f : e.weights[bh * stride + from];
+        if (e.positions_out) e.positions_out[bh * e.out_stride + to] = pos;
+        e.weights_out[bh * e.out_stride + to] = weight;
+        if (to == 0 && head == 0)  // the one thread that reads this length: it may be the same array
+            e.lengths_out[b] = (int32_t)max((int64_t)0, min(min((int64_t)c.lengths[b], stride), (int64_t)e.budget));
+    }
+    if (from < 0 || from == to) return;
+    const int p0 = page_of(c, b, from), p1 = page_of(c, b, to);
+    if (p0 < 0 || p1 < 0) return;
+    const int in_page = (1 << c.page_shift) - 1;
+    const int64_t src = (((int64_t)p0 * c.heads + head) << c.page_shift) + (from & in_page);
+    const int64_t dst = (((int64_t)p1 * c.heads + head) << c.page_shift) + (to & in_page);
+    const int codes = c.dim / 2, scales = c.dim / 32;  // bytes
+    // 32, 64 or 128 bytes of codes: 2, 4 or 8 to a lane; 2, 4 or 8 of scales: one to a lane
+    if (codes == 32) {
+        ((uint16_t *)(c.k_codes + dst * codes))[part] = ((const uint16_t *)(c.k_codes + src * codes))[part];
+        ((uint16_t *)(c.v_codes + dst * codes))[part] = ((const uint16_t *)(c.v_codes + src * codes))[part];
+    } else if (codes == 64) {
+        ((uint32_t *)(c.k_codes + dst * codes))[part] = ((const uint32_t *)(c.k_codes + src * codes))[part];
+        ((uint32_t *)(c.v_codes + dst * codes))[part] = ((const uint32_t *)(c.v_codes + src * codes))[part];
+    } else {
+        ((u32x2 *)(c.k_codes + dst * codes))[part] = ((const u32x2 *)(c.k_codes + src * codes))[part];
+        ((u32x2 *)(c.v_codes + dst * codes))[part] = ((const u32x2 *)(c.v_codes + src * codes))[part];
+    }
+    if (part < scales) {
+        c.k_scales[dst * scales + part] = c.k_scales[src * scales + part];
+        c.v_scales[dst * scales + part] = c.v_scales[src * scales + part];
+    }
+}
+
+template <int DT, int D>
+int run_append(const KvView &c, const KvRows &r, hipStream_t s)
+{
+    const int64_t blocks = ((int64_t)r.nrows * c.heads * (D / 8) + 255) / 256;
+    kv_append_kernel<DT, D><<<(uint32_t)blocks, 256, 0, s>>>(c, r);
+    PSC_HIP_TRY(hipGetLastError());
+    return PSC_OK;
+}
+template <int DT, int D>
+int run_read(const KvView &c, const KvRows &r, void *k, void *v, hipStream_t s)
+{
+    const int64_t blocks = ((int64_t)r.nrows * c.heads * (D / 8) + 255) / 256;
+    kv_read_kernel<DT, D><<<(uint32_t)blocks, 256, 0, s>>>(c, r, k, v);
+    PSC_HIP_TRY(hipGetLastError());
+    return PSC_OK;
+}
+
+// Rows of a workgroup that shares them (tokens split over its waves), and of one whose waves have their own.
+template <int DT, int D>
+constexpr int most_row_tiles()
+{
+    return DT == PSC_F32 ? (D == 256 ? 1 : 2) : D == 256 ? 2 : 4;
+}
+
+template <int DT, int D>
+int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const float *given, float *received, hipStream_t s)
+{
+    constexpr int kMost = most_row_tiles<DT, D>();
+    if (q.nrows > 0) {
+        const dim3 grid((uint32_t)p.splits, (uint32_t)p.row_groups, (uint32_t)(c.batch * c.heads));
+        if (!p.split_tokens) kv_attention_kernel<D, DT, kMost, false><<<grid, 256, 0, s>>>(c, q);
+        else if (p.row_tiles == 1) kv_attention_kernel<D, DT, 1, true><<<grid, 256, 0, s>>>(c, q);
+        else if constexpr (kMost >= 2) kv_attention_kernel<D, DT, 2, true><<<grid, 256, 0, s>>>(c, q);
+        PSC_HIP_TRY(hipGetLastError());
+        if (p.splits > 1) {
+            kv_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * q.q_heads + 15) / 16), 256, 0, s>>>(q);
+            PSC_HIP_TRY(hipGetLastError());
+        }
+    }
+    if (received) {
+        const int64_t slots = (int64_t)c.width << c.page_shift;
+        kv_weights_kernel<D, DT><<<dim3((uint32_t)((slots + 127) / 128), 1, (uint32_t)(c.batch * c.heads)), 256, 0, s>>>(c, q, given, received);
+        PSC_HIP_TRY(hipGetLastError());
+    }
+    return PSC_OK;
+}
+
+#define PSC_KV_DISPATCH(fn, dtype, dim, ...)                                   \
+    (dim == 64    ? (dtype == PSC_BF16  ? fn<PSC_BF16, 64>(__VA_ARGS__)        \
+                     : dtype == PSC_F16 ? fn<PSC_F16, 64>(__VA_ARGS__)         \
+                                        : fn<PSC_F32, 64>(__VA_ARGS__))        \
+     : dim == 128 ? (dtype == PSC_BF16  ? fn<PSC_BF16, 128>(__VA_ARGS__)       \
+                     : dtype == PSC_F16 ? fn<PSC_F16, 128>(__VA_ARGS__)        \
+                                        : fn<PSC_F32, 128>(__VA_ARGS__))       \
+                  : (dtype == PSC_BF16  ? fn<PSC_BF16, 256>(__VA_ARGS__)       \
+                     : dtype == PSC_F16 ? fn<PSC_F16, 256>(__VA_ARGS__)        \
+                                        : fn<PSC_F32, 256>(__VA_ARGS__)))
+
+}  // namespace
+
+int launch_kv_append(const KvView &c, int dtype, const KvRows &r, hipStream_t s)
+{
+    return PSC_KV_DISPATCH(run_append, dtype, c.dim, c, r, s);
+}
+
+int launch_kv_read(const KvView &c, int dtype, const KvRows &r, void *k_out, void *v_out, hipStream_t s)
+{
+    return PSC_KV_DISPATCH(run_read, dtype, c.dim, c, r, k_out, v_out, s);
+}
+
+KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered, bool weights)
+{
+    KvPlan p;
+    const int64_t m = (int64_t)max_rows * group, q_heads = (int64_t)group * c.heads;
+    const int most = dtype == PSC_F32 ? (c.dim == 256 ? 1 : 2) : c.dim == 256 ? 2 : 4;
+    // Waves with rows of their own pay once most of them have some.
+    p.split_tokens = m <= 4 * 16 * most / 2;
+    p.row_tiles = !p.split_tokens ? most : std::min(most, m <= 16 ? 1 : 2);
+    const int64_t rows_each = (int64_t)16 * p.row_tiles * (p.split_tokens ? 1 : 4);
+    p.row_groups = (m + rows_each - 1) / rows_each;
+    // blocks of 32 tokens that a group of rows can see at most
+    int64_t blocks = (((int64_t)c.width << c.page_shift) + 31) / 32;
+    if (ordered && window > 0) {
+        const int64_t per_wave = p.split_tokens ? rows_each : rows_each / 4;
+        blocks = std::min(blocks, ((int64_t)window + per_wave / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
+    }
+    const int64_t units = std::max<int64_t>(1, p.row_groups * c.batch * c.heads), wanted = 2048;
+    const int least = p.split_tokens ? 4 : 16;  // blocks that are worth a workgroup
+    p.splits = std::max<int64_t>(1, std::min((wanted + units - 1) / units, blocks / least));
+    p.split_blocks = std::max<int64_t>(1, (blocks + p.splits - 1) / p.splits);
+    if (p.split_tokens) p.split_blocks = (p.split_blocks + 3) / 4 * 4;
+    p.splits = std::max<int64_t>(1, (blocks + p.split_blocks - 1) / p.split_blocks);
+    const int64_t rows = nrows * q_heads;
+    p.part_stat_bytes = p.splits > 1 ? (size_t)(p.splits * rows * 8 + 255) / 256 * 256 : 0;
+    p.part_acc_bytes = p.splits > 1 ? (size_t)(p.splits * rows * c.dim * 4 + 255) / 256 * 256 : 0;
+    p.stat_bytes = weights ? (size_t)(rows * 8 + 255) / 256 * 256 : 0;
+    return p;
+}
+
+int launch_kv_attention(const KvView &c, int dtype, const KvQueries &q, const KvPlan &p, const float *given, float *received, hipStream_t s)
+{
+    return PSC_KV_DISPATCH(run_attention, dtype, c.dim, c, q, p, given, received, s);
+}
+
+int launch_kv_evict(const KvView &c, const KvEvict &e, hipStream_t s)
+{
+    kv_select_kernel<<<(uint32_t)(c.batch * c.heads), kEvictThreads, 0, s>>>(c, e);
+    PSC_HIP_TRY(hipGetLastError());
+    const int64_t items = (int64_t)c.batch * c.heads * e.budget;
+    kv_move_kernel<<<(uint32_t)((items + 15) / 16), 256, 0, s>>>(c, e);
+    PSC_HIP_TRY(hipGetLastError());
+    return PSC_OK;
+}
+
+}  // namespace psc
