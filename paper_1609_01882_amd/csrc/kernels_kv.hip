@@ -251,9 +251,18 @@ __device__ __forceinline__ Blocks blocks_of(const KvQueries &q, int n, int lo_po
 template <int D>
 struct Raw {
     uint32_t k[2][D / 32], ks[2];
-    uint32_t v[8][D == 256 ? 2 : 1], vs[8];
-    int pos[8];  // positions of the value tokens, where they have some of their own
+    uint32_t v[8][D == 256 ? 2 : 1];
+    uint32_t vs[2][4];  // of the tokens' scale bytes the words that hold the lane's (value_scale)
+    int pos[8];         // positions of the value tokens, where they have some of their own
 };
+// The lane's scale byte of token r of four.
+template <int D>
+__device__ __forceinline__ uint32_t value_scale(const uint32_t (&vs)[4], int r, int i)
+{
+    if constexpr (D == 64) return vs[r >> 1] >> ((r & 1) * 16 + (i >> 3) * 8) & 255u;
+    else if constexpr (D == 128) return vs[r] >> ((i >> 2) * 8) & 255u;
+    else return vs[r];
+}
 
 template <int D>
 __device__ __forceinline__ void load_keys(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (&k)[D / 32], uint32_t &ks)
@@ -281,7 +290,7 @@ __device__ __forceinline__ void load_keys(const KvView &c, int head, int page, i
 }
 
 template <int D>
-__device__ __forceinline__ void load_values(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (*v)[D == 256 ? 2 : 1], uint32_t *vs)
+__device__ __forceinline__ void load_values(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (*v)[D == 256 ? 2 : 1], uint32_t (&vs)[4])
 {
     const int64_t at = (((int64_t)page * c.heads + head) << c.page_shift) + in_page;
     const uint8_t *p = c.v_codes + at * (D / 2), *s = c.v_scales + at * (D / 32);
@@ -295,7 +304,16 @@ __device__ __forceinline__ void load_values(const KvView &c, int head, int page,
             v[r][0] = t.x;
             v[r][1] = t.y;
         }
-        vs[r] = s[(uint32_t)((g * 4 + r) * (D / 32) + i * (D / 16) / 32)];
+        if constexpr (D == 256) vs[r] = s[(uint32_t)((g * 4 + r) * 8 + (i >> 1))];
+    }
+    if constexpr (D == 64) {
+        const u32x2 t = *(const u32x2 *)(s + (uint32_t)(g * 8));
+        vs[0] = t.x;
+        vs[1] = t.y;
+    } else if constexpr (D == 128) {
+        const u32x4 t = *(const u32x4 *)(s + (uint32_t)(g * 16));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) vs[r] = t[r];
     }
 }
 
@@ -394,14 +412,14 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // coordinates of 8 tokens and pairs up the tokens' values of one coordinate with one permutation each.
 // Scores, maximum, sum and output are 32-bit floats.  Probabilities are rounded to float16 (at most 2^-11 of each, an
 // eighth of what the output's own rounding to bfloat16 may add); for float32 rows two float16 hold 22 bits.
-template <int D, int DT, int RT>
+template <int D, int DT, int RT, bool kPos>
 struct Attention {
     f32x4 acc[RT][D / 16];
     float top[RT], sum[RT];  // of the scaled scores in units of log 2; the sum is the lane's own share
     Rows<D, DT> rows[RT];
 
     __device__ void block(const KvView &c, const KvQueries &q, const Raw<D> &raw, const RowMask (&mask)[RT], int slot, int lim0,
-                          int lim1, bool whole, float factor, int g)
+                          int lim1, bool whole, float factor, int i, int g)
     {
         f32x4 s[RT][2];
 #pragma unroll
@@ -418,7 +436,7 @@ struct Attention {
                 for (int r = 0; r < 4; ++r) {
                     const int at = slot + 16 * h + 4 * g + r;
                     const bool there = at < (h ? lim1 : lim0);
-                    const int pos = q.positions ? raw.pos[4 * h + r] : at;
+                    const int pos = kPos ? raw.pos[4 * h + r] : at;
 #pragma unroll
                     for (int t = 0; t < RT; ++t)
                         if (!(there && sees(q, mask[t], pos))) s[t][h][r] = kNegInf;
@@ -463,8 +481,11 @@ struct Attention {
         uint32_t held[8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const int at = slot + (t < 4 ? 4 * g + t : 12 + 4 * g + t);
-            held[t] = whole || at < (t < 4 ? lim0 : lim1) ? raw.vs[t] : 0u;  // what lies past the end may be NaN: scale 2^-127, zeros in float16
+            held[t] = value_scale<D>(raw.vs[t >> 2], t & 3, i);
+        }
+        if (!whole) {  // what lies past the end may be NaN: with the scale 2^-127 it is zeros in float16
+#pragma unroll
+            for (int t = 0; t < 8; ++t) held[t] = slot + (t < 4 ? 4 * g + t : 12 + 4 * g + t) < (t < 4 ? lim0 : lim1) ? held[t] : 0u;
         }
         constexpr int kBytes = D / 32;  // code bytes of a token in this lane
 #pragma unroll
@@ -497,7 +518,7 @@ struct Attention {
 
 // kSplitTokens: the workgroup's four waves share 16 RT rows, every fourth block each, and are joined in LDS; otherwise
 // each wave has 16 RT rows of its own and all blocks.
-template <int D, int DT, int RT, bool kSplitTokens>
+template <int D, int DT, int RT, bool kSplitTokens, bool kPos>
 __global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
@@ -514,7 +535,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q
     const int begin = (int)blockIdx.x * q.split_blocks, end = min(count, begin + q.split_blocks);
     const int step = kSplitTokens ? 4 : 1;
 
-    Attention<D, DT, RT> a;
+    Attention<D, DT, RT, kPos> a;
     RowMask mask[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -527,25 +548,24 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q
     }
     const int64_t dense = ((int64_t)b * c.heads + head) * ((int64_t)c.width << c.page_shift);
 
-    // the block that is being worked on, the one whose codes are on their way, the one whose pages are
-    Raw<D> raw;
-    int pages[2] = {-1, -1}, slot = 0, lim[2] = {0, 0};
-    auto find_pages = [&](int at, int (&pg)[2]) {
-        if (at >= end) return;
-        const int sl = blocks.block(at) * 32;
-        pg[0] = page_of(c, b, sl);
-        pg[1] = sl + 16 < s.n ? page_of(c, b, sl + 16) : -1;
+    // The wave's blocks are those at begin + wave (or 0), and every `step` further.  The pages of 32 of them are held across
+    // the lanes; the codes of the block after the one that is worked on are on their way, without a branch around their
+    // loads (past the last block: of a page that is there).
+    const int own = begin + (kSplitTokens ? wave : 0), mine = end > own ? (end - own + step - 1) / step : 0;
+    auto pages_from = [&](int k) {
+        const int at = min(own + (k + (lane >> 1)) * step, end - 1), sl = blocks.block(at) * 32 + (lane & 1) * 16;
+        const int page = c.table[(int64_t)b * c.width + min(sl >> c.page_shift, c.width - 1)];
+        return sl < s.n && (uint32_t)page < (uint32_t)c.pages ? page : -1;
     };
-    auto load = [&](int at, const int (&pg)[2], Raw<D> &r) {
-        if (at >= end) return;
-        const int sl = blocks.block(at) * 32, mask_page = (1 << c.page_shift) - 1;
+    auto load = [&](int k, const int (&pg)[2], Raw<D> &r) {
+        const int sl = blocks.block(min(own + k * step, end - 1)) * 32, in_page = (1 << c.page_shift) - 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int page = max(pg[h], 0);
-            load_keys<D>(c, head, page, (sl + 16 * h) & mask_page, i, g, r.k[h], r.ks[h]);
-            load_values<D>(c, head, page, (sl + 16 * h) & mask_page, i, g, &r.v[4 * h], &r.vs[4 * h]);
-            if (q.positions && sl + 16 * h < s.n) {
-                const int4 x = *(const int4 *)(q.positions + dense + sl + 16 * h + 4 * g);
+            load_keys<D>(c, head, page, (sl + 16 * h) & in_page, i, g, r.k[h], r.ks[h]);
+            load_values<D>(c, head, page, (sl + 16 * h) & in_page, i, g, &r.v[4 * h], r.vs[h]);
+            if constexpr (kPos) {
+                const int4 x = *(const int4 *)(q.positions + dense + min(sl + 16 * h, (c.width << c.page_shift) - 16) + 4 * g);
                 r.pos[4 * h] = x.x;
                 r.pos[4 * h + 1] = x.y;
                 r.pos[4 * h + 2] = x.z;
@@ -553,28 +573,34 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q
             }
         }
     };
-    int at = begin + (kSplitTokens ? wave : 0);
-    find_pages(at, pages);
-    load(at, pages, raw);
-    int next_pages[2] = {-1, -1};
-    find_pages(at + step, next_pages);
-    for (; at < end; at += step) {
-        Raw<D> next = raw;
-        load(at + step, next_pages, next);
-        int then[2] = {-1, -1};
-        find_pages(at + 2 * step, then);
-        slot = blocks.block(at) * 32;
-        lim[0] = pages[0] >= 0 ? s.n : 0;
-        lim[1] = pages[1] >= 0 ? s.n : 0;
-        const bool there = slot + 32 <= s.n && pages[0] >= 0 && pages[1] >= 0 && !q.positions;
-        const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
-                           (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-        a.block(c, q, raw, mask, slot, lim[0], lim[1], whole, q.factor, g);
-        raw = next;
-        pages[0] = next_pages[0];
-        pages[1] = next_pages[1];
-        next_pages[0] = then[0];
-        next_pages[1] = then[1];
+    if (mine > 0) {
+        Raw<D> raw;
+        int ids = pages_from(0), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
+        load(0, pages, raw);
+        for (int k0 = 0; k0 < mine; k0 += 32) {
+            const int ids_then = pages_from(k0 + 32), k_end = min(32, mine - k0);
+            for (int k = 0; k < k_end; ++k) {
+                int next_pages[2];
+                if (k < 31) {
+                    next_pages[0] = __builtin_amdgcn_readlane(ids, 2 * k + 2);
+                    next_pages[1] = __builtin_amdgcn_readlane(ids, 2 * k + 3);
+                } else {
+                    next_pages[0] = __builtin_amdgcn_readlane(ids_then, 0);
+                    next_pages[1] = __builtin_amdgcn_readlane(ids_then, 1);
+                }
+                Raw<D> next;
+                load(k0 + k + 1, next_pages, next);
+                const int slot = blocks.block(own + (k0 + k) * step) * 32;
+                const bool there = slot + 32 <= s.n && pages[0] >= 0 && pages[1] >= 0 && !kPos;
+                const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
+                                   (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
+                a.block(c, q, raw, mask, slot, pages[0] >= 0 ? s.n : 0, pages[1] >= 0 ? s.n : 0, whole, q.factor, i, g);
+                raw = next;
+                pages[0] = next_pages[0];
+                pages[1] = next_pages[1];
+            }
+            ids = ids_then;
+        }
     }
     const bool parts = q.splits > 1;
 #pragma unroll
@@ -676,36 +702,56 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q
     }
 }
 
-// Joins a row's parts: 16 lanes to a row.
+// Joins a row's parts, a wave to a row: each lane takes a part's maximum and sum (64 parts at a time), then the lanes take
+// D / 16 coordinates of every fourth part each.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
 {
-    const int64_t all = (int64_t)q.nrows * q.q_heads, row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int part = (int)threadIdx.x & 15;
+    const int lane = lane_id(), part = lane & 15, quarter = lane >> 4;
+    const int64_t all = (int64_t)q.nrows * q.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= all) return;
     float top = kNegInf, sum = 0.f, x[D / 16];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) x[j] = 0.f;
-    for (int p = 0; p < q.splits; ++p) {
-        const float2 st = *(const float2 *)(q.part_stat + (p * all + row) * 2);
-        if (st.y == 0.f) continue;  // nothing seen there
-        const float now = fmaxf(top, st.x);
-        const float mine = now == kNegInf ? 1.f : exp2_fast(top - now), theirs = now == kNegInf ? 1.f : exp2_fast(st.x - now);
-        float y[D / 16];
-        load_row<PSC_F32, D / 16>(q.part_acc + (p * all + row) * D + part * (D / 16), y);
+    for (int p0 = 0; p0 < q.splits; p0 += 64) {
+        float2 st = make_float2(kNegInf, 0.f);
+        if (p0 + lane < q.splits) st = *(const float2 *)(q.part_stat + ((p0 + lane) * all + row) * 2);
+        float now = top;
+        if (st.y != 0.f) now = fmaxf(now, st.x);
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) x[j] = __builtin_fmaf(x[j], mine, y[j] * theirs);
-        sum = __builtin_fmaf(sum, mine, st.y * theirs);
+        for (int d = 1; d < 64; d *= 2) now = fmaxf(now, __shfl_xor(now, d));
+        const float shrink = now == kNegInf ? 1.f : exp2_fast(top - now);
+        const float theirs = st.y == 0.f ? 0.f : now == kNegInf ? 1.f : exp2_fast(st.x - now);
+        float add = st.y * theirs;  // (a part that saw nothing: 0)
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) add += __shfl_xor(add, d);
+        sum = __builtin_fmaf(sum, shrink, add);
         top = now;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) x[j] *= shrink;
+        const int last = min(64, q.splits - p0);
+        for (int p = quarter; p < last; p += 4) {
+            const float w = __shfl(theirs, p);
+            if (w == 0.f) continue;  // (its sums were not written)
+            float y[D / 16];
+            load_row<PSC_F32, D / 16>(q.part_acc + ((p0 + p) * all + row) * D + part * (D / 16), y);
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) x[j] = __builtin_fmaf(y[j], w, x[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+        x[j] += __shfl_xor(x[j], 16);
+        x[j] += __shfl_xor(x[j], 32);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (part == 0) {
+    if (lane == 0) {
         if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (top + __log2f(sum)) * kLn2;
         if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(top == kNegInf ? 0.f : top, inv);
     }
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) x[j] *= inv;
-    store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
+    if (quarter == 0) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
 }
 
 // The weight that every token received: scores once more, from the same products as in the attention itself, so that
@@ -965,12 +1011,18 @@ int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const fl
     constexpr int kMost = most_row_tiles<DT, D>();
     if (q.nrows > 0) {
         const dim3 grid((uint32_t)p.splits, (uint32_t)p.row_groups, (uint32_t)(c.batch * c.heads));
-        if (!p.split_tokens) kv_attention_kernel<D, DT, kMost, false><<<grid, 256, 0, s>>>(c, q);
-        else if (p.row_tiles == 1) kv_attention_kernel<D, DT, 1, true><<<grid, 256, 0, s>>>(c, q);
-        else if constexpr (kMost >= 2) kv_attention_kernel<D, DT, 2, true><<<grid, 256, 0, s>>>(c, q);
+        if (q.positions) {
+            if (!p.split_tokens) kv_attention_kernel<D, DT, kMost, false, true><<<grid, 256, 0, s>>>(c, q);
+            else if (p.row_tiles == 1) kv_attention_kernel<D, DT, 1, true, true><<<grid, 256, 0, s>>>(c, q);
+            else if constexpr (kMost >= 2) kv_attention_kernel<D, DT, 2, true, true><<<grid, 256, 0, s>>>(c, q);
+        } else {
+            if (!p.split_tokens) kv_attention_kernel<D, DT, kMost, false, false><<<grid, 256, 0, s>>>(c, q);
+            else if (p.row_tiles == 1) kv_attention_kernel<D, DT, 1, true, false><<<grid, 256, 0, s>>>(c, q);
+            else if constexpr (kMost >= 2) kv_attention_kernel<D, DT, 2, true, false><<<grid, 256, 0, s>>>(c, q);
+        }
         PSC_HIP_TRY(hipGetLastError());
         if (p.splits > 1) {
-            kv_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * q.q_heads + 15) / 16), 256, 0, s>>>(q);
+            kv_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * q.q_heads + 3) / 4), 256, 0, s>>>(q);
             PSC_HIP_TRY(hipGetLastError());
         }
     }
