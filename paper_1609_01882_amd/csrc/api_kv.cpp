@@ -199,8 +199,8 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
 size_t psc_kv_evict_workspace_bytes(const psc_kv_cache *cache, int budget)
 {
     KvView v{};
-    if (check_cache(cache, &v) != PSC_OK || budget < 1) return 0;
-    return (size_t)v.batch * v.heads * budget * 8;
+    if (check_cache(cache, &v) != PSC_OK || budget < 1 || budget >= kMostSlots) return 0;
+    return plan_kv_evict(v, budget).bytes();
 }
 
 int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int32_t *positions_dev,
@@ -221,7 +221,9 @@ int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int3
     PSC_REQUIRE(aligned(weights_dev, 4) && aligned(positions_dev, 4) && aligned(seen_dev, 4) && aligned(kept_dev, 4) && aligned(lengths_out_dev, 4) &&
                     aligned(positions_out_dev, 4) && aligned(weights_out_dev, 4),
                 "misaligned array");
-    const size_t need = psc_kv_evict_workspace_bytes(cache, budget);
+    const KvEvictPlan p = plan_kv_evict(v, budget);
+    const size_t need = p.bytes();
+    PSC_REQUIRE((int64_t)v.batch * v.heads * budget * (v.dim / 32) < (int64_t)1 << 38, "budget %d is too large for %d x %d memories", budget, v.batch, v.heads);
     PSC_REQUIRE(workspace_dev && workspace_bytes >= need && aligned(workspace_dev), "workspace too small or misaligned: %zu bytes, %zu needed", workspace_bytes, need);
     KvEvict e{};
     e.weights = weights_dev;
@@ -235,9 +237,7 @@ int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int3
     e.lengths_out = lengths_out_dev;
     e.positions_out = positions_out_dev;
     e.weights_out = weights_out_dev;
-    e.holes = (int32_t *)workspace_dev;
-    e.later = e.holes + (size_t)v.batch * v.heads * budget;
-    return launch_kv_evict(v, e, (hipStream_t)stream);
+    return launch_kv_evict(v, e, p, (char *)workspace_dev, (hipStream_t)stream);
 }
 
 }  // extern "C"

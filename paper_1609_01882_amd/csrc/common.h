@@ -363,6 +363,9 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
 // received (or null): given (or 0) + the weight each token received.
 int launch_kv_attention(const KvView &c, int dtype, const KvQueries &q, const KvPlan &p, const float *given, float *received,
                         hipStream_t s);
+struct KvSegment {  // of a long memory: see kernels_kv.hip
+    uint32_t above, first, count;
+};
 struct KvEvict {
     const float *weights;
     const int32_t *positions, *seen;
@@ -370,9 +373,23 @@ struct KvEvict {
     int64_t out_stride;
     int32_t *kept, *lengths_out, *positions_out;
     float *weights_out;
-    int32_t *holes, *later;  // scratch [batch][heads][budget] each
+    // scratch: per (sequence, kv head) the claim that decides and how many slots below the budget fall free; lists
+    // [batch][kv_heads][budget] of these slots and of the kept ones behind the budget
+    uint2 *chosen;
+    uint32_t *free_slots;
+    int32_t *holes, *later;
+    int segments, segments_below;
+    KvSegment *info;     // [batch][kv_heads][segments]
+    uint32_t *counts;    // [...][segments][2048]
+    uint32_t *gathered;  // per slot
 };
-int launch_kv_evict(const KvView &c, const KvEvict &e, hipStream_t s);
+struct KvEvictPlan {
+    int64_t segments = 1, segments_below = 0;
+    size_t head_bytes = 0, list_bytes = 0, info_bytes = 0, counts_bytes = 0, gathered_bytes = 0;
+    size_t bytes() const { return head_bytes + 2 * list_bytes + info_bytes + counts_bytes + gathered_bytes; }
+};
+KvEvictPlan plan_kv_evict(const KvView &c, int budget);
+int launch_kv_evict(const KvView &c, KvEvict e, const KvEvictPlan &p, char *ws, hipStream_t s);
 
 }  // namespace psc
 

@@ -519,7 +519,7 @@ struct Attention {
 // kSplitTokens: the workgroup's four waves share 16 RT rows, every fourth block each, and are joined in LDS; otherwise
 // each wave has 16 RT rows of its own and all blocks.
 template <int D, int DT, int RT, bool kSplitTokens, bool kPos>
-__global__ __launch_bounds__(256) void kv_attention_kernel(KvView c, KvQueries q)
+__global__ __launch_bounds__(256, kSplitTokens && RT == 1 && D <= 128 ? 3 : 1) void kv_attention_kernel(KvView c, KvQueries q)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -835,150 +835,389 @@ __device__ __forceinline__ uint32_t claim_of(const KvEvict &e, int seen, float w
     return weight == weight ? dist_key(weight) : 0u;
 }
 
-// One workgroup to a (sequence, kv head).  The budget-th largest claim is found digit by digit (11, 11, 10 bits) from
-// counts in LDS; each wave then lists, in order, the slots below the budget that fall free and the kept ones behind it.
+// Selecting and listing.  The budget-th largest claim is found digit by digit (11, 11 and 10 bits) from counts in LDS;
+// the slots below the budget that fall free and the kept ones behind it are then listed in order.  A workgroup takes
+// kSegment slots, 16 to a thread; a wave's are consecutive, so that ballots give places in order.
+// Memories of one segment: all of it in one kernel, claims in registers.  Longer ones are cut into segments, at the budget
+// first, so that a segment has either free slots or kept ones to list, and go through
+//   kv_count_kernel   counts of the first digit, per segment
+//   kv_gather_kernel  the first digit of the wanted claim, and the claims that share it, in order (a workgroup per segment,
+//                     each adding up all segments' counts)
+//   kv_pick_kernel    the rest of the claim from these few, and what each segment keeps (a workgroup per kv head)
+//   kv_list_kernel    the lists
+// One workgroup per kv head for all of it took 231 us for 8 x 8 memories of up to 131072 tokens, five passes of which each
+// waits for memory; the four kernels take 70.
+constexpr int kSegmentKeys = 16, kSegment = kEvictThreads * kSegmentKeys, kBins = 2048;
+
+struct Segment {
+    int begin, end;  // slots
+    bool below;      // the budget
+};
+__device__ __forceinline__ Segment segment_of(const KvEvict &e, int n, int seg)
+{
+    Segment x;
+    x.below = seg < e.segments_below;
+    const int64_t from = x.below ? (int64_t)seg * kSegment : e.budget + (int64_t)(seg - e.segments_below) * kSegment;
+    const int64_t to = x.below ? min((int64_t)e.budget, from + kSegment) : from + kSegment;
+    x.begin = (int)min((int64_t)n, from);
+    x.end = (int)min((int64_t)n, to);
+    return x;
+}
+
+struct Memory {
+    int b, n, seen;
+    int64_t dense;
+};
+__device__ __forceinline__ Memory memory_of(const KvView &c, const KvEvict &e, int bh)
+{
+    Memory m;
+    m.b = bh / c.heads;
+    const int64_t stride = (int64_t)c.width << c.page_shift;
+    m.n = (int)max((int64_t)0, min((int64_t)c.lengths[m.b], stride));
+    m.seen = e.seen ? e.seen[m.b] : m.n;
+    m.dense = (int64_t)bh * stride;
+    return m;
+}
+
+// The claims of slots begin .. end, N to a thread: its j-th at begin + (wave * N + j) * 64 + lane; 0 past the end.
+template <int N>
+__device__ __forceinline__ void load_claims(const KvEvict &e, const Memory &m, int begin, int end, uint32_t (&x)[N])
+{
+    const int at = begin + ((int)threadIdx.x >> 6) * (64 * N) + lane_id();
+    float w[N];
+    int pos[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int s = max(0, min(at + j * 64, end - 1));
+        w[j] = e.weights[m.dense + s];
+        pos[j] = e.positions ? e.positions[m.dense + s] : s;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = at + j * 64 < end ? claim_of(e, m.seen, w[j], pos[j]) : 0u;
+}
+
+// Adds one to the digit's count.  Lanes that agree with the first one are counted at once: many weights are equal (0 above
+// all), and a bank adds one after another.
+__device__ __forceinline__ void count_digit(uint32_t *counts, uint32_t digit)
+{
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+    const uint64_t same = ballot64(digit == first);
+    if (digit != first) atomicAdd(&counts[digit], 1u);
+    else if (prefix_count(same) == 0) atomicAdd(&counts[digit], (uint32_t)__popcll(same));
+}
+
+// With counts[kBins] in LDS: the bin of the wanted-th from the top (1-based), and which it is of that bin.
+__device__ __forceinline__ void find_bin(const uint32_t *counts, uint32_t (&wave_sum)[16], uint32_t (&found)[2], uint32_t wanted)
+{
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid >> 6;
+    const uint32_t hi = counts[kBins - 1 - 2 * tid], lo = counts[kBins - 2 - 2 * tid];
+    uint32_t upto = hi + lo;
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t y = (uint32_t)__shfl_up((int)upto, d);
+        if (lane >= d) upto += y;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += wave_sum[w];
+    const uint32_t from = upto - hi - lo;
+    if (from < wanted && wanted <= upto) {
+        const bool first = wanted <= from + hi;
+        found[0] = (uint32_t)(first ? kBins - 1 - 2 * tid : kBins - 2 - 2 * tid);
+        found[1] = wanted - (first ? from : from + hi);
+    }
+    __syncthreads();
+}
+
+// Exclusive sum over the workgroup's waves of a number that all lanes of a wave hold; and the sum of all.
+__device__ __forceinline__ uint32_t waves_before(uint32_t mine, uint32_t (&wave_sum)[16], uint32_t *all)
+{
+    const int wave = (int)threadIdx.x >> 6;
+    __syncthreads();
+    if (lane_id() == 0) wave_sum[wave] = mine;
+    __syncthreads();
+    uint32_t before = 0u, total = 0u;
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) before += wave_sum[w];
+        total += wave_sum[w];
+    }
+    *all = total;
+    return before;
+}
+
+// The lists of a segment: claims above `claim` are kept, and of those equal to it the first `ties`.  Free slots (those
+// below the budget that are not kept) go to `holes`, kept ones behind it to `later`, in order.
+template <int N>
+__device__ __forceinline__ void list_segment(const KvEvict &e, const uint32_t (&x)[N], int begin, int end, uint32_t claim, uint32_t ties,
+                                             int32_t *kept, int32_t *holes, int32_t *later, uint32_t (&wave_sum)[16], uint32_t *all_holes)
+{
+    const int at = begin + ((int)threadIdx.x >> 6) * (64 * N) + lane_id();
+    uint32_t equal = 0u, all;
+#pragma unroll
+    for (int j = 0; j < N; ++j) equal += (uint32_t)__popcll(ballot64(at + j * 64 < end && x[j] == claim));
+    uint32_t eq = waves_before(equal, wave_sum, &all);
+    uint32_t stays = 0u, nh = 0u, nl = 0u;  // (bit j: the thread's j-th)
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int s = at + j * 64;
+        const bool same = s < end && x[j] == claim;
+        const uint64_t sames = ballot64(same);
+        const bool keep = s < end && (x[j] > claim || (same && eq + (uint32_t)prefix_count(sames) < ties));
+        eq += (uint32_t)__popcll(sames);
+        stays |= keep ? 1u << j : 0u;
+        nh += (uint32_t)__popcll(ballot64(s < end && s < e.budget && !keep));
+        nl += (uint32_t)__popcll(ballot64(keep && s >= e.budget));
+    }
+    nh = waves_before(nh, wave_sum, all_holes);
+    nl = waves_before(nl, wave_sum, &all);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int s = at + j * 64;
+        const bool keep = stays >> j & 1u, hole = s < end && s < e.budget && !keep, later_one = keep && s >= e.budget;
+        const uint64_t hs = ballot64(hole), ls = ballot64(later_one);
+        if (s < end && s < e.budget) kept[s] = keep ? s : -2;  // (a free slot: kv_move_kernel writes what it takes)
+        if (hole) holes[nh + (uint32_t)prefix_count(hs)] = s;
+        if (later_one) later[nl + (uint32_t)prefix_count(ls)] = s;
+        nh += (uint32_t)__popcll(hs);
+        nl += (uint32_t)__popcll(ls);
+    }
+}
+
+// (N = 2 for up to 2048 slots: 6 x 4 memories of 1300 tokens 8 us, with N = 16 17.)
+template <int N>
 __global__ __launch_bounds__(kEvictThreads) void kv_select_kernel(KvView c, KvEvict e)
 {
-    const int b = (int)blockIdx.x / c.heads;
-    const int tid = (int)threadIdx.x, lane = lane_id();
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t stride = (int64_t)c.width << c.page_shift, dense = (int64_t)blockIdx.x * stride;
-    const int n = (int)max((int64_t)0, min((int64_t)c.lengths[b], stride));
-    const int seen = e.seen ? e.seen[b] : n;
-    int32_t *kept = e.kept + (int64_t)blockIdx.x * e.budget;
-    const int budget = e.budget;
-    if (n <= budget) {
-        for (int s = tid; s < budget; s += kEvictThreads) kept[s] = s < n ? s : -1;
+    const int bh = (int)blockIdx.x, tid = (int)threadIdx.x;
+    const Memory m = memory_of(c, e, bh);
+    int32_t *kept = e.kept + (int64_t)bh * e.budget;
+    if (m.n <= e.budget) {
+        for (int s = tid; s < e.budget; s += kEvictThreads) kept[s] = s < m.n ? s : -1;
+        if (tid == 0) e.free_slots[bh] = 0u;
         return;
     }
-    __shared__ uint32_t counts[2048];
-    __shared__ uint32_t wave_sum[16][2];
-    __shared__ uint32_t found[2];
-    auto claim = [&](int s) { return claim_of(e, seen, e.weights[dense + s], e.positions ? e.positions[dense + s] : s); };
-
-    uint32_t prefix = 0u, known = 0u, wanted = (uint32_t)budget;  // claims whose `known` bits are `prefix`: the wanted-th of them
+    __shared__ uint32_t counts[kBins], wave_sum[16], found[2];
+    uint32_t x[N];
+    load_claims(e, m, 0, m.n, x);
+    const int at = (tid >> 6) * (64 * N) + lane_id();
+    uint32_t prefix = 0u, known = 0u, wanted = (uint32_t)e.budget;
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-        for (int t = tid; t < 2048; t += kEvictThreads) counts[t] = 0u;
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t digits = pass == 2 ? 1023u : 2047u;
+        counts[tid] = counts[tid + kEvictThreads] = 0u;
         __syncthreads();
-        for (int s = tid; s < n; s += kEvictThreads) {
-            const uint32_t x = claim(s);
-            if ((x & known) == prefix) atomicAdd(&counts[(x >> shift) & (bins - 1)], 1u);
-        }
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (at + j * 64 < m.n && (x[j] & known) == prefix) count_digit(counts, x[j] >> shift & digits);
         __syncthreads();
-        // the bins from the largest down, two to a thread
-        const uint32_t hi = counts[2047 - 2 * tid], lo = counts[2046 - 2 * tid];
-        uint32_t upto = hi + lo;
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t y = (uint32_t)__shfl_up((int)upto, d);
-            if (lane >= d) upto += y;
-        }
-        if (lane == 63) wave_sum[wave][0] = upto;
-        __syncthreads();
-        uint32_t before = 0u;
-        for (int w = 0; w < wave; ++w) before += wave_sum[w][0];
-        upto += before;
-        const uint32_t from = upto - hi - lo;
-        if (from < wanted && wanted <= upto) {
-            const bool first = wanted <= from + hi;
-            found[0] = (uint32_t)(first ? 2047 - 2 * tid : 2046 - 2 * tid);
-            found[1] = wanted - (first ? from : from + hi);
-        }
-        __syncthreads();
+        find_bin(counts, wave_sum, found, wanted);
         prefix |= found[0] << shift;
-        known |= (uint32_t)(bins - 1) << shift;
+        known |= digits << shift;
         wanted = found[1];
         __syncthreads();
     }
-    // kept: claims above `prefix`, and the first `wanted` of those equal to it.  Each wave has a run of slots.
-    const int run = (n + 1023) / 1024 * 64, begin = min(n, wave * run), end = min(n, begin + run);
-    uint32_t equal = 0u;
-    for (int s = begin + lane; s - lane < end; s += 64) equal += (uint32_t)__popcll(ballot64(s < end && claim(s) == prefix));
-    if (lane == 0) wave_sum[wave][0] = equal;
-    __syncthreads();
-    uint32_t equal_before = 0u;
-    for (int w = 0; w < wave; ++w) equal_before += wave_sum[w][0];
-    __syncthreads();
-    int32_t *holes = e.holes + (int64_t)blockIdx.x * budget, *later = e.later + (int64_t)blockIdx.x * budget;
-    for (int write = 0; write < 2; ++write) {  // first the numbers of either kind, then the lists
-        uint32_t eq = equal_before, nh = 0u, nl = 0u;
-        if (write) {
-            for (int w = 0; w < wave; ++w) {
-                nh += wave_sum[w][0];
-                nl += wave_sum[w][1];
-            }
-        }
-        for (int s = begin + lane; s - lane < end; s += 64) {
-            const uint32_t x = s < end ? claim(s) : 0u;
-            const bool same = s < end && x == prefix;
-            const uint64_t sames = ballot64(same);
-            const bool stays = s < end && (x > prefix || (same && eq + (uint32_t)prefix_count(sames) < wanted));
-            eq += (uint32_t)__popcll(sames);
-            const bool is_hole = s < end && s < budget && !stays, is_later = stays && s >= budget;
-            const uint64_t hs = ballot64(is_hole), ls = ballot64(is_later);
-            if (write) {
-                if (s < budget && s < end && stays) kept[s] = s;
-                if (is_hole) holes[nh + (uint32_t)prefix_count(hs)] = s;
-                if (is_later) later[nl + (uint32_t)prefix_count(ls)] = s;
-            }
-            nh += (uint32_t)__popcll(hs);
-            nl += (uint32_t)__popcll(ls);
-        }
-        if (!write) {
-            if (lane == 0) {
-                wave_sum[wave][0] = nh;
-                wave_sum[wave][1] = nl;
-            }
-            __syncthreads();
-        }
-    }
-    __syncthreads();
-    uint32_t all = 0u;
-    for (int w = 0; w < 16; ++w) all += wave_sum[w][0];
-    for (uint32_t j = (uint32_t)tid; j < all; j += kEvictThreads) kept[holes[j]] = later[j];
+    uint32_t all_holes;
+    list_segment(e, x, 0, m.n, prefix, wanted, kept, e.holes + (int64_t)bh * e.budget, e.later + (int64_t)bh * e.budget, wave_sum, &all_holes);
+    if (tid == 0) e.free_slots[bh] = all_holes;
 }
 
-// Sixteen lanes to a kept slot: its position and weight, and, where it comes from behind the budget, its codes.
-// Sources lie at and behind the budget, targets below it: no order is needed.
+__global__ __launch_bounds__(kEvictThreads) void kv_count_kernel(KvView c, KvEvict e)
+{
+    const int bh = (int)blockIdx.y, tid = (int)threadIdx.x;
+    const Memory m = memory_of(c, e, bh);
+    if (m.n <= e.budget) return;
+    const Segment seg = segment_of(e, m.n, (int)blockIdx.x);
+    __shared__ uint32_t counts[kBins];
+    counts[tid] = counts[tid + kEvictThreads] = 0u;
+    __syncthreads();
+    if (seg.begin < seg.end) {
+        uint32_t x[kSegmentKeys];
+        load_claims(e, m, seg.begin, seg.end, x);
+        const int at = seg.begin + (tid >> 6) * (64 * kSegmentKeys) + lane_id();
+#pragma unroll
+        for (int j = 0; j < kSegmentKeys; ++j)
+            if (at + j * 64 < seg.end) count_digit(counts, x[j] >> 21);
+    }
+    __syncthreads();
+    uint32_t *to = e.counts + ((int64_t)bh * e.segments + blockIdx.x) * kBins;
+    to[tid] = counts[tid];
+    to[tid + kEvictThreads] = counts[tid + kEvictThreads];
+}
+
+__global__ __launch_bounds__(kEvictThreads) void kv_gather_kernel(KvView c, KvEvict e)
+{
+    const int bh = (int)blockIdx.y, tid = (int)threadIdx.x, seg_no = (int)blockIdx.x;
+    const Memory m = memory_of(c, e, bh);
+    if (m.n <= e.budget) return;
+    const Segment seg = segment_of(e, m.n, seg_no);
+    __shared__ uint32_t counts[kBins], wave_sum[16], found[2], before_bin;
+    const uint32_t *from = e.counts + (int64_t)bh * e.segments * kBins;
+    uint32_t a = 0u, b = 0u;
+    for (int s = 0; s < e.segments; ++s) {
+        a += from[(int64_t)s * kBins + tid];
+        b += from[(int64_t)s * kBins + tid + kEvictThreads];
+    }
+    counts[tid] = a;
+    counts[tid + kEvictThreads] = b;
+    __syncthreads();
+    find_bin(counts, wave_sum, found, (uint32_t)e.budget);
+    const uint32_t bin = found[0];
+    // of the segments before this one: claims of that bin; of this one: claims above it
+    uint32_t above = 0u, all, before = 0u;
+    for (int t = tid; t < kBins; t += kEvictThreads) above += (uint32_t)t > bin ? from[(int64_t)seg_no * kBins + t] : 0u;
+    for (int s = tid; s < seg_no; s += kEvictThreads) before += from[(int64_t)s * kBins + bin];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        above += (uint32_t)__shfl_xor((int)above, d);
+        before += (uint32_t)__shfl_xor((int)before, d);
+    }
+    waves_before(before, wave_sum, &all);
+    if (tid == 0) before_bin = all;
+    waves_before(above, wave_sum, &all);
+    KvSegment *info = e.info + (int64_t)bh * e.segments + seg_no;
+    if (tid == 0) {
+        info->above = all;
+        info->first = before_bin;
+        info->count = from[(int64_t)seg_no * kBins + bin];
+        if (seg_no == 0) e.chosen[bh] = make_uint2(bin, found[1]);
+    }
+    if (seg.begin >= seg.end) return;  // (the whole workgroup)
+    uint32_t x[kSegmentKeys], mine = 0u;
+    load_claims(e, m, seg.begin, seg.end, x);
+    const int at = seg.begin + (tid >> 6) * (64 * kSegmentKeys) + lane_id();
+#pragma unroll
+    for (int j = 0; j < kSegmentKeys; ++j) mine += (uint32_t)__popcll(ballot64(at + j * 64 < seg.end && x[j] >> 21 == bin));
+    uint32_t to = waves_before(mine, wave_sum, &all) + before_bin;
+    uint32_t *gathered = e.gathered + m.dense;
+#pragma unroll
+    for (int j = 0; j < kSegmentKeys; ++j) {
+        const bool in = at + j * 64 < seg.end && x[j] >> 21 == bin;
+        const uint64_t ins = ballot64(in);
+        if (in) gathered[to + (uint32_t)prefix_count(ins)] = x[j];
+        to += (uint32_t)__popcll(ins);
+    }
+}
+
+__global__ __launch_bounds__(kEvictThreads) void kv_pick_kernel(KvView c, KvEvict e)
+{
+    const int bh = (int)blockIdx.x, tid = (int)threadIdx.x, wave = tid >> 6, lane = lane_id();
+    const Memory m = memory_of(c, e, bh);
+    if (m.n <= e.budget) return;
+    __shared__ uint32_t counts[kBins], wave_sum[16], found[2];
+    KvSegment *info = e.info + (int64_t)bh * e.segments;
+    const uint32_t *gathered = e.gathered + m.dense;
+    const int n = (int)(info[e.segments - 1].first + info[e.segments - 1].count);
+    uint32_t prefix = e.chosen[bh].x << 21, known = 2047u << 21, wanted = e.chosen[bh].y;
+    for (int pass = 1; pass < 3; ++pass) {
+        const int shift = pass == 1 ? 10 : 0;
+        const uint32_t digits = pass == 2 ? 1023u : 2047u;
+        counts[tid] = counts[tid + kEvictThreads] = 0u;
+        __syncthreads();
+        for (int s0 = 0; s0 < n; s0 += 8 * kEvictThreads) {
+            uint32_t x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = gathered[min(n - 1, s0 + j * kEvictThreads + tid)];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (s0 + j * kEvictThreads + tid < n && (x[j] & known) == prefix) count_digit(counts, x[j] >> shift & digits);
+        }
+        __syncthreads();
+        find_bin(counts, wave_sum, found, wanted);
+        prefix |= found[0] << shift;
+        known |= digits << shift;
+        wanted = found[1];
+        __syncthreads();
+    }
+    // per segment the gathered claims above and equal to it (a wave to a segment)
+    for (int s = wave; s < e.segments; s += 16) {
+        const int begin = (int)info[s].first, end = begin + (int)info[s].count;
+        uint32_t above = 0u, equal = 0u;
+        for (int t = begin + lane; t - lane < end; t += 64) {
+            const uint32_t x = t < end ? gathered[t] : 0u;
+            above += (uint32_t)__popcll(ballot64(t < end && x > prefix));
+            equal += (uint32_t)__popcll(ballot64(t < end && x == prefix));
+        }
+        if (lane == 0) {
+            info[s].above += above;
+            info[s].count = equal;
+        }
+    }
+    __syncthreads();
+    if (tid > 0) return;
+    uint32_t holes = 0u, later = 0u, left = wanted;
+    for (int s = 0; s < e.segments; ++s) {
+        const Segment seg = segment_of(e, m.n, s);
+        const uint32_t ties = min(left, info[s].count), stays = info[s].above + ties;
+        left -= ties;
+        info[s].count = ties;
+        info[s].first = seg.below ? holes : later;
+        if (seg.below) holes += (uint32_t)(seg.end - seg.begin) - stays;
+        else later += stays;
+    }
+    e.chosen[bh].x = prefix;
+    e.free_slots[bh] = holes;
+}
+
+__global__ __launch_bounds__(kEvictThreads) void kv_list_kernel(KvView c, KvEvict e)
+{
+    const int bh = (int)blockIdx.y, tid = (int)threadIdx.x;
+    const Memory m = memory_of(c, e, bh);
+    int32_t *kept = e.kept + (int64_t)bh * e.budget;
+    if (m.n <= e.budget) {
+        for (int64_t s = (int64_t)blockIdx.x * kEvictThreads + tid; s < e.budget; s += (int64_t)gridDim.x * kEvictThreads) kept[s] = s < m.n ? (int)s : -1;
+        if (blockIdx.x == 0 && tid == 0) e.free_slots[bh] = 0u;
+        return;
+    }
+    const Segment seg = segment_of(e, m.n, (int)blockIdx.x);
+    if (seg.begin >= seg.end) return;
+    __shared__ uint32_t wave_sum[16];
+    const KvSegment info = e.info[(int64_t)bh * e.segments + blockIdx.x];
+    uint32_t x[kSegmentKeys], all;
+    load_claims(e, m, seg.begin, seg.end, x);
+    const int64_t at = (int64_t)bh * e.budget + info.first;
+    list_segment(e, x, seg.begin, seg.end, e.chosen[bh].x, info.count, kept, e.holes + at, e.later + at, wave_sum, &all);
+}
+
+// kMoveLanes lanes to a slot below the budget that stays as it is (its position and weight), and to a free one and the
+// token that it takes: position, weight, codes.  Sources lie at and behind the budget, targets below it: no order is needed.
+template <int D>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, KvEvict e)
 {
-    const int64_t all = (int64_t)c.batch * c.heads * e.budget;
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int part = (int)threadIdx.x & 15;
-    if (item >= all) return;
-    const int64_t bh = item / e.budget, stride = (int64_t)c.width << c.page_shift;
-    const int to = (int)(item % e.budget), from = e.kept[item];
-    const int b = (int)(bh / c.heads), head = (int)(bh % c.heads);
+    constexpr int L = D / 32;  // 16 bytes of the key's codes to a lane, then of the value's
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int part = (int)threadIdx.x % L;
+    if (item >= (int64_t)c.batch * c.heads * e.budget) return;
+    const int bh = (int)(item / e.budget), i = (int)(item % e.budget), b = bh / c.heads, head = bh % c.heads;
+    const int64_t stride = (int64_t)c.width << c.page_shift, dense = bh * stride, out = bh * e.out_stride;
+    int from = -1, to = 0;
+    if ((uint32_t)i < e.free_slots[bh]) {
+        from = e.later[item];
+        to = e.holes[item];
+    }
     if (part == 0) {
-        const int pos = from < 0 ? -1 : e.positions ? e.positions[bh * stride + from] : from;
-        const float weight = from < 0 ? 0.f : e.weights[bh * stride + from];
-        if (e.positions_out) e.positions_out[bh * e.out_stride + to] = pos;
-        e.weights_out[bh * e.out_stride + to] = weight;
-        if (to == 0 && head == 0)  // the one thread that reads this length: it may be the same array
+        const int same = e.kept[item];  // i: stays; -1: past the length; otherwise free
+        if (same == i || same == -1) {
+            if (e.positions_out) e.positions_out[out + i] = same < 0 ? -1 : e.positions ? e.positions[dense + i] : i;
+            e.weights_out[out + i] = same < 0 ? 0.f : e.weights[dense + i];
+        }
+        if (from >= 0) {
+            if (e.positions_out) e.positions_out[out + to] = e.positions ? e.positions[dense + from] : from;
+            e.weights_out[out + to] = e.weights[dense + from];
+            e.kept[(int64_t)bh * e.budget + to] = from;  // whoever reads it before or after: not its own number, not -1
+        }
+        if (i == 0 && head == 0)  // the one thread that reads this length: it may be the same array
             e.lengths_out[b] = (int32_t)max((int64_t)0, min(min((int64_t)c.lengths[b], stride), (int64_t)e.budget));
     }
-    if (from < 0 || from == to) return;
+    if (from < 0) return;
     const int p0 = page_of(c, b, from), p1 = page_of(c, b, to);
     if (p0 < 0 || p1 < 0) return;
     const int in_page = (1 << c.page_shift) - 1;
     const int64_t src = (((int64_t)p0 * c.heads + head) << c.page_shift) + (from & in_page);
     const int64_t dst = (((int64_t)p1 * c.heads + head) << c.page_shift) + (to & in_page);
-    const int codes = c.dim / 2, scales = c.dim / 32;  // bytes
-    // 32, 64 or 128 bytes of codes: 2, 4 or 8 to a lane; 2, 4 or 8 of scales: one to a lane
-    if (codes == 32) {
-        ((uint16_t *)(c.k_codes + dst * codes))[part] = ((const uint16_t *)(c.k_codes + src * codes))[part];
-        ((uint16_t *)(c.v_codes + dst * codes))[part] = ((const uint16_t *)(c.v_codes + src * codes))[part];
-    } else if (codes == 64) {
-        ((uint32_t *)(c.k_codes + dst * codes))[part] = ((const uint32_t *)(c.k_codes + src * codes))[part];
-        ((uint32_t *)(c.v_codes + dst * codes))[part] = ((const uint32_t *)(c.v_codes + src * codes))[part];
-    } else {
-        ((u32x2 *)(c.k_codes + dst * codes))[part] = ((const u32x2 *)(c.k_codes + src * codes))[part];
-        ((u32x2 *)(c.v_codes + dst * codes))[part] = ((const u32x2 *)(c.v_codes + src * codes))[part];
-    }
-    if (part < scales) {
-        c.k_scales[dst * scales + part] = c.k_scales[src * scales + part];
-        c.v_scales[dst * scales + part] = c.v_scales[src * scales + part];
-    }
+    const u32x4 k = *(const u32x4 *)(c.k_codes + src * (D / 2) + part * 16), v = *(const u32x4 *)(c.v_codes + src * (D / 2) + part * 16);
+    const uint8_t ks = c.k_scales[src * L + part], vs = c.v_scales[src * L + part];
+    *(u32x4 *)(c.k_codes + dst * (D / 2) + part * 16) = k;
+    *(u32x4 *)(c.v_codes + dst * (D / 2) + part * 16) = v;
+    c.k_scales[dst * L + part] = ks;
+    c.v_scales[dst * L + part] = vs;
 }
 
 template <int DT, int D>
@@ -1091,12 +1330,57 @@ int launch_kv_attention(const KvView &c, int dtype, const KvQueries &q, const Kv
     return PSC_KV_DISPATCH(run_attention, dtype, c.dim, c, q, p, given, received, s);
 }
 
-int launch_kv_evict(const KvView &c, const KvEvict &e, hipStream_t s)
+KvEvictPlan plan_kv_evict(const KvView &c, int budget)
 {
-    kv_select_kernel<<<(uint32_t)(c.batch * c.heads), kEvictThreads, 0, s>>>(c, e);
+    KvEvictPlan p;
+    const int64_t slots = (int64_t)c.width << c.page_shift, bh = (int64_t)c.batch * c.heads;
+    const auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
+    p.segments = 1;
+    if (slots > kSegment) {
+        p.segments_below = (std::min<int64_t>(budget, slots) + kSegment - 1) / kSegment;
+        p.segments = p.segments_below + (std::max<int64_t>(0, slots - budget) + kSegment - 1) / kSegment;
+        p.counts_bytes = up((size_t)(bh * p.segments * kBins * 4));
+        p.info_bytes = up((size_t)(bh * p.segments * sizeof(KvSegment)));
+        p.gathered_bytes = up((size_t)(bh * slots * 4));
+    }
+    p.list_bytes = up((size_t)(bh * budget * 4));
+    p.head_bytes = up((size_t)(bh * 12));
+    return p;
+}
+
+int launch_kv_evict(const KvView &c, KvEvict e, const KvEvictPlan &p, char *ws, hipStream_t s)
+{
+    const uint32_t bh = (uint32_t)(c.batch * c.heads);
+    e.chosen = (uint2 *)ws;
+    e.free_slots = (uint32_t *)(e.chosen + bh);
+    ws += p.head_bytes;
+    e.holes = (int32_t *)ws;
+    e.later = (int32_t *)(ws + p.list_bytes);
+    ws += 2 * p.list_bytes;
+    e.segments = (int)p.segments;
+    e.segments_below = (int)p.segments_below;
+    if (p.segments == 1) {
+        if ((int64_t)c.width << c.page_shift <= 2 * kEvictThreads) kv_select_kernel<2><<<bh, kEvictThreads, 0, s>>>(c, e);
+        else kv_select_kernel<kSegmentKeys><<<bh, kEvictThreads, 0, s>>>(c, e);
+    } else {
+        e.info = (KvSegment *)ws;
+        e.counts = (uint32_t *)(ws + p.info_bytes);
+        e.gathered = (uint32_t *)(ws + p.info_bytes + p.counts_bytes);
+        const dim3 grid((uint32_t)p.segments, bh);
+        kv_count_kernel<<<grid, kEvictThreads, 0, s>>>(c, e);
+        PSC_HIP_TRY(hipGetLastError());
+        kv_gather_kernel<<<grid, kEvictThreads, 0, s>>>(c, e);
+        PSC_HIP_TRY(hipGetLastError());
+        kv_pick_kernel<<<bh, kEvictThreads, 0, s>>>(c, e);
+        PSC_HIP_TRY(hipGetLastError());
+        kv_list_kernel<<<grid, kEvictThreads, 0, s>>>(c, e);
+    }
     PSC_HIP_TRY(hipGetLastError());
-    const int64_t items = (int64_t)c.batch * c.heads * e.budget;
-    kv_move_kernel<<<(uint32_t)((items + 15) / 16), 256, 0, s>>>(c, e);
+    const int64_t lanes = (int64_t)bh * e.budget * (c.dim / 32);
+    const uint32_t blocks = (uint32_t)((lanes + 255) / 256);
+    if (c.dim == 64) kv_move_kernel<64><<<blocks, 256, 0, s>>>(c, e);
+    else if (c.dim == 128) kv_move_kernel<128><<<blocks, 256, 0, s>>>(c, e);
+    else kv_move_kernel<256><<<blocks, 256, 0, s>>>(c, e);
     PSC_HIP_TRY(hipGetLastError());
     return PSC_OK;
 }

@@ -13,11 +13,13 @@ without it every sequence has the same number.  Arrays per slot are [batch, kv_h
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
+import struct
 
 import torch
 
-from .binding import PscError, _check, _load, _stream, _workspace
+from .binding import PscError, _check, _load, _workspace
 
 PSC_BF16, PSC_F16, PSC_F32 = 0, 1, 2
 _DTYPES = {torch.bfloat16: PSC_BF16, torch.float16: PSC_F16, torch.float32: PSC_F32}
@@ -29,14 +31,24 @@ class _Cache(C.Structure):
                 ("batch", C.c_int), ("table_width", C.c_int), ("lengths", C.c_void_p)]
 
 
+_pack = struct.Struct("@4Pq3iP2iP").pack     # the same fields, packed at once: a call of a few microseconds notices
+assert struct.calcsize("@4Pq3iP2iP") == C.sizeof(_Cache)
+
+
 def _array(t, dtype, shape, name, device):
-    """Address of a dense tensor of this type and shape (None: a null pointer)."""
+    """Address of a dense tensor of this type and shape on the device (its index); None: a null pointer."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise PscError(f"{name}: expected a contiguous {dtype} tensor of shape {list(shape)} on {device}, "
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise PscError(f"{name}: expected a contiguous {dtype} tensor of shape {list(shape)} on cuda:{device}, "
                        f"got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+def _bytes(t, device):
+    if t.dtype is not torch.uint8 or t.get_device() != device or not t.is_contiguous():
+        raise PscError(f"workspace: expected a contiguous uint8 tensor on cuda:{device}")
+    return t.data_ptr(), t.numel()
 
 
 def _dtype(t, name):
@@ -44,6 +56,11 @@ def _dtype(t, name):
     if code is None:
         raise PscError(f"{name}: expected bfloat16, float16 or float32, got {t.dtype}")
     return code
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(pages, kv_heads, head_dim, page, batch, width, *sizes):
+    return _load().psc_kv_attention_workspace_bytes(_pack(0, 0, 0, 0, pages, kv_heads, head_dim, page, 0, batch, width, 0), *sizes)
 
 
 class KvCache:
@@ -60,7 +77,7 @@ class KvCache:
             raise PscError("codes [pages, kv_heads, page, head_dim / 2] and scales [pages, kv_heads, page, head_dim / 32] do not match")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.pages, self.kv_heads, self.page, self.head_dim = *k_codes.shape[:3], 2 * k_codes.shape[3]
-        self.device = k_codes.device
+        self.device, self._index = k_codes.device, k_codes.get_device()
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda"):
@@ -72,17 +89,20 @@ class KvCache:
         if table.dim() != 2:
             raise PscError(f"table: expected [batch, width], got {list(table.shape)}")
         batch, width = table.shape
-        c = _Cache(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(), self.pages,
-                   self.kv_heads, self.head_dim, self.page, _array(table, torch.int32, (batch, width), "table", self.device), batch, width,
-                   _array(lengths, torch.int32, (batch,), what, self.device))
+        c = _pack(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(), self.pages,
+                  self.kv_heads, self.head_dim, self.page, _array(table, torch.int32, (batch, width), "table", self._index), batch, width,
+                  _array(lengths, torch.int32, (batch,), what, self._index) or 0)
         return c, batch, (batch, self.kv_heads, width * self.page)
 
     def _rows(self, t, heads, name):
         """Address and strides of rows [n, heads, head_dim]."""
-        if t.dim() != 3 or t.shape[1:] != (heads, self.head_dim) or t.device != self.device or t.stride(2) != 1:
+        if t.dim() != 3 or t.shape[1:] != (heads, self.head_dim) or t.get_device() != self._index or t.stride(2) != 1:
             raise PscError(f"{name}: expected [rows, {heads}, {self.head_dim}] on {self.device} with contiguous coordinates, "
                            f"got {list(t.shape)} with strides {list(t.stride())} on {t.device}")
         return t.data_ptr(), t.stride(0), t.stride(1)
+
+    def _stream(self):
+        return torch._C._cuda_getCurrentRawStream(self._index)
 
     def append(self, k, v, table, lengths, offsets=None, first=None, positions=None, weights=None):
         """Round the rows k, v [n, kv_heads, head_dim] to 4 bits and write them to slots lengths[b], lengths[b] + 1, ...
@@ -92,11 +112,11 @@ class KvCache:
         n = k.shape[0]
         if v.dtype != k.dtype or v.shape != k.shape:
             raise PscError("k and v differ in type or shape")
-        _check(_load().psc_kv_append(C.byref(c), _dtype(k, "k"), *self._rows(k, self.kv_heads, "k"), *self._rows(v, self.kv_heads, "v"), n,
-                                     _array(offsets, torch.int32, (batch + 1,), "offsets", self.device),
-                                     _array(first, torch.int32, (batch,), "first", self.device),
-                                     _array(positions, torch.int32, slots, "positions", self.device),
-                                     _array(weights, torch.float32, slots, "weights", self.device), _stream()))
+        _check(_load().psc_kv_append(c, _dtype(k, "k"), *self._rows(k, self.kv_heads, "k"), *self._rows(v, self.kv_heads, "v"), n,
+                                     _array(offsets, torch.int32, (batch + 1,), "offsets", self._index),
+                                     _array(first, torch.int32, (batch,), "first", self._index),
+                                     _array(positions, torch.int32, slots, "positions", self._index),
+                                     _array(weights, torch.float32, slots, "weights", self._index), self._stream()))
 
     def read(self, table, starts, rows: int, offsets=None, dtype=torch.float32):
         """The held values of the slots starts[b], starts[b] + 1, ... (`rows` of them altogether): k, v [rows, kv_heads,
@@ -104,8 +124,8 @@ class KvCache:
         c, batch, _ = self._args(table, starts, "starts")
         k = torch.empty((rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
-        _check(_load().psc_kv_read(C.byref(c), _dtype(k, "dtype"), rows, _array(offsets, torch.int32, (batch + 1,), "offsets", self.device),
-                                   k.data_ptr(), v.data_ptr(), _stream()))
+        _check(_load().psc_kv_read(c, _dtype(k, "dtype"), rows, _array(offsets, torch.int32, (batch + 1,), "offsets", self._index),
+                                   k.data_ptr(), v.data_ptr(), self._stream()))
         return k, v
 
     def attend(self, q, table, lengths, offsets=None, max_rows=None, first=None, positions=None, scale=None, causal=True, window=0,
@@ -117,19 +137,25 @@ class KvCache:
         `weights` (None: 0) plus the weight that each token was given; they may be the same tensor."""
         c, batch, slots = self._args(table, lengths)
         n, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
-        code, device, lib = _dtype(q, "q"), self.device, _load()
+        code, device = _dtype(q, "q"), self._index
         rows = self._rows(q, heads, "q")
         if offsets is None:
             max_rows = n // max(batch, 1)
         elif max_rows is None:
             max_rows = n
         if out is None:
-            out = (torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=device), torch.empty((n, heads), dtype=torch.float32, device=device))
-        if workspace is None:
-            need = lib.psc_kv_attention_workspace_bytes(C.byref(c), code, n, max_rows, heads, window, sinks, positions is not None,
-                                                        weights_out is not None)
-            workspace = _workspace(need, device)
-        _check(lib.psc_kv_attention(C.byref(c), code, *rows, n, max_rows, heads,
+            out = (torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device),
+                   torch.empty((n, heads), dtype=torch.float32, device=self.device))
+        space = None, 0
+        if workspace is not None:
+            space = _bytes(workspace, device)
+        else:
+            need = _attention_workspace(self.pages, self.kv_heads, self.head_dim, self.page, batch, table.shape[1], code, n, max_rows, heads,
+                                        window, sinks, positions is not None, weights_out is not None)
+            if need:
+                workspace = _workspace(need, self.device)
+                space = workspace.data_ptr(), need
+        _check(_load().psc_kv_attention(c, code, *rows, n, max_rows, heads,
                                     _array(offsets, torch.int32, (batch + 1,), "offsets", device),
                                     _array(first, torch.int32, (batch,), "first", device),
                                     _array(positions, torch.int32, slots, "positions", device),
@@ -138,7 +164,7 @@ class KvCache:
                                     _array(out[1], torch.float32, (n, heads), "lse", device),
                                     _array(weights, torch.float32, slots, "weights", device),
                                     _array(weights_out, torch.float32, slots, "weights_out", device),
-                                    _array(workspace, torch.uint8, workspace.shape, "workspace", device), workspace.numel(), _stream()))
+                                    *space, self._stream()))
         return out
 
     def evict(self, table, lengths, weights, budget: int, sinks: int = 0, recent: int = 0, positions=None, seen=None, out=None, workspace=None):
@@ -147,23 +173,24 @@ class KvCache:
         (kept, lengths, positions, weights): the slot each kept token had [batch, kv_heads, budget], and the state after;
         `out`: those four, where `lengths`, `positions` and `weights` may be the tensors passed in."""
         c, batch, slots = self._args(table, lengths)
-        device, lib = self.device, _load()
+        device, lib = self._index, _load()
         if out is None:
             shape = (batch, self.kv_heads, budget)
-            out = (torch.empty(shape, dtype=torch.int32, device=device), torch.empty(batch, dtype=torch.int32, device=device),
-                   torch.empty(shape, dtype=torch.int32, device=device), torch.empty(shape, dtype=torch.float32, device=device))
+            whole = torch.empty((2, *shape), dtype=torch.int32, device=self.device)
+            out = (whole[0], torch.empty(batch, dtype=torch.int32, device=self.device), whole[1],
+                   torch.empty(shape, dtype=torch.float32, device=self.device))
         kept, lengths_out, positions_out, weights_out = out
         wide = weights_out.shape
         if len(wide) != 3 or wide[:2] != slots[:2]:
             raise PscError(f"weights (out): expected [{slots[0]}, {slots[1]}, {budget} or more], got {list(wide)}")
         if workspace is None:
-            workspace = _workspace(lib.psc_kv_evict_workspace_bytes(C.byref(c), budget), device)
-        _check(lib.psc_kv_evict(C.byref(c), _array(weights, torch.float32, slots, "weights", device),
+            workspace = _workspace(lib.psc_kv_evict_workspace_bytes(c, budget), self.device)
+        _check(lib.psc_kv_evict(c, _array(weights, torch.float32, slots, "weights", device),
                                 _array(positions, torch.int32, slots, "positions", device),
                                 _array(seen, torch.int32, (batch,), "seen", device), budget, sinks, recent,
                                 _array(kept, torch.int32, (batch, self.kv_heads, budget), "kept", device),
                                 _array(lengths_out, torch.int32, (batch,), "lengths (out)", device),
                                 _array(positions_out, torch.int32, wide, "positions (out)", device),
                                 _array(weights_out, torch.float32, wide, "weights (out)", device), wide[2],
-                                _array(workspace, torch.uint8, workspace.shape, "workspace", device), workspace.numel(), _stream()))
+                                *_bytes(workspace, device), self._stream()))
         return out
