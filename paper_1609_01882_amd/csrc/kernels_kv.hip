@@ -516,10 +516,19 @@ struct Attention {
     }
 };
 
+// Waves of a SIMD that the registers are to leave room for.  (8 x 128k tokens, one row, 128 coordinates: 191 us without a
+// bound, 175 with 2 or 3, 317 with 4; 2048 rows over 16k tokens, 32 rows to a wave: 1336, 792 with 2, 2477 with 3.)
+template <int D, int DT, int RT, bool kSplitTokens>
+constexpr int attention_waves()
+{
+    if (D == 256) return DT == PSC_F32 ? 1 : 2;
+    return kSplitTokens && RT == 1 ? (DT == PSC_F32 ? 2 : 3) : DT == PSC_F32 && RT == 2 ? 1 : 2;
+}
+
 // kSplitTokens: the workgroup's four waves share 16 RT rows, every fourth block each, and are joined in LDS; otherwise
 // each wave has 16 RT rows of its own and all blocks.
 template <int D, int DT, int RT, bool kSplitTokens, bool kPos>
-__global__ __launch_bounds__(256, kSplitTokens && RT == 1 && D <= 128 ? 3 : 1) void kv_attention_kernel(KvView c, KvQueries q)
+__global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) void kv_attention_kernel(KvView c, KvQueries q)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -1241,7 +1250,7 @@ int run_read(const KvView &c, const KvRows &r, void *k, void *v, hipStream_t s)
 template <int DT, int D>
 constexpr int most_row_tiles()
 {
-    return DT == PSC_F32 ? (D == 256 ? 1 : 2) : D == 256 ? 2 : 4;
+    return DT == PSC_F32 || D == 256 ? 1 : 2;
 }
 
 template <int DT, int D>
@@ -1300,7 +1309,7 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
 {
     KvPlan p;
     const int64_t m = (int64_t)max_rows * group, q_heads = (int64_t)group * c.heads;
-    const int most = dtype == PSC_F32 ? (c.dim == 256 ? 1 : 2) : c.dim == 256 ? 2 : 4;
+    const int most = dtype == PSC_F32 || c.dim == 256 ? 1 : 2;
     // Waves with rows of their own pay once most of them have some.
     p.split_tokens = m <= 4 * 16 * most / 2;
     p.row_tiles = !p.split_tokens ? most : std::min(most, m <= 16 ? 1 : 2);
@@ -1312,7 +1321,8 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
         const int64_t per_wave = p.split_tokens ? rows_each : rows_each / 4;
         blocks = std::min(blocks, ((int64_t)window + per_wave / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
     }
-    const int64_t units = std::max<int64_t>(1, p.row_groups * c.batch * c.heads), wanted = 2048;
+    // as many workgroups as run at a time (3 and 2 to a compute unit): more make a second round, and more parts to join
+    const int64_t units = std::max<int64_t>(1, p.row_groups * c.batch * c.heads), wanted = p.split_tokens ? 768 : 512;
     const int least = p.split_tokens ? 4 : 16;  // blocks that are worth a workgroup
     p.splits = std::max<int64_t>(1, std::min((wanted + units - 1) / units, blocks / least));
     p.split_blocks = std::max<int64_t>(1, (blocks + p.splits - 1) / p.splits);
