@@ -193,6 +193,8 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
     q.part_stat = (float *)ws;
     q.part_acc = (float *)(ws + p.part_stat_bytes);
     q.stat = p.stat_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes) : nullptr;
+    q.scores = p.scores_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes + p.stat_bytes) : nullptr;
+    q.scores_rows = p.scores_rows;
     return launch_kv_attention(v, dtype, q, p, weights_in_dev, weights_out_dev, (hipStream_t)stream);
 }
 

@@ -350,13 +350,16 @@ struct KvQueries {
     int splits, split_blocks;
     float *part_stat, *part_acc;  // [splits][nrows][q_heads][2], [...][dim]
     float *stat;                  // [nrows][q_heads][2]: maximum (units of log 2), 1 / sum
+    float *scores;                // [batch][kv_heads][scores_rows][slots], or null
+    int scores_rows;
 };
 struct KvPlan {
     bool split_tokens = false;  // the waves of a workgroup share rows and split tokens
     int row_tiles = 0;          // of 16, to a wave
     int64_t row_groups = 0, splits = 0, split_blocks = 0;
-    size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0;
-    size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes; }
+    int scores_rows = 0;        // the scores of so many rows are kept for the weights (0: they are computed again)
+    size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0, scores_bytes = 0;
+    size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes + scores_bytes; }
 };
 KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered,
                          bool weights);

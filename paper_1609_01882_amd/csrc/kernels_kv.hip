@@ -344,12 +344,10 @@ struct Rows {
     u32x4 x[kTerms][D / 32];
 };
 template <int D, int DT>
-__device__ __forceinline__ void load_rows(const KvQueries &q, const RowSet &s, int head, int m, int g, Rows<D, DT> &rows)
+__device__ __forceinline__ void load_rows(const KvQueries &q, int row, int q_head, int g, Rows<D, DT> &rows)
 {
     typedef typename Element<DT>::type T;
-    const int mm = max(0, min(m, s.rows * q.group - 1));
-    const int t = mm / q.group, h = head * q.group + mm % q.group;
-    const T *p = (const T *)q.q + (int64_t)(s.first_row + t) * q.row_stride + (int64_t)h * q.head_stride + g * (D / 4);
+    const T *p = (const T *)q.q + (int64_t)row * q.row_stride + (int64_t)q_head * q.head_stride + g * (D / 4);
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
         if constexpr (DT != PSC_F32) rows.x[0][j] = *(const u32x4 *)(p + j * 8);
@@ -419,7 +417,7 @@ struct Attention {
     Rows<D, DT> rows[RT];
 
     __device__ void block(const KvView &c, const KvQueries &q, const Raw<D> &raw, const RowMask (&mask)[RT], int slot, int lim0,
-                          int lim1, bool whole, float factor, int i, int g)
+                          int lim1, int n, bool whole, float factor, int i, int g, float *scores)
     {
         f32x4 s[RT][2];
 #pragma unroll
@@ -441,6 +439,13 @@ struct Attention {
                     for (int t = 0; t < RT; ++t)
                         if (!(there && sees(q, mask[t], pos))) s[t][h][r] = kNegInf;
                 }
+        }
+        if constexpr (RT == 1) {
+            if (scores) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (slot + 16 * h < n) *(f32x4 *)(scores + slot + 16 * h + 4 * g) = s[0][h];
+            }
         }
         uint32_t p[RT][2][4];  // float16 pairs (the second array: what the first leaves of float32 rows' probabilities)
 #pragma unroll
@@ -548,8 +553,9 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
     RowMask mask[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        load_rows<D, DT>(q, s, head, m0 + t * 16 + i, g, a.rows[t]);
-        mask[t] = row_mask(q, s.first_pos + (m0 + t * 16 + i) / q.group);
+        const int m = min(m0 + t * 16 + i, m_all - 1), place = m / q.group;  // (rows past the last: the last one again)
+        load_rows<D, DT>(q, s.first_row + place, head * q.group + m - place * q.group, g, a.rows[t]);
+        mask[t] = row_mask(q, s.first_pos + place);
         a.top[t] = kNegInf;
         a.sum[t] = 0.f;
 #pragma unroll
@@ -582,6 +588,10 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
             }
         }
     };
+    // where the scores of the lane's row are left for kv_weights_of_scores_kernel
+    float *scores = nullptr;
+    if constexpr (kSplitTokens && RT == 1)
+        if (q.scores && i < m_all) scores = q.scores + ((int64_t)blockIdx.z * q.scores_rows + i) * ((int64_t)c.width << c.page_shift);
     if (mine > 0) {
         Raw<D> raw;
         int ids = pages_from(0), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
@@ -603,7 +613,7 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
                 const bool there = slot + 32 <= s.n && pages[0] >= 0 && pages[1] >= 0 && !kPos;
                 const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
                                    (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-                a.block(c, q, raw, mask, slot, pages[0] >= 0 ? s.n : 0, pages[1] >= 0 ? s.n : 0, whole, q.factor, i, g);
+                a.block(c, q, raw, mask, slot, pages[0] >= 0 ? s.n : 0, pages[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
                 raw = next;
                 pages[0] = next_pages[0];
                 pages[1] = next_pages[1];
@@ -763,19 +773,59 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
     if (quarter == 0) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
 }
 
-// The weight that every token received: scores once more, from the same products as in the attention itself, so that
-// with the row's maximum and sum each probability is the one that was used.  A wave has 32 tokens and goes through all
-// rows that can see one; the rows' shares are added in one order.  Rows that came out NaN add nothing.
-template <int D, int DT>
-__global__ __launch_bounds__(256) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
+// The weight that every token received, from the scores that the attention left: a thread to four slots.  For up to
+// kScoreRows rows (query heads times rows of a sequence): the scores' 4 bytes to a row, written and read, are then less than
+// the keys' bytes and what comes with expanding them (32 x 4k tokens, 4 rows: 31 us with the keys once more).
+constexpr int kScoreRows = 8;
+template <int N>
+__global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQueries q, const float *given, float *received)
+{
+    const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads;
+    const int64_t stride = (int64_t)c.width << c.page_shift, dense = (int64_t)blockIdx.z * stride;
+    const int64_t first = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (first >= stride) return;
+    const int slot = (int)first;
+    const RowSet s = rows_of(c, q, b);
+    const int m_all = s.rows * q.group;
+    f32x4 total = {0.f, 0.f, 0.f, 0.f};
+    if (given) total = *(const f32x4 *)(given + dense + slot);
+    if (slot < s.n && m_all > 0) {
+        const Blocks blocks = blocks_of(q, s.n, s.first_pos, s.first_pos + s.rows - 1);
+        if (slot / 32 < blocks.sink_blocks || (slot / 32 >= blocks.main && slot / 32 < blocks.end)) {
+            f32x4 x[N], sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < N; ++m)
+                x[m] = *(const f32x4 *)(q.scores + ((int64_t)blockIdx.z * q.scores_rows + min(m, m_all - 1)) * stride + slot);
+#pragma unroll
+            for (int m = 0; m < N; ++m) {
+                const int mm = min(m, m_all - 1);
+                const float2 st = *(const float2 *)(q.stat + ((int64_t)(s.first_row + mm / q.group) * q.q_heads + head * q.group + mm % q.group) * 2);
+                const float inv = m < m_all ? st.y : 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)  // (the larger of NaN and 0 is 0: rows that came out NaN add nothing)
+                    sum[j] += fmaxf(exp2_fast(__builtin_fmaf(x[m][j], q.factor, -st.x)) * inv, 0.f);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) total[j] += slot + j < s.n ? sum[j] : 0.f;
+        }
+    }
+    *(f32x4 *)(received + dense + slot) = total;
+}
+
+// The same with the scores once more, from the same products as in the attention itself, so that with the row's maximum and
+// sum each probability is the one that was used.  kSplitRows: a workgroup has 32 tokens and each wave a quarter of the rows
+// that can see one; otherwise a wave has 32 tokens and all rows.  The next 16 rows are on their way while 16 are worked on,
+// their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.
+template <int D, int DT, bool kSplitRows>
+__global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads;
     const RowSet s = rows_of(c, q, b);
-    const int64_t stride = (int64_t)c.width << c.page_shift, dense = ((int64_t)b * c.heads + head) * stride;
-    const int64_t block = (int64_t)blockIdx.x * 4 + wave;
-    if (block * 32 >= stride) return;
+    const int64_t stride = (int64_t)c.width << c.page_shift, dense = (int64_t)blockIdx.z * stride;
+    const int64_t block = kSplitRows ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
+    if (block * 32 >= stride) return;  // (with kSplitRows the whole workgroup)
     const int slot = (int)(block * 32), m_all = s.rows * q.group;
 
     float total[2][4] = {};
@@ -800,24 +850,52 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(KvView c, KvQueries q, 
             if (q.window > 0 && slot >= q.sinks)
                 m_end = min(m_end, max((int64_t)0, (int64_t)slot + 31 + q.window - s.first_pos) * q.group);
         }
-        for (int64_t m0 = m_begin; m0 < m_end; m0 += 16) {
-            const int m = (int)m0 + i;
+        const bool there = !q.positions && pages[0] >= 0 && pages[1] >= 0 && slot + 32 <= s.n;
+        const int step = kSplitRows ? 64 : 16, places = step / q.group, heads = step % q.group;
+        int64_t m0 = m_begin + (kSplitRows ? wave * 16 : 0);
+        if (m0 < m_end) {
+            // the lane's row: place of its sequence, query head of its group
+            int place = (int)((m0 + i) / q.group), in_group = (int)((m0 + i) % q.group);
             Rows<D, DT> rows;
-            load_rows<D, DT>(q, s, head, m, g, rows);
-            const bool valid = m < m_all;
-            const int mm = min(m, m_all - 1);
-            const int64_t row = (int64_t)(s.first_row + mm / q.group) * q.q_heads + head * q.group + mm % q.group;
-            const float2 st = *(const float2 *)(q.stat + row * 2);
-            const RowMask mask = row_mask(q, s.first_pos + mm / q.group);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4 x = scores_of<D, DT>(a[h], rows);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = exp2_fast(__builtin_fmaf(x[r], q.factor, -st.x)) * st.y;
-                    const bool adds = valid && pages[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]) && p == p;
-                    total[h][r] += adds ? p : 0.f;
+            float2 st;
+            auto load = [&](int m, int at, int h, Rows<D, DT> &r, float2 &stat) {
+                if (m >= m_all) {
+                    at = s.rows - 1;
+                    h = q.group - 1;
                 }
+                load_rows<D, DT>(q, s.first_row + at, head * q.group + h, g, r);
+                stat = *(const float2 *)(q.stat + ((int64_t)(s.first_row + at) * q.q_heads + head * q.group + h) * 2);
+            };
+            load((int)m0 + i, place, in_group, rows, st);
+            for (; m0 < m_end; m0 += step) {
+                const int m = (int)m0 + i, at = place;
+                place += places;
+                in_group += heads;
+                if (in_group >= q.group) {
+                    in_group -= q.group;
+                    ++place;
+                }
+                Rows<D, DT> next;
+                float2 next_st;
+                load((int)min(m0 + step, (int64_t)m_all) + i, place, in_group, next, next_st);
+                const float inv = m < m_all ? st.y : 0.f;
+                f32x4 x[2] = {scores_of<D, DT>(a[0], rows), scores_of<D, DT>(a[1], rows)};
+                const int pos_q = s.first_pos + at;
+                const bool mine = there && (!q.causal || pos_q >= slot + 31) && (q.window <= 0 || (int64_t)pos_q - slot < q.window || slot + 32 <= q.sinks);
+                if (!__all(mine)) {
+                    const RowMask mask = row_mask(q, pos_q);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (!(pages[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]))) x[h][r] = kNegInf;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) total[h][r] += fmaxf(exp2_fast(__builtin_fmaf(x[h][r], q.factor, -st.x)) * inv, 0.f);
+                rows = next;
+                st = next_st;
             }
         }
     }
@@ -830,8 +908,15 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(KvView c, KvQueries q, 
     float mine = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) mine = i == j ? total[j >> 2][j & 3] : mine;
-    const int at = slot + (i & 4) * 4 + 4 * g + (i & 3);
-    if (i < 8 && at < stride) received[dense + at] = (given ? given[dense + at] : 0.f) + mine;
+    const int in_block = (i & 4) * 4 + 4 * g + (i & 3);
+    if constexpr (kSplitRows) {
+        __shared__ float parts[4][32];
+        if (i < 8) parts[wave][in_block] = mine;
+        __syncthreads();
+        if (wave > 0) return;
+        if (i < 8) mine = parts[0][in_block] + parts[1][in_block] + parts[2][in_block] + parts[3][in_block];
+    }
+    if (i < 8 && slot + in_block < stride) received[dense + slot + in_block] = (given ? given[dense + slot + in_block] : 0.f) + mine;
 }
 
 // ------------------------------------------------------------------------------------------- eviction
@@ -1276,7 +1361,17 @@ int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const fl
     }
     if (received) {
         const int64_t slots = (int64_t)c.width << c.page_shift;
-        kv_weights_kernel<D, DT><<<dim3((uint32_t)((slots + 127) / 128), 1, (uint32_t)(c.batch * c.heads)), 256, 0, s>>>(c, q, given, received);
+        const uint32_t groups = (uint32_t)(c.batch * c.heads);
+        if (p.scores_rows > 0) {
+            const dim3 grid((uint32_t)((slots + 1023) / 1024), 1, groups);
+            if (p.scores_rows == 1) kv_weights_of_scores_kernel<1><<<grid, 256, 0, s>>>(c, q, given, received);
+            else if (p.scores_rows <= 4) kv_weights_of_scores_kernel<4><<<grid, 256, 0, s>>>(c, q, given, received);
+            else kv_weights_of_scores_kernel<kScoreRows><<<grid, 256, 0, s>>>(c, q, given, received);
+        } else if (q.max_rows * (int64_t)q.group > 64) {
+            kv_weights_kernel<D, DT, true><<<dim3((uint32_t)((slots + 31) / 32), 1, groups), 256, 0, s>>>(c, q, given, received);
+        } else {
+            kv_weights_kernel<D, DT, false><<<dim3((uint32_t)((slots + 127) / 128), 1, groups), 256, 0, s>>>(c, q, given, received);
+        }
         PSC_HIP_TRY(hipGetLastError());
     }
     return PSC_OK;
@@ -1332,6 +1427,10 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
     p.part_stat_bytes = p.splits > 1 ? (size_t)(p.splits * rows * 8 + 255) / 256 * 256 : 0;
     p.part_acc_bytes = p.splits > 1 ? (size_t)(p.splits * rows * c.dim * 4 + 255) / 256 * 256 : 0;
     p.stat_bytes = weights ? (size_t)(rows * 8 + 255) / 256 * 256 : 0;
+    if (weights && nrows > 0 && m <= kScoreRows && p.split_tokens && p.row_tiles == 1) {
+        p.scores_rows = (int)m;
+        p.scores_bytes = (size_t)((int64_t)c.batch * c.heads * m * ((int64_t)c.width << c.page_shift) * 4 + 255) / 256 * 256;
+    }
     return p;
 }
 
