@@ -23,6 +23,8 @@ int check_cache(const psc_kv_cache *c, KvView *v)
     PSC_REQUIRE(c->pages >= 1 && c->pages <= 0x7fffffff, "%lld pages: 1 to 2^31 - 1", (long long)c->pages);
     PSC_REQUIRE(c->table_width >= 1 && (int64_t)c->table_width * c->page < kMostSlots, "table of %d pages of %d slots: 1 page to under 2^30 slots",
                 c->table_width, c->page);
+    PSC_REQUIRE((__int128)c->pages * c->kv_heads * c->page < (__int128)1 << 35, "%lld pages of %d heads and %d slots: under 2^35 together",
+                (long long)c->pages, c->kv_heads, c->page);
     v->pages = c->pages;
     v->heads = c->kv_heads;
     v->dim = c->head_dim;

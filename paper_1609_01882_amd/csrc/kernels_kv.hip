@@ -72,6 +72,21 @@ __device__ __forceinline__ void store_row(void *p, const float (&x)[N])
     __builtin_memcpy(__builtin_assume_aligned(p, N * sizeof(T) < 16 ? N * sizeof(T) : 16), t, sizeof t);
 }
 
+// The larger of the values, and the sum of them, that the four lanes lane % 16 + 0, 16, 32, 48 hold.
+__device__ __forceinline__ float column_max(float x)
+{
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    u2 y = __builtin_bit_cast(u2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    x = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+    y = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+}
+__device__ __forceinline__ float column_sum(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Two held values: byte B of `codes`.
@@ -105,6 +120,15 @@ __device__ __forceinline__ int page_of(const KvView &c, int b, int64_t slot)
     if (slot < 0 || slot >= (int64_t)c.width << c.page_shift) return -1;
     const int p = c.table[(int64_t)b * c.width + (int)(slot >> c.page_shift)];
     return p >= 0 && p < c.pages ? p : -1;
+}
+
+// Number of the 16 slots that begin at `slot` in a buffer taken as [pages * heads * page / 16] of them (under 2^31: checked by
+// the host); -1 where there are none: past the n tokens, or no page.
+__device__ __forceinline__ int sixteen_of(const KvView &c, int b, int head, int n, int slot)
+{
+    const int p = c.table[(int64_t)b * c.width + min(slot >> c.page_shift, c.width - 1)];
+    if (slot >= n || (uint32_t)p >= (uint32_t)c.pages) return -1;
+    return ((p * c.heads + head) << (c.page_shift - 4)) + ((slot & ((1 << c.page_shift) - 1)) >> 4);
 }
 
 // ------------------------------------------------------------------------------------------- append, read
@@ -255,19 +279,20 @@ struct Raw {
     uint32_t vs[2][4];  // of the tokens' scale bytes the words that hold the lane's (value_scale)
     int pos[8];         // positions of the value tokens, where they have some of their own
 };
-// The lane's scale byte of token r of four.
+// The lane's scale byte of token r of four, in the place of a float's exponent.  The conversions look at these eight bits
+// alone, so the others may hold what they like.
 template <int D>
 __device__ __forceinline__ uint32_t value_scale(const uint32_t (&vs)[4], int r, int i)
 {
-    if constexpr (D == 64) return vs[r >> 1] >> ((r & 1) * 16 + (i >> 3) * 8) & 255u;
-    else if constexpr (D == 128) return vs[r] >> ((i >> 2) * 8) & 255u;
-    else return vs[r];
+    if constexpr (D == 64) return __builtin_amdgcn_alignbit(vs[r >> 1], vs[r >> 1], (9 + (r & 1) * 16 + (i >> 3) * 8) & 31);
+    else if constexpr (D == 128) return __builtin_amdgcn_alignbit(vs[r], vs[r], (9 + (i >> 2) * 8) & 31);
+    else return vs[r] << 23;
 }
 
 template <int D>
-__device__ __forceinline__ void load_keys(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (&k)[D / 32], uint32_t &ks)
+__device__ __forceinline__ void load_keys(const KvView &c, int sixteen, int i, int g, uint32_t (&k)[D / 32], uint32_t &ks)
 {
-    const int64_t at = (((int64_t)page * c.heads + head) << c.page_shift) + in_page;  // uniform
+    const int64_t at = (int64_t)max(sixteen, 0) << 4;  // uniform
     const uint8_t *p = c.k_codes + at * (D / 2), *s = c.k_scales + at * (D / 32);
     const uint32_t off = (uint32_t)(i * (D / 2) + g * (D / 8));
     if constexpr (D == 64) {
@@ -290,9 +315,9 @@ __device__ __forceinline__ void load_keys(const KvView &c, int head, int page, i
 }
 
 template <int D>
-__device__ __forceinline__ void load_values(const KvView &c, int head, int page, int in_page, int i, int g, uint32_t (*v)[D == 256 ? 2 : 1], uint32_t (&vs)[4])
+__device__ __forceinline__ void load_values(const KvView &c, int sixteen, int i, int g, uint32_t (*v)[D == 256 ? 2 : 1], uint32_t (&vs)[4])
 {
-    const int64_t at = (((int64_t)page * c.heads + head) << c.page_shift) + in_page;
+    const int64_t at = (int64_t)max(sixteen, 0) << 4;
     const uint8_t *p = c.v_codes + at * (D / 2), *s = c.v_scales + at * (D / 32);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -455,9 +480,7 @@ struct Attention {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) m = fmaxf(m, s[t][h][r]);
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            m *= factor;
+            m = column_max(m) * factor;
             if (__any(m > top[t])) {
                 const float now = fmaxf(top[t], m);
                 const float shrink = now == kNegInf ? 1.f : exp2_fast(top[t] - now);
@@ -498,7 +521,7 @@ struct Attention {
             uint32_t w[8];
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
-                const float sc = scale_of(held[t]);
+                const float sc = __uint_as_float(held[t]);
                 const uint32_t x = raw.v[t][y / 4];
                 w[t] = y % 4 == 0 ? two_h16<0>(x, sc) : y % 4 == 1 ? two_h16<1>(x, sc) : y % 4 == 2 ? two_h16<2>(x, sc) : two_h16<3>(x, sc);
             }
@@ -568,18 +591,15 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
     // loads (past the last block: of a page that is there).
     const int own = begin + (kSplitTokens ? wave : 0), mine = end > own ? (end - own + step - 1) / step : 0;
     auto pages_from = [&](int k) {
-        const int at = min(own + (k + (lane >> 1)) * step, end - 1), sl = blocks.block(at) * 32 + (lane & 1) * 16;
-        const int page = c.table[(int64_t)b * c.width + min(sl >> c.page_shift, c.width - 1)];
-        return sl < s.n && (uint32_t)page < (uint32_t)c.pages ? page : -1;
+        return sixteen_of(c, b, head, s.n, blocks.block(min(own + (k + (lane >> 1)) * step, end - 1)) * 32 + (lane & 1) * 16);
     };
     auto load = [&](int k, const int (&pg)[2], Raw<D> &r) {
-        const int sl = blocks.block(min(own + k * step, end - 1)) * 32, in_page = (1 << c.page_shift) - 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int page = max(pg[h], 0);
-            load_keys<D>(c, head, page, (sl + 16 * h) & in_page, i, g, r.k[h], r.ks[h]);
-            load_values<D>(c, head, page, (sl + 16 * h) & in_page, i, g, &r.v[4 * h], r.vs[h]);
+            load_keys<D>(c, pg[h], i, g, r.k[h], r.ks[h]);
+            load_values<D>(c, pg[h], i, g, &r.v[4 * h], r.vs[h]);
             if constexpr (kPos) {
+                const int sl = blocks.block(min(own + k * step, end - 1)) * 32;
                 const int4 x = *(const int4 *)(q.positions + dense + min(sl + 16 * h, (c.width << c.page_shift) - 16) + 4 * g);
                 r.pos[4 * h] = x.x;
                 r.pos[4 * h + 1] = x.y;
@@ -624,8 +644,7 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
     const bool parts = q.splits > 1;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        a.sum[t] += __shfl_xor(a.sum[t], 16);
-        a.sum[t] += __shfl_xor(a.sum[t], 32);
+        a.sum[t] = column_sum(a.sum[t]);
     }
 
     if constexpr (!kSplitTokens) {
@@ -759,10 +778,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
         }
     }
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) {
-        x[j] += __shfl_xor(x[j], 16);
-        x[j] += __shfl_xor(x[j], 32);
-    }
+    for (int j = 0; j < D / 16; ++j) x[j] = column_sum(x[j]);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     if (lane == 0) {
         if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (top + __log2f(sum)) * kLn2;
@@ -830,13 +846,13 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
 
     float total[2][4] = {};
     if (slot < s.n && m_all > 0) {
-        const int pages[2] = {page_of(c, b, slot), slot + 16 < s.n ? page_of(c, b, slot + 16) : -1};
+        const int pages[2] = {sixteen_of(c, b, head, s.n, slot), sixteen_of(c, b, head, s.n, slot + 16)};
         u32x4 a[2][D / 32];
         int pos[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             uint32_t k[D / 32], ks;
-            load_keys<D>(c, head, max(pages[h], 0), (slot + 16 * h) & ((1 << c.page_shift) - 1), i, g, k, ks);
+            load_keys<D>(c, pages[h], i, g, k, ks);
             expand_keys<D, DT>(k, ks, a[h]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {

@@ -45,7 +45,7 @@ def _evict(lib, cache=None, w=A, positions=None, seen=None, budget=16, sinks=4, 
 
 
 BAD_CACHES = [dict(head_dim=96), dict(head_dim=0), dict(page=48), dict(page=8), dict(page=512), dict(kv_heads=0), dict(batch=0), dict(batch=40_000),
-              dict(pages=0), dict(pages=1 << 31), dict(table_width=0), dict(table_width=1 << 26), dict(k_codes=None), dict(v_scales=None),
+              dict(pages=0), dict(pages=1 << 31), dict(pages=1 << 29, page=64), dict(table_width=0), dict(table_width=1 << 26), dict(k_codes=None), dict(v_scales=None),
               dict(k_codes=4104), dict(table=None), dict(lengths=None), dict(lengths=4097)]
 
 
