@@ -168,7 +168,7 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
     }
     const int group = q_heads / v.heads;
     const KvPlan p = plan_kv_attention(v, dtype, group, nrows, max_rows, window, sinks, !positions_dev, weights_out_dev != nullptr);
-    PSC_REQUIRE(p.row_groups <= kMostGroups, "%d rows of a sequence are too many", max_rows);
+    PSC_REQUIRE(p.row_groups * v.heads < kMostSlots, "%d rows of a sequence are too many", max_rows);
     PSC_REQUIRE(workspace_bytes >= p.bytes() && (p.bytes() == 0 || workspace_dev), "workspace too small: %zu bytes, %zu needed", workspace_bytes, p.bytes());
     PSC_REQUIRE(aligned(workspace_dev), "workspace must be 16-byte aligned");
     KvQueries q{};
@@ -189,8 +189,9 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
     q.sinks = sinks;
     q.out = out_dev;
     q.lse = lse_dev;
-    q.splits = (int)p.splits;
-    q.split_blocks = (int)p.split_blocks;
+    q.unit_rows = 16 * p.row_tiles;
+    q.workgroups = (uint32_t)p.workgroups;
+    q.least_blocks = (uint32_t)p.least_blocks;
     char *ws = (char *)workspace_dev;
     q.part_stat = (float *)ws;
     q.part_acc = (float *)(ws + p.part_stat_bytes);

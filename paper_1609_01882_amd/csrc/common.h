@@ -347,16 +347,19 @@ struct KvQueries {
     int causal, window, sinks;
     void *out;
     float *lse;
-    int splits, split_blocks;
-    float *part_stat, *part_acc;  // [splits][nrows][q_heads][2], [...][dim]
+    int unit_rows;                // rows (times query heads) of a unit
+    uint32_t workgroups, least_blocks;
+    float *part_stat, *part_acc;  // [most_parts][unit_rows][2], [...][dim]
     float *stat;                  // [nrows][q_heads][2]: maximum (units of log 2), 1 / sum
     float *scores;                // [batch][kv_heads][scores_rows][slots], or null
     int scores_rows;
 };
 struct KvPlan {
-    bool split_tokens = false;  // the waves of a workgroup share rows and split tokens
-    int row_tiles = 0;          // of 16, to a wave
-    int64_t row_groups = 0, splits = 0, split_blocks = 0;
+    int row_tiles = 0;       // of 16, to a unit
+    int64_t row_groups = 0;  // units of a sequence's kv head
+    int64_t workgroups = 0;  // units are cut into parts, about so many together; 0: a workgroup has a unit
+    int64_t most_parts = 0;
+    int least_blocks = 0;    // of a part
     int scores_rows = 0;        // the scores of so many rows are kept for the weights (0: they are computed again)
     size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0, scores_bytes = 0;
     size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes + scores_bytes; }

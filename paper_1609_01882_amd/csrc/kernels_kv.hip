@@ -11,6 +11,7 @@
 // rows too, as 0 * NaN).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "entry.h"
@@ -546,31 +547,120 @@ struct Attention {
 
 // Waves of a SIMD that the registers are to leave room for.  (8 x 128k tokens, one row, 128 coordinates: 191 us without a
 // bound, 175 with 2 or 3, 317 with 4; 2048 rows over 16k tokens, 32 rows to a wave: 1336, 792 with 2, 2477 with 3.)
-template <int D, int DT, int RT, bool kSplitTokens>
+template <int D, int DT, int RT>
 constexpr int attention_waves()
 {
     if (D == 256) return DT == PSC_F32 ? 1 : 2;
-    return kSplitTokens && RT == 1 ? (DT == PSC_F32 ? 2 : 3) : DT == PSC_F32 && RT == 2 ? 1 : 2;
+    return RT == 1 ? (DT == PSC_F32 ? 2 : D == 64 ? 4 : 3) : DT == PSC_F32 ? 1 : 2;
 }
 
-// kSplitTokens: the workgroup's four waves share 16 RT rows, every fourth block each, and are joined in LDS; otherwise
-// each wave has 16 RT rows of its own and all blocks.
-template <int D, int DT, int RT, bool kSplitTokens, bool kPos>
-__global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) void kv_attention_kernel(KvView c, KvQueries q)
+// A unit of work is 16 RT rows of a (sequence, kv head) and all blocks that they see.  Where there are enough units, a
+// workgroup has one.  Where there are few, each is cut into equal parts of at most `per` blocks, a part to a workgroup, with
+// `per` such that about as many workgroups come out as run at a time, whatever the lengths of the sequences; kv_join_kernel
+// joins the parts.  The units of a sequence count alike, as the widest of them.  (8 sequences of 53 to 131 thousand tokens
+// 156 us; every sequence cut into as many parts 175; all units' blocks cut into equal shares, which may end inside units, 162,
+// and 32 sequences of 2 to 4 thousand 47 instead of 42, for what a second unit costs a workgroup.)
+__device__ __forceinline__ uint32_t scan64(uint32_t x)  // inclusive sums over the wave
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+struct Parts {
+    uint32_t parts, upto;  // workgroups of the lane's sequence of 64, and of those up to it
+    uint32_t total, per;   // workgroups; blocks of each
+
+    __device__ static uint32_t units_of(const KvView &c, const KvQueries &q, const RowSet &s) { return (uint32_t)((s.rows * q.group + q.unit_rows - 1) / q.unit_rows * c.heads); }
+    __device__ static uint32_t blocks_of_unit(const KvQueries &q, const RowSet &s)
+    {
+        if (s.rows == 0) return 0u;
+        const Blocks k = blocks_of(q, s.n, s.first_pos, s.first_pos + s.rows - 1);
+        const int most = q.positions || q.window <= 0 ? k.count() : (int)min((int64_t)k.count(), k.sink_blocks + ((int64_t)q.window + q.unit_rows / q.group + 1) / 32 + 2);
+        return (uint32_t)most;
+    }
+    __device__ uint32_t parts_of_unit(uint32_t blocks) const { return (blocks + per - 1) / per; }
+    __device__ void load(const KvView &c, const KvQueries &q, int b0)
+    {
+        const int b = b0 + lane_id();
+        parts = 0u;
+        if (b < c.batch) {
+            const RowSet s = rows_of(c, q, b);
+            parts = units_of(c, q, s) * parts_of_unit(blocks_of_unit(q, s));
+        }
+        upto = scan64(parts);
+    }
+    __device__ Parts(const KvView &c, const KvQueries &q)
+    {
+        uint32_t blocks = 0u, units = 0u;
+        for (int b = lane_id(); b < c.batch; b += 64) {
+            const RowSet s = rows_of(c, q, b);
+            const uint32_t n = units_of(c, q, s);
+            blocks += n * blocks_of_unit(q, s);
+            units += n;
+        }
+        blocks = (uint32_t)__builtin_amdgcn_readlane((int)scan64(blocks), 63);
+        units = (uint32_t)__builtin_amdgcn_readlane((int)scan64(units), 63);
+        // rounding up leaves half a part too many per unit
+        const uint32_t wanted = max(q.workgroups / 2, q.workgroups - min(q.workgroups, units / 2));
+        per = max((uint32_t)q.least_blocks, (blocks + wanted - 1) / wanted);
+        total = 0u;
+        for (int b0 = 0; b0 < c.batch; b0 += 64) {
+            load(c, q, b0);
+            total += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        }
+    }
+    // The sequence of workgroup `at` < total, and its first workgroup.
+    __device__ int find(const KvView &c, const KvQueries &q, uint32_t at, uint32_t *first)
+    {
+        uint32_t base = 0u;
+        for (int b0 = 0; b0 < c.batch; b0 += 64) {
+            if (c.batch > 64) load(c, q, b0);
+            const uint64_t behind = ballot64(at - base < upto);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                *first = base + (uint32_t)__builtin_amdgcn_readlane((int)(upto - parts), l);
+                return b0 + l;
+            }
+            base += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        }
+        return c.batch - 1;  // (not reached)
+    }
+    // The first workgroup of sequence b.
+    __device__ uint32_t first_of(const KvView &c, const KvQueries &q, int b)
+    {
+        uint32_t base = 0u;
+        for (int b0 = 0; b0 < c.batch; b0 += 64) {
+            if (c.batch > 64) load(c, q, b0);
+            if (b < b0 + 64) return base + (uint32_t)__builtin_amdgcn_readlane((int)(upto - parts), b - b0);
+            base += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        }
+        return base;
+    }
+};
+
+template <int D, int RT>
+struct Joined {  // of a workgroup's four waves
+    static constexpr int kStride = D + 4;
+    float acc[4][16 * kStride];
+    float tops[4][16 * RT], sums[4][16 * RT];
+};
+
+// Blocks begin .. end - 1 of the rows from m0 on of (b, head): the workgroup's four waves take every fourth each and are
+// joined in LDS.  part < 0: these are all blocks, and the result is final.
+template <int D, int DT, int RT, bool kPos>
+__device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q, const RowSet &s, int b, int head, int m0, const Blocks &blocks, int begin,
+                                            int end, int64_t part, Joined<D, RT> &joined)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads;
-    const RowSet s = rows_of(c, q, b);
-    const int m_all = s.rows * q.group;
-    const int m0 = ((int)blockIdx.y * (kSplitTokens ? 1 : 4) + (kSplitTokens ? 0 : wave)) * 16 * RT;
-    if ((int)blockIdx.y * (kSplitTokens ? 1 : 4) * 16 * RT >= m_all) return;  // (the whole workgroup)
-    const int m_end = min(m0 + 16 * RT, m_all);
-    const int lo_pos = s.first_pos + m0 / q.group, hi_pos = s.first_pos + (max(m_end, 1) - 1) / q.group;
-    const Blocks blocks = blocks_of(q, s.n, lo_pos, hi_pos);
-    const int count = m0 < m_all ? blocks.count() : 0;
-    const int begin = (int)blockIdx.x * q.split_blocks, end = min(count, begin + q.split_blocks);
-    const int step = kSplitTokens ? 4 : 1;
+    const int m_all = s.rows * q.group, m_end = min(m0 + 16 * RT, m_all);
+    const int lo_pos = s.first_pos + m0 / q.group, hi_pos = s.first_pos + (m_end - 1) / q.group;
+    constexpr int step = 4;
 
     Attention<D, DT, RT, kPos> a;
     RowMask mask[RT];
@@ -586,10 +676,9 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
     }
     const int64_t dense = ((int64_t)b * c.heads + head) * ((int64_t)c.width << c.page_shift);
 
-    // The wave's blocks are those at begin + wave (or 0), and every `step` further.  The pages of 32 of them are held across
-    // the lanes; the codes of the block after the one that is worked on are on their way, without a branch around their
-    // loads (past the last block: of a page that is there).
-    const int own = begin + (kSplitTokens ? wave : 0), mine = end > own ? (end - own + step - 1) / step : 0;
+    // The places of 32 of the wave's blocks are held across the lanes; the codes of the block after the one that is worked on
+    // are on their way, without a branch around their loads (past the last block: of a page that is there).
+    const int own = begin + wave, mine = end > own ? (end - own + step - 1) / step : 0;
     auto pages_from = [&](int k) {
         return sixteen_of(c, b, head, s.n, blocks.block(min(own + (k + (lane >> 1)) * step, end - 1)) * 32 + (lane & 1) * 16);
     };
@@ -610,8 +699,8 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
     };
     // where the scores of the lane's row are left for kv_weights_of_scores_kernel
     float *scores = nullptr;
-    if constexpr (kSplitTokens && RT == 1)
-        if (q.scores && i < m_all) scores = q.scores + ((int64_t)blockIdx.z * q.scores_rows + i) * ((int64_t)c.width << c.page_shift);
+    if constexpr (RT == 1)
+        if (q.scores && i < m_all) scores = q.scores + (((int64_t)b * c.heads + head) * q.scores_rows + i) * ((int64_t)c.width << c.page_shift);
     if (mine > 0) {
         Raw<D> raw;
         int ids = pages_from(0), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
@@ -641,119 +730,113 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT, kSplitTokens>())) 
             ids = ids_then;
         }
     }
-    const bool parts = q.splits > 1;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) a.sum[t] = column_sum(a.sum[t]);
+    if (g == 0) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            joined.tops[wave][t * 16 + i] = a.top[t];
+            joined.sums[wave][t * 16 + i] = a.sum[t];
+        }
+    }
+    __syncthreads();
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        a.sum[t] = column_sum(a.sum[t]);
-    }
-
-    if constexpr (!kSplitTokens) {
+        float top = kNegInf;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int m = m0 + t * 16 + i;
-            if (m >= m_all) continue;
-            const int64_t row = (int64_t)(s.first_row + m / q.group) * q.q_heads + head * q.group + m % q.group;
-            if (parts) {
-                const int64_t at_part = (int64_t)blockIdx.x * q.nrows * q.q_heads + row;
-                if (g == 0) *(float2 *)(q.part_stat + at_part * 2) = make_float2(a.top[t], a.sum[t]);
-                if (a.sum[t] == 0.f) continue;
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, joined.tops[w][t * 16 + i]);
+        const float shrink = top == kNegInf ? 1.f : exp2_fast(a.top[t] - top);
+        if (t) __syncthreads();
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x[D / 16];
+        for (int r = 0; r < 4; ++r) {
+            float x[D / 16];
 #pragma unroll
-                    for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r];
-                    store_row<PSC_F32, D / 16>(q.part_acc + at_part * D + (g * 4 + r) * (D / 16), x);
-                }
-            } else {
-                const float inv = a.sum[t] == 0.f ? 0.f : 1.f / a.sum[t];
-                if (g == 0) {
-                    if (q.lse) q.lse[row] = a.sum[t] == 0.f ? kNegInf : (a.top[t] + __log2f(a.sum[t])) * kLn2;
-                    if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(a.top[t] == kNegInf ? 0.f : a.top[t], inv);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x[D / 16];
-#pragma unroll
-                    for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r] * inv;
-                    store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + (g * 4 + r) * (D / 16), x);
-                }
-            }
-        }
-    } else {
-        constexpr int kStride = D + 4;
-        __shared__ float joined[4][16 * kStride];
-        __shared__ float tops[4][16 * RT], sums[4][16 * RT];
-        if (g == 0) {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                tops[wave][t * 16 + i] = a.top[t];
-                sums[wave][t * 16 + i] = a.sum[t];
-            }
+            for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r] * shrink;
+            store_row<PSC_F32, D / 16>(&joined.acc[wave][i * joined.kStride + (g * 4 + r) * (D / 16)], x);
         }
         __syncthreads();
+        const int local = (int)threadIdx.x >> 4, run = (int)threadIdx.x & 15, m = m0 + t * 16 + local;
+        if (m < m_all) {
+            float best = kNegInf, sum = 0.f;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            float top = kNegInf;
+            for (int w = 0; w < 4; ++w) best = fmaxf(best, joined.tops[w][t * 16 + local]);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, tops[w][t * 16 + i]);
-            const float shrink = top == kNegInf ? 1.f : exp2_fast(a.top[t] - top);
-            if (t) __syncthreads();
+            for (int w = 0; w < 4; ++w) sum += joined.sums[w][t * 16 + local] * (best == kNegInf ? 1.f : exp2_fast(joined.tops[w][t * 16 + local] - best));
+            float x[D / 16];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x[D / 16];
+            for (int j = 0; j < D / 16; ++j) {
+                x[j] = 0.f;
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) x[j] = a.acc[t][j][r] * shrink;
-                store_row<PSC_F32, D / 16>(&joined[wave][i * kStride + (g * 4 + r) * (D / 16)], x);
+                for (int w = 0; w < 4; ++w) x[j] += joined.acc[w][local * joined.kStride + run * (D / 16) + j];
             }
-            __syncthreads();
-            const int local = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, m = m0 + t * 16 + local;
-            if (m < m_all) {
-                float best = kNegInf, sum = 0.f;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) best = fmaxf(best, tops[w][t * 16 + local]);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) sum += sums[w][t * 16 + local] * (best == kNegInf ? 1.f : exp2_fast(tops[w][t * 16 + local] - best));
-                float x[D / 16];
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) {
-                    x[j] = 0.f;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) x[j] += joined[w][local * kStride + part * (D / 16) + j];
-                }
+            if (part >= 0) {
+                const int64_t at = part * (16 * RT) + t * 16 + local;
+                if (run == 0) *(float2 *)(q.part_stat + at * 2) = make_float2(best, sum);
+                store_row<PSC_F32, D / 16>(q.part_acc + at * D + run * (D / 16), x);
+            } else {
                 const int64_t row = (int64_t)(s.first_row + m / q.group) * q.q_heads + head * q.group + m % q.group;
-                if (parts) {
-                    const int64_t at_part = (int64_t)blockIdx.x * q.nrows * q.q_heads + row;
-                    if (part == 0) *(float2 *)(q.part_stat + at_part * 2) = make_float2(best, sum);
-                    if (sum != 0.f) store_row<PSC_F32, D / 16>(q.part_acc + at_part * D + part * (D / 16), x);
-                } else {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    if (part == 0) {
-                        if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (best + __log2f(sum)) * kLn2;
-                        if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(best == kNegInf ? 0.f : best, inv);
-                    }
-#pragma unroll
-                    for (int j = 0; j < D / 16; ++j) x[j] *= inv;
-                    store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                if (run == 0) {
+                    if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (best + __log2f(sum)) * kLn2;
+                    if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(best == kNegInf ? 0.f : best, inv);
                 }
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) x[j] *= inv;
+                store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + run * (D / 16), x);
             }
         }
     }
 }
 
-// Joins a row's parts, a wave to a row: each lane takes a part's maximum and sum (64 parts at a time), then the lanes take
-// D / 16 coordinates of every fourth part each.
-template <int D, int DT>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
+template <int D, int DT, int RT, bool kPos, bool kParts>
+__global__ __launch_bounds__(256, (attention_waves<D, DT, RT>())) void kv_attention_kernel(KvView c, KvQueries q)
 {
-    const int lane = lane_id(), part = lane & 15, quarter = lane >> 4;
-    const int64_t all = (int64_t)q.nrows * q.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= all) return;
+    __shared__ Joined<D, RT> joined;
+    if constexpr (!kParts) {
+        const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads, m0 = (int)blockIdx.x * 16 * RT;
+        const RowSet s = rows_of(c, q, b);
+        if (m0 >= s.rows * q.group) return;
+        const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
+        attend_unit<D, DT, RT, kPos>(c, q, s, b, head, m0, blocks, 0, blocks.count(), -1, joined);
+    } else {
+        Parts all(c, q);
+        if (blockIdx.x >= all.total) return;
+        uint32_t first;
+        const int b = all.find(c, q, blockIdx.x, &first);
+        const RowSet s = rows_of(c, q, b);
+        const uint32_t each = Parts::blocks_of_unit(q, s), parts = all.parts_of_unit(each);
+        const uint32_t unit = (blockIdx.x - first) / parts, part = blockIdx.x - first - unit * parts;
+        const int head = (int)unit % c.heads, m0 = (int)unit / c.heads * 16 * RT;
+        const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
+        const int count = blocks.count(), from = (int)((uint64_t)part * each / parts), to = (int)((uint64_t)(part + 1) * each / parts);
+        attend_unit<D, DT, RT, kPos>(c, q, s, b, head, m0, blocks, min(count, from), min(count, to), parts == 1 ? -1 : (int64_t)blockIdx.x, joined);
+    }
+}
+
+// Joins a row's parts, a wave to a row: each lane takes a part's maximum and sum (64 parts at a time), then the lanes take
+// D / 16 coordinates of every fourth part each.  Sequences without a block have no part: zeros.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvView c, KvQueries q)
+{
+    const int lane = lane_id(), run = lane & 15, quarter = lane >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (row >= (int64_t)q.nrows * q.q_heads) return;
+    const int r = (int)(row / q.q_heads), q_head = (int)(row % q.q_heads), b = __builtin_amdgcn_readfirstlane(sequence_of_row(q.offsets, c.batch, q.each, r));
+    const RowSet s = rows_of(c, q, b);
+    const int place = r - s.first_row;
+    if (place < 0 || place >= s.rows) return;
+    const int m = place * q.group + q_head % q.group, in_unit = m % q.unit_rows;
+    const uint32_t unit = (uint32_t)(m / q.unit_rows * c.heads + q_head / q.group);
+    Parts all(c, q);
+    const int parts = (int)all.parts_of_unit(Parts::blocks_of_unit(q, s));
+    if (parts == 1) return;  // (final already)
+    const int64_t at = ((int64_t)all.first_of(c, q, b) + (int64_t)unit * parts) * q.unit_rows + in_unit;  // and every unit_rows further
     float top = kNegInf, sum = 0.f, x[D / 16];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) x[j] = 0.f;
-    for (int p0 = 0; p0 < q.splits; p0 += 64) {
+    for (int p0 = 0; p0 < parts; p0 += 64) {
         float2 st = make_float2(kNegInf, 0.f);
-        if (p0 + lane < q.splits) st = *(const float2 *)(q.part_stat + ((p0 + lane) * all + row) * 2);
+        if (p0 + lane < parts) st = *(const float2 *)(q.part_stat + (at + (int64_t)(p0 + lane) * q.unit_rows) * 2);
         float now = top;
         if (st.y != 0.f) now = fmaxf(now, st.x);
 #pragma unroll
@@ -767,12 +850,12 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
         top = now;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) x[j] *= shrink;
-        const int last = min(64, q.splits - p0);
-        for (int p = quarter; p < last; p += 4) {
-            const float w = __shfl(theirs, p);
-            if (w == 0.f) continue;  // (its sums were not written)
+        const int last = min(64, parts - p0);
+        for (int k = 0; k < last; k += 4) {  // (all lanes to the end: a lane's weight is asked of another one)
+            const int p = k + quarter;
+            const float w = __shfl(theirs, p);  // past the last: 0
             float y[D / 16];
-            load_row<PSC_F32, D / 16>(q.part_acc + ((p0 + p) * all + row) * D + part * (D / 16), y);
+            load_row<PSC_F32, D / 16>(q.part_acc + (at + (int64_t)(p0 + min(p, last - 1)) * q.unit_rows) * D + run * (D / 16), y);
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) x[j] = __builtin_fmaf(y[j], w, x[j]);
         }
@@ -786,7 +869,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvQueries q)
     }
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) x[j] *= inv;
-    if (quarter == 0) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + part * (D / 16), x);
+    if (quarter == 0) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + run * (D / 16), x);
 }
 
 // The weight that every token received, from the scores that the attention left: a thread to four slots.  For up to
@@ -1347,7 +1430,11 @@ int run_read(const KvView &c, const KvRows &r, void *k, void *v, hipStream_t s)
     return PSC_OK;
 }
 
-// Rows of a workgroup that shares them (tokens split over its waves), and of one whose waves have their own.
+// Blocks of a part at least, and blocks of a memory up to which a unit stays whole (128 rows over 1500 tokens, 47 blocks:
+// 28 us in parts, 20 whole; one row over 16000 tokens: 23.5 us with parts of 8 blocks or more, 21.0 with 16, 21.6 with 24).
+constexpr int64_t kLeastBlocks = 16, kFewBlocks = 64;
+
+// Rows of a wave, in sixteens, at most.
 template <int DT, int D>
 constexpr int most_row_tiles()
 {
@@ -1359,19 +1446,20 @@ int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const fl
 {
     constexpr int kMost = most_row_tiles<DT, D>();
     if (q.nrows > 0) {
-        const dim3 grid((uint32_t)p.splits, (uint32_t)p.row_groups, (uint32_t)(c.batch * c.heads));
-        if (q.positions) {
-            if (!p.split_tokens) kv_attention_kernel<D, DT, kMost, false, true><<<grid, 256, 0, s>>>(c, q);
-            else if (p.row_tiles == 1) kv_attention_kernel<D, DT, 1, true, true><<<grid, 256, 0, s>>>(c, q);
-            else if constexpr (kMost >= 2) kv_attention_kernel<D, DT, 2, true, true><<<grid, 256, 0, s>>>(c, q);
-        } else {
-            if (!p.split_tokens) kv_attention_kernel<D, DT, kMost, false, false><<<grid, 256, 0, s>>>(c, q);
-            else if (p.row_tiles == 1) kv_attention_kernel<D, DT, 1, true, false><<<grid, 256, 0, s>>>(c, q);
-            else if constexpr (kMost >= 2) kv_attention_kernel<D, DT, 2, true, false><<<grid, 256, 0, s>>>(c, q);
-        }
+        const uint32_t groups = (uint32_t)(c.batch * c.heads);
+        const auto launch = [&](auto rt, auto pos) {
+            if (p.workgroups) kv_attention_kernel<D, DT, rt.value, pos.value, true><<<(uint32_t)p.most_parts, 256, 0, s>>>(c, q);
+            else kv_attention_kernel<D, DT, rt.value, pos.value, false><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q);
+        };
+        const auto launch_rows = [&](auto pos) {
+            if (p.row_tiles == 1) launch(std::integral_constant<int, 1>(), pos);
+            else launch(std::integral_constant<int, kMost>(), pos);
+        };
+        if (q.positions) launch_rows(std::true_type());
+        else launch_rows(std::false_type());
         PSC_HIP_TRY(hipGetLastError());
-        if (p.splits > 1) {
-            kv_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * q.q_heads + 3) / 4), 256, 0, s>>>(q);
+        if (p.workgroups) {
+            kv_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * q.q_heads + 3) / 4), 256, 0, s>>>(c, q);
             PSC_HIP_TRY(hipGetLastError());
         }
     }
@@ -1419,31 +1507,27 @@ int launch_kv_read(const KvView &c, int dtype, const KvRows &r, void *k_out, voi
 KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered, bool weights)
 {
     KvPlan p;
-    const int64_t m = (int64_t)max_rows * group, q_heads = (int64_t)group * c.heads;
-    const int most = dtype == PSC_F32 || c.dim == 256 ? 1 : 2;
-    // Waves with rows of their own pay once most of them have some.
-    p.split_tokens = m <= 4 * 16 * most / 2;
-    p.row_tiles = !p.split_tokens ? most : std::min(most, m <= 16 ? 1 : 2);
-    const int64_t rows_each = (int64_t)16 * p.row_tiles * (p.split_tokens ? 1 : 4);
-    p.row_groups = (m + rows_each - 1) / rows_each;
+    const int64_t m = (int64_t)max_rows * group, rows = nrows * group * c.heads;
+    p.row_tiles = m <= 16 || dtype == PSC_F32 || c.dim == 256 ? 1 : 2;
+    p.row_groups = (m + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
     // blocks of 32 tokens that a group of rows can see at most
     int64_t blocks = (((int64_t)c.width << c.page_shift) + 31) / 32;
-    if (ordered && window > 0) {
-        const int64_t per_wave = p.split_tokens ? rows_each : rows_each / 4;
-        blocks = std::min(blocks, ((int64_t)window + per_wave / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
+    if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
+    const int64_t units = p.row_groups * c.batch * c.heads;
+    // workgroups that run at a time (attention_waves of them to a compute unit)
+    const int waves = dtype == PSC_F32 ? (c.dim == 256 ? 1 : 2) : c.dim == 256 || p.row_tiles == 2 ? 2 : c.dim == 64 ? 4 : 3;
+    // As many units as that, or memories of a few blocks to a wave: parts and their join would cost more than they save.
+    if (units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31)
+        p.workgroups = 256 * waves;
+    if (p.workgroups) {
+        // at most one part more to a unit than `wanted` of Parts, which is half of the workgroups or more
+        p.most_parts = std::min(p.workgroups + units, units * ((blocks + kLeastBlocks - 1) / kLeastBlocks));
+        p.part_stat_bytes = (size_t)(p.most_parts * 16 * p.row_tiles * 8 + 255) / 256 * 256;
+        p.part_acc_bytes = (size_t)(p.most_parts * 16 * p.row_tiles * c.dim * 4 + 255) / 256 * 256;
     }
-    // as many workgroups as run at a time (3 and 2 to a compute unit): more make a second round, and more parts to join
-    const int64_t units = std::max<int64_t>(1, p.row_groups * c.batch * c.heads), wanted = p.split_tokens ? 768 : 512;
-    const int least = p.split_tokens ? 4 : 16;  // blocks that are worth a workgroup
-    p.splits = std::max<int64_t>(1, std::min((wanted + units - 1) / units, blocks / least));
-    p.split_blocks = std::max<int64_t>(1, (blocks + p.splits - 1) / p.splits);
-    if (p.split_tokens) p.split_blocks = (p.split_blocks + 3) / 4 * 4;
-    p.splits = std::max<int64_t>(1, (blocks + p.split_blocks - 1) / p.split_blocks);
-    const int64_t rows = nrows * q_heads;
-    p.part_stat_bytes = p.splits > 1 ? (size_t)(p.splits * rows * 8 + 255) / 256 * 256 : 0;
-    p.part_acc_bytes = p.splits > 1 ? (size_t)(p.splits * rows * c.dim * 4 + 255) / 256 * 256 : 0;
+    p.least_blocks = kLeastBlocks;
     p.stat_bytes = weights ? (size_t)(rows * 8 + 255) / 256 * 256 : 0;
-    if (weights && nrows > 0 && m <= kScoreRows && p.split_tokens && p.row_tiles == 1) {
+    if (weights && nrows > 0 && m <= kScoreRows) {
         p.scores_rows = (int)m;
         p.scores_bytes = (size_t)((int64_t)c.batch * c.heads * m * ((int64_t)c.width << c.page_shift) * 4 + 255) / 256 * 256;
     }

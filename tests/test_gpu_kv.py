@@ -156,6 +156,18 @@ def test_several_rows(dtype, dim, rows):
     _attend_case(2, dtype, dim, 2, 3, 64, [rows, rows + 1, 200, 333], [rows, rows, rows, rows])
 
 
+@pytest.mark.parametrize("batch", [64, 65, 150])
+@pytest.mark.parametrize("rows", [1, 3])
+def test_many_sequences_of_very_different_lengths(batch, rows):
+    lengths = np.random.default_rng(batch).integers(0, 60, batch)
+    lengths[[3, batch - 1]] = 900, 1300
+    lengths[[0, 40]] = 0
+    _attend_case(14, "bf16", 64, 1, 2, 16, lengths, [rows] * batch, first=None if rows == 1 else lengths)
+    lengths[:] = 0
+    lengths[batch // 2] = 700
+    _attend_case(15, "f32", 64, 1, 2, 16, lengths, [rows] * batch, weights=False)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("page", [16, 128, 256])
 def test_ragged_rows(dtype, page):
@@ -197,6 +209,21 @@ def test_tokens_that_are_not_finite_reach_only_the_rows_that_see_them(dtype, row
 @pytest.mark.parametrize("rows", [1, 100])
 def test_tables_with_missing_pages(rows):
     _attend_case(8, "bf16", 128, 2, 2, 16, [200, 210, 220], [rows] * 3, missing=[(0, 0, -1), (0, 5, 1 << 20), (1, 13, -9), (2, 2, 44), (2, 3, -1)])
+
+
+@pytest.mark.parametrize("rows,window", [(1, 0), (9, 0), (9, 700), (100, 300), (60, 0)])
+def test_memories_of_a_thousand_tokens_and_more(rows, window):
+    """Few sequences: their blocks are shared out over the workgroups."""
+    _attend_case(16, "f16", 128, 1, 3, 64, [2300, 1, 1500, 0], [rows] * 4, window=window, sinks=5)
+    _attend_case(17, "bf16", 256, 1, 2, 16, [1900, 700], [rows] * 2, window=window, evicted=True)
+    _attend_case(18, "f32", 64, 1, 1, 32, [3000, 40], [rows] * 2, window=window, missing=[(0, 7, -1), (0, 50, 1 << 20)])
+
+
+@pytest.mark.parametrize("blocks", [65, 129, 257, 272, 288, 305, 513, 529, 785, 800, 1025, 1040])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_numbers_of_parts(blocks, dtype):
+    """One memory of many blocks of 32 tokens: its parts are joined, four at a time, 64 at a time."""
+    _attend_case(19, dtype, 64, 1, 1, 32, [32 * blocks - 5], [1], weights=False, garbage=False)
 
 
 @pytest.mark.parametrize("q_scale", [1e-3, 60.0])
