@@ -5,4 +5,5 @@ Each builds its index with the library, runs the search on cuda:0 and prints one
     python -m paper_1609_01882_amd.benchmarks.flat128
     python -m paper_1609_01882_amd.benchmarks.ivf
     python -m paper_1609_01882_amd.benchmarks.graph
+    python -m paper_1609_01882_amd.benchmarks.decode     # attention memory in 4 bits
 """

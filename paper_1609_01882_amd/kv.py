@@ -167,6 +167,16 @@ class KvCache:
                                     *space, self._stream()))
         return out
 
+    def attend_workspace_bytes(self, batch: int, width: int, rows: int, max_rows: int, q_heads: int, dtype, window: int = 0, sinks: int = 0,
+                               positions: bool = False, weights: bool = False) -> int:
+        """What `attend` needs for `rows` rows, at most `max_rows` of a sequence, over tables [batch, width]; `positions` and
+        `weights`: whether there are positions and weights_out."""
+        return int(_attention_workspace(self.pages, self.kv_heads, self.head_dim, self.page, batch, width, _DTYPES[dtype], rows, max_rows,
+                                        q_heads, window, sinks, positions, weights))
+
+    def evict_workspace_bytes(self, batch: int, width: int, budget: int) -> int:
+        return int(_load().psc_kv_evict_workspace_bytes(_pack(0, 0, 0, 0, self.pages, self.kv_heads, self.head_dim, self.page, 0, batch, width, 0), budget))
+
     def evict(self, table, lengths, weights, budget: int, sinks: int = 0, recent: int = 0, positions=None, seen=None, out=None, workspace=None):
         """Cut every sequence's heads to the `budget` tokens of the largest `weights` (per slot), the tokens at positions
         below `sinks` and the `recent` last ones of the `seen` [batch] (None: lengths) always among them.  Returns

@@ -433,3 +433,14 @@ def test_a_recorded_step_replays():
         torch.cuda.synchronize()
         for x, y in zip(state(), want):
             assert torch.equal(x, y)
+
+
+def test_the_example_runs(monkeypatch, capsys):
+    import json
+    import sys
+
+    from paper_1609_01882_amd.benchmarks import decode
+    monkeypatch.setattr(sys, "argv", "decode --batch 2 --kv-heads 2 --group 3 --prompt 301 --chunk 100 --budget 120 --recent 30 --slack 8 --tokens 30".split())
+    decode.main()
+    res = json.loads(capsys.readouterr().out)
+    assert 0.0 < res["first_chunk_off_by"] < 0.3 and res["token_ms"] > 0
