@@ -370,7 +370,7 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
 int launch_kv_attention(const KvView &c, int dtype, const KvQueries &q, const KvPlan &p, const float *given, float *received,
                         hipStream_t s);
 struct KvSegment {  // of a long memory: see kernels_kv.hip
-    uint32_t above, first, count;
+    uint32_t above, first, count, ties;
 };
 struct KvEvict {
     const float *weights;

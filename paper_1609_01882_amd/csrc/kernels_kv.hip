@@ -1039,7 +1039,7 @@ __device__ __forceinline__ uint32_t claim_of(const KvEvict &e, int seen, float w
 //   kv_pick_kernel    the rest of the claim from these few, and what each segment keeps (a workgroup per kv head)
 //   kv_list_kernel    the lists
 // One workgroup per kv head for all of it took 231 us for 8 x 8 memories of up to 131072 tokens, five passes of which each
-// waits for memory; the four kernels take 70.
+// waits for memory; the four kernels take 64.
 constexpr int kSegmentKeys = 16, kSegment = kEvictThreads * kSegmentKeys, kBins = 2048;
 
 struct Segment {
@@ -1244,9 +1244,19 @@ __global__ __launch_bounds__(kEvictThreads) void kv_gather_kernel(KvView c, KvEv
     __shared__ uint32_t counts[kBins], wave_sum[16], found[2], before_bin;
     const uint32_t *from = e.counts + (int64_t)bh * e.segments * kBins;
     uint32_t a = 0u, b = 0u;
-    for (int s = 0; s < e.segments; ++s) {
-        a += from[(int64_t)s * kBins + tid];
-        b += from[(int64_t)s * kBins + tid + kEvictThreads];
+    for (int s0 = 0; s0 < e.segments; s0 += 8) {  // (eight at a time on their way)
+        uint32_t y[8], z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t at = (int64_t)min(s0 + j, e.segments - 1) * kBins + tid;
+            y[j] = from[at];
+            z[j] = from[at + kEvictThreads];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            a += s0 + j < e.segments ? y[j] : 0u;
+            b += s0 + j < e.segments ? z[j] : 0u;
+        }
     }
     counts[tid] = a;
     counts[tid + kEvictThreads] = b;
@@ -1340,7 +1350,7 @@ __global__ __launch_bounds__(kEvictThreads) void kv_pick_kernel(KvView c, KvEvic
         const Segment seg = segment_of(e, m.n, s);
         const uint32_t ties = min(left, info[s].count), stays = info[s].above + ties;
         left -= ties;
-        info[s].count = ties;
+        info[s].ties = ties;
         info[s].first = seg.below ? holes : later;
         if (seg.below) holes += (uint32_t)(seg.end - seg.begin) - stays;
         else later += stays;
@@ -1365,12 +1375,34 @@ __global__ __launch_bounds__(kEvictThreads) void kv_list_kernel(KvView c, KvEvic
     const KvSegment info = e.info[(int64_t)bh * e.segments + blockIdx.x];
     uint32_t x[kSegmentKeys], all;
     load_claims(e, m, seg.begin, seg.end, x);
-    const int64_t at = (int64_t)bh * e.budget + info.first;
-    list_segment(e, x, seg.begin, seg.end, e.chosen[bh].x, info.count, kept, e.holes + at, e.later + at, wave_sum, &all);
+    const int64_t first = (int64_t)bh * e.budget + info.first;
+    const uint32_t claim = e.chosen[bh].x;
+    if (info.ties != 0u && info.ties != info.count) {
+        list_segment(e, x, seg.begin, seg.end, claim, info.ties, kept, e.holes + first, e.later + first, wave_sum, &all);
+        return;
+    }
+    // none or all of the equal ones: a comparison decides, and the slots lie on one side of the budget
+    const int at = seg.begin + (tid >> 6) * (64 * kSegmentKeys) + lane_id();
+    const auto stays = [&](int j) { return x[j] > claim || (info.ties != 0u && x[j] == claim); };
+    uint32_t mine = 0u;
+#pragma unroll
+    for (int j = 0; j < kSegmentKeys; ++j) mine += (uint32_t)__popcll(ballot64(at + j * 64 < seg.end && stays(j) != seg.below));
+    uint32_t to = waves_before(mine, wave_sum, &all);
+    int32_t *list = (seg.below ? e.holes : e.later) + first;
+#pragma unroll
+    for (int j = 0; j < kSegmentKeys; ++j) {
+        const bool in = at + j * 64 < seg.end, keep = stays(j), listed = in && keep != seg.below;
+        const uint64_t those = ballot64(listed);
+        if (listed) list[to + (uint32_t)prefix_count(those)] = at + j * 64;
+        if (in && seg.below) kept[at + j * 64] = keep ? at + j * 64 : -2;
+        to += (uint32_t)__popcll(those);
+    }
 }
 
-// kMoveLanes lanes to a slot below the budget that stays as it is (its position and weight), and to a free one and the
-// token that it takes: position, weight, codes.  Sources lie at and behind the budget, targets below it: no order is needed.
+// D / 32 lanes to a slot below the budget that stays as it is (its position and weight), and to a free one and the token that
+// it takes: position, weight, codes.  Sources lie at and behind the budget, targets below it: no order is needed.  Bound by
+// the sectors of memory that scattered rows of D / 2 and D / 32 bytes touch (504 thousand tokens of 136 bytes in 45 us); two or
+// four tokens to a lane, to have more on the way: 47 and 60.
 template <int D>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, KvEvict e)
 {
