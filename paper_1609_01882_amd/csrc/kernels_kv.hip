@@ -78,9 +78,9 @@ __device__ __forceinline__ float column_max(float x)
 {
     typedef uint32_t u2 __attribute__((ext_vector_type(2)));
     u2 y = __builtin_bit_cast(u2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-    x = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+    x = __builtin_elementwise_maximum(__uint_as_float(y.x), __uint_as_float(y.y));
     y = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-    return fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+    return __builtin_elementwise_maximum(__uint_as_float(y.x), __uint_as_float(y.y));
 }
 __device__ __forceinline__ float column_sum(float x)
 {
@@ -476,11 +476,11 @@ struct Attention {
         uint32_t p[RT][2][4];  // float16 pairs (the second array: what the first leaves of float32 rows' probabilities)
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            float m = kNegInf;
+            float m = kNegInf;  // (NaN where a score is: the row is lost then, whatever the maximum)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) m = fmaxf(m, s[t][h][r]);
+                for (int r = 0; r < 4; ++r) m = __builtin_elementwise_maximum(m, s[t][h][r]);
             m = column_max(m) * factor;
             if (__any(m > top[t])) {
                 const float now = fmaxf(top[t], m);
@@ -702,13 +702,13 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
     if constexpr (RT == 1)
         if (q.scores && i < m_all) scores = q.scores + (((int64_t)b * c.heads + head) * q.scores_rows + i) * ((int64_t)c.width << c.page_shift);
     if (mine > 0) {
-        Raw<D> raw;
-        int ids = pages_from(0), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
-        load(0, pages, raw);
+        // (two sets of registers in turn: copying the next block's costs 8 % of a block of 32 rows)
+        Raw<D> raw[2];
+        int ids = pages_from(0), pages[2][2] = {{__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)}, {-1, -1}};
+        load(0, pages[0], raw[0]);
         for (int k0 = 0; k0 < mine; k0 += 32) {
             const int ids_then = pages_from(k0 + 32), k_end = min(32, mine - k0);
-            for (int k = 0; k < k_end; ++k) {
-                int next_pages[2];
+            const auto turn = [&](int k, const Raw<D> &now, const int (&now_pages)[2], Raw<D> &next, int (&next_pages)[2]) {
                 if (k < 31) {
                     next_pages[0] = __builtin_amdgcn_readlane(ids, 2 * k + 2);
                     next_pages[1] = __builtin_amdgcn_readlane(ids, 2 * k + 3);
@@ -716,16 +716,16 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
                     next_pages[0] = __builtin_amdgcn_readlane(ids_then, 0);
                     next_pages[1] = __builtin_amdgcn_readlane(ids_then, 1);
                 }
-                Raw<D> next;
                 load(k0 + k + 1, next_pages, next);
                 const int slot = blocks.block(own + (k0 + k) * step) * 32;
-                const bool there = slot + 32 <= s.n && pages[0] >= 0 && pages[1] >= 0 && !kPos;
+                const bool there = slot + 32 <= s.n && now_pages[0] >= 0 && now_pages[1] >= 0 && !kPos;
                 const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
                                    (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-                a.block(c, q, raw, mask, slot, pages[0] >= 0 ? s.n : 0, pages[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
-                raw = next;
-                pages[0] = next_pages[0];
-                pages[1] = next_pages[1];
+                a.block(c, q, now, mask, slot, now_pages[0] >= 0 ? s.n : 0, now_pages[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
+            };
+            for (int k = 0; k < k_end; k += 2) {  // (32 is even: a set's turn does not change from one 32 to the next)
+                turn(k, raw[0], pages[0], raw[1], pages[1]);
+                if (k + 1 < k_end) turn(k + 1, raw[1], pages[1], raw[0], pages[0]);
             }
             ids = ids_then;
         }
