@@ -8,7 +8,9 @@
  * are dropped, the survivors are scored with the asymmetric distance estimator
  * (a sum of per-sub-quantizer table entries, Section 4.2 "ADC") and the best k
  * per query are returned; plus the inverted-file variant with residual codes
- * (Section 4.3) and the all-against-all k-NN-graph mode (Section 5).
+ * (Section 4.3) and the all-against-all k-NN-graph mode (Section 5).  Next to it (psc_kv_*): attention
+ * over a language model's keys and values held in 4 bits, the same comparison of full-precision queries
+ * with compressed vectors.
  *
  * General rules
  *   - Pointers named *_dev are device (HBM) pointers, *_host are host pointers.
@@ -37,6 +39,8 @@
  *     psc_last_error() gives a message for the last failure on the calling thread.
  *     Nothing throws or aborts across this boundary.
  *   - n = 0 or nq = 0 succeed; with n = 0 every result row is padding.
+ *   - The psc_kv_* calls take no index and keep no state; several may run at once on different streams as
+ *     long as none writes what another uses.
  */
 #ifndef PSC_H
 #define PSC_H

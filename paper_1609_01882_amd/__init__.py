@@ -1,7 +1,7 @@
 """Polysemous-code search on AMD MI355X: Python face of libpsc.so (HIP, gfx950).
 
 The compute lives in `csrc/` behind the C ABI declared in `include/psc.h`; this package only
-marshals arguments (see `binding.py`).
+marshals arguments (see `binding.py`; `kv.py` for attention over a memory held in 4 bits).
 """
 from .binding import (  # noqa: F401
     Index,

@@ -133,7 +133,9 @@ __device__ __forceinline__ int sixteen_of(const KvView &c, int b, int head, int 
 }
 
 // ------------------------------------------------------------------------------------------- append, read
-// D / 8 lanes to a (row, head), 8 coordinates of its key and of its value to a lane; four lanes share a scale.
+// D / 8 lanes to a (row, head), 8 coordinates of its key and of its value to a lane; four lanes share a scale, whose largest
+// magnitude they find as integers.  Bound by HBM: 27 thousand rows of 8 heads x 128 float16 (141 MB) in 33 us, 4.3 TB/s;
+// kv_read_kernel gives the same back in 28 us, 5.1 TB/s.
 template <int DT, int D>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRows r)
 {
@@ -427,13 +429,16 @@ __device__ __forceinline__ bool sees(const KvQueries &q, const RowMask &m, int p
 // exp2 of the probability's exponent; values below 2^-126 come out as 0 or denormal, nothing depends on which.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// One wave attends with 16 RT rows over every nwaves-th block of the workgroup's part of the blocks.
+// One wave attends with 16 RT rows over every fourth of the workgroup's blocks.
 //
 // The transposed products keep everything of a row in the lanes of its column: scores K Q^T have the tokens in rows and
 // the rows in columns, so a lane holds 8 scores of one row; they are the operand of V^T P^T as they are, since the
 // order of the tokens inside a product is free as long as both sides agree; and the running maximum, which rescales
 // a column of the output, is the lane's own.  Values have to be transposed for that: a lane takes a run of
 // coordinates of 8 tokens and pairs up the tokens' values of one coordinate with one permutation each.
+// What it is bound by: a few rows read the cache at 5.7 TB/s (8 sequences of 53 to 131 thousand tokens x 8 heads x 128, 825 MB
+// in 145 us); many rows are bound by vector instructions (32 rows x 32 tokens: 16 exp2 of four issue slots each, 64 conversions,
+// 32 permutations, 110 others for 32 products): 2048 rows of 4 x 8 heads over 16384 tokens 653 us, 800 TFLOP/s.
 // Scores, maximum, sum and output are 32-bit floats.  Probabilities are rounded to float16 (at most 2^-11 of each, an
 // eighth of what the output's own rounding to bfloat16 may add); for float32 rows two float16 hold 22 bits.
 template <int D, int DT, int RT, bool kPos>
@@ -914,7 +919,8 @@ __global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQ
 // The same with the scores once more, from the same products as in the attention itself, so that with the row's maximum and
 // sum each probability is the one that was used.  kSplitRows: a workgroup has 32 tokens and each wave a quarter of the rows
 // that can see one; otherwise a wave has 32 tokens and all rows.  The next 16 rows are on their way while 16 are worked on,
-// their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.
+// their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.  Bound by
+// vector instructions (8 exp2 and some 60 others for 16 rows x 32 tokens): 700 rows of 3 x 4 heads x 64 over 5003, 49 us.
 template <int D, int DT, bool kSplitRows>
 __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
 {
@@ -1039,7 +1045,9 @@ __device__ __forceinline__ uint32_t claim_of(const KvEvict &e, int seen, float w
 //   kv_pick_kernel    the rest of the claim from these few, and what each segment keeps (a workgroup per kv head)
 //   kv_list_kernel    the lists
 // One workgroup per kv head for all of it took 231 us for 8 x 8 memories of up to 131072 tokens, five passes of which each
-// waits for memory; the four kernels take 64.
+// waits for memory; the four
+// kernels take 64 (whole call 121.6; with 8, 12, 24, 32 claims to a thread 127, 123, 131, 146): issue of the ballots and the
+// counts' conflicts in LDS, then what each waits for at its start.
 constexpr int kSegmentKeys = 16, kSegment = kEvictThreads * kSegmentKeys, kBins = 2048;
 
 struct Segment {
@@ -1242,6 +1250,8 @@ __global__ __launch_bounds__(kEvictThreads) void kv_gather_kernel(KvView c, KvEv
     if (m.n <= e.budget) return;
     const Segment seg = segment_of(e, m.n, seg_no);
     __shared__ uint32_t counts[kBins], wave_sum[16], found[2], before_bin;
+    uint32_t x[kSegmentKeys];  // (asked for first: they come while the counts are added up)
+    if (seg.begin < seg.end) load_claims(e, m, seg.begin, seg.end, x);
     const uint32_t *from = e.counts + (int64_t)bh * e.segments * kBins;
     uint32_t a = 0u, b = 0u;
     for (int s0 = 0; s0 < e.segments; s0 += 8) {  // (eight at a time on their way)
@@ -1283,8 +1293,7 @@ __global__ __launch_bounds__(kEvictThreads) void kv_gather_kernel(KvView c, KvEv
         if (seg_no == 0) e.chosen[bh] = make_uint2(bin, found[1]);
     }
     if (seg.begin >= seg.end) return;  // (the whole workgroup)
-    uint32_t x[kSegmentKeys], mine = 0u;
-    load_claims(e, m, seg.begin, seg.end, x);
+    uint32_t mine = 0u;
     const int at = seg.begin + (tid >> 6) * (64 * kSegmentKeys) + lane_id();
 #pragma unroll
     for (int j = 0; j < kSegmentKeys; ++j) mine += (uint32_t)__popcll(ballot64(at + j * 64 < seg.end && x[j] >> 21 == bin));
@@ -1600,7 +1609,7 @@ int launch_kv_evict(const KvView &c, KvEvict e, const KvEvictPlan &p, char *ws, 
     ws += 2 * p.list_bytes;
     e.segments = (int)p.segments;
     e.segments_below = (int)p.segments_below;
-    if (p.segments == 1) {
+    if (p.counts_bytes == 0) {
         if ((int64_t)c.width << c.page_shift <= 2 * kEvictThreads) kv_select_kernel<2><<<bh, kEvictThreads, 0, s>>>(c, e);
         else kv_select_kernel<kSegmentKeys><<<bh, kEvictThreads, 0, s>>>(c, e);
     } else {
