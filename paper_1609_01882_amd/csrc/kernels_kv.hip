@@ -917,11 +917,12 @@ __global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQ
 }
 
 // The same with the scores once more, from the same products as in the attention itself, so that with the row's maximum and
-// sum each probability is the one that was used.  kSplitRows: a workgroup has 32 tokens and each wave a quarter of the rows
-// that can see one; otherwise a wave has 32 tokens and all rows.  The next 16 rows are on their way while 16 are worked on,
+// sum each probability is the one that was used.  kSplitRows: a workgroup has 16 kTiles tokens and each wave a quarter of the
+// rows that can see one; otherwise a wave has 16 kTiles tokens and all rows.  The next 16 rows are on their way while 16 are worked on,
 // their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.  Bound by
-// vector instructions (8 exp2 and some 60 others for 16 rows x 32 tokens): 700 rows of 3 x 4 heads x 64 over 5003, 49 us.
-template <int D, int DT, bool kSplitRows>
+// vector instructions (16 exp2 and some 90 others for 16 rows x 64 tokens): up to 701 rows of 3 x 4 heads x 64 over 5003, 40 us
+// (with 32 tokens 52).
+template <int D, int DT, bool kSplitRows, int kTiles>
 __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
@@ -930,18 +931,20 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
     const RowSet s = rows_of(c, q, b);
     const int64_t stride = (int64_t)c.width << c.page_shift, dense = (int64_t)blockIdx.z * stride;
     const int64_t block = kSplitRows ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-    if (block * 32 >= stride) return;  // (with kSplitRows the whole workgroup)
-    const int slot = (int)(block * 32), m_all = s.rows * q.group;
+    if (block * 16 * kTiles >= stride) return;  // (with kSplitRows the whole workgroup)
+    const int slot = (int)(block * 16 * kTiles), m_all = s.rows * q.group;
 
-    float total[2][4] = {};
+    float total[kTiles][4] = {};
     if (slot < s.n && m_all > 0) {
-        const int pages[2] = {sixteen_of(c, b, head, s.n, slot), sixteen_of(c, b, head, s.n, slot + 16)};
-        u32x4 a[2][D / 32];
-        int pos[2][4];
+        int places[kTiles], pos[kTiles][4];
+        bool there = !q.positions;
+        u32x4 a[kTiles][D / 32];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kTiles; ++h) {
             uint32_t k[D / 32], ks;
-            load_keys<D>(c, pages[h], i, g, k, ks);
+            places[h] = sixteen_of(c, b, head, s.n, slot + 16 * h);
+            there = there && places[h] >= 0 && slot + 16 * h + 16 <= s.n;
+            load_keys<D>(c, places[h], i, g, k, ks);
             expand_keys<D, DT>(k, ks, a[h]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -953,10 +956,9 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
         if (!q.positions) {
             if (q.causal) m_begin = max((int64_t)0, (int64_t)slot - s.first_pos) * q.group / 16 * 16;
             if (q.window > 0 && slot >= q.sinks)
-                m_end = min(m_end, max((int64_t)0, (int64_t)slot + 31 + q.window - s.first_pos) * q.group);
+                m_end = min(m_end, max((int64_t)0, (int64_t)slot + 16 * kTiles - 1 + q.window - s.first_pos) * q.group);
         }
-        const bool there = !q.positions && pages[0] >= 0 && pages[1] >= 0 && slot + 32 <= s.n;
-        const int step = kSplitRows ? 64 : 16, places = step / q.group, heads = step % q.group;
+        const int step = kSplitRows ? 64 : 16, more_rows = step / q.group, more_heads = step % q.group;
         int64_t m0 = m_begin + (kSplitRows ? wave * 16 : 0);
         if (m0 < m_end) {
             // the lane's row: place of its sequence, query head of its group
@@ -974,8 +976,8 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
             load((int)m0 + i, place, in_group, rows, st);
             for (; m0 < m_end; m0 += step) {
                 const int m = (int)m0 + i, at = place;
-                place += places;
-                in_group += heads;
+                place += more_rows;
+                in_group += more_heads;
                 if (in_group >= q.group) {
                     in_group -= q.group;
                     ++place;
@@ -984,19 +986,21 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
                 float2 next_st;
                 load((int)min(m0 + step, (int64_t)m_all) + i, place, in_group, next, next_st);
                 const float inv = m < m_all ? st.y : 0.f;
-                f32x4 x[2] = {scores_of<D, DT>(a[0], rows), scores_of<D, DT>(a[1], rows)};
+                f32x4 x[kTiles];
+#pragma unroll
+                for (int h = 0; h < kTiles; ++h) x[h] = scores_of<D, DT>(a[h], rows);
                 const int pos_q = s.first_pos + at;
-                const bool mine = there && (!q.causal || pos_q >= slot + 31) && (q.window <= 0 || (int64_t)pos_q - slot < q.window || slot + 32 <= q.sinks);
+                const bool mine = there && (!q.causal || pos_q >= slot + 16 * kTiles - 1) && (q.window <= 0 || (int64_t)pos_q - slot < q.window || slot + 16 * kTiles <= q.sinks);
                 if (!__all(mine)) {
                     const RowMask mask = row_mask(q, pos_q);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < kTiles; ++h)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (!(pages[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]))) x[h][r] = kNegInf;
+                            if (!(places[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]))) x[h][r] = kNegInf;
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < kTiles; ++h)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) total[h][r] += fmaxf(exp2_fast(__builtin_fmaf(x[h][r], q.factor, -st.x)) * inv, 0.f);
                 rows = next;
@@ -1005,23 +1009,25 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
         }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < kTiles; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int d = 1; d < 16; d *= 2) total[h][r] += __shfl_xor(total[h][r], d);
+    // lane (i, g) of the first 4 kTiles in i: token 4 g + i % 4 of the (i / 4)-th sixteen
     float mine = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mine = i == j ? total[j >> 2][j & 3] : mine;
-    const int in_block = (i & 4) * 4 + 4 * g + (i & 3);
+    for (int j = 0; j < 4 * kTiles; ++j) mine = i == j ? total[j >> 2][j & 3] : mine;
+    const int in_block = (i & ~3) * 4 + 4 * g + (i & 3);
+    const bool one = i < 4 * kTiles;
     if constexpr (kSplitRows) {
-        __shared__ float parts[4][32];
-        if (i < 8) parts[wave][in_block] = mine;
+        __shared__ float parts[4][16 * kTiles];
+        if (one) parts[wave][in_block] = mine;
         __syncthreads();
         if (wave > 0) return;
-        if (i < 8) mine = parts[0][in_block] + parts[1][in_block] + parts[2][in_block] + parts[3][in_block];
+        if (one) mine = parts[0][in_block] + parts[1][in_block] + parts[2][in_block] + parts[3][in_block];
     }
-    if (i < 8 && slot + in_block < stride) received[dense + slot + in_block] = (given ? given[dense + slot + in_block] : 0.f) + mine;
+    if (one && slot + in_block < stride) received[dense + slot + in_block] = (given ? given[dense + slot + in_block] : 0.f) + mine;
 }
 
 // ------------------------------------------------------------------------------------------- eviction
@@ -1513,9 +1519,11 @@ int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const fl
             else if (p.scores_rows <= 4) kv_weights_of_scores_kernel<4><<<grid, 256, 0, s>>>(c, q, given, received);
             else kv_weights_of_scores_kernel<kScoreRows><<<grid, 256, 0, s>>>(c, q, given, received);
         } else if (q.max_rows * (int64_t)q.group > 64) {
-            kv_weights_kernel<D, DT, true><<<dim3((uint32_t)((slots + 31) / 32), 1, groups), 256, 0, s>>>(c, q, given, received);
+            constexpr int kTiles = D == 256 ? 2 : 4;  // sixteens of tokens: as many as leave room for two waves' registers
+            const int64_t tokens = 16 * kTiles;
+            kv_weights_kernel<D, DT, true, kTiles><<<dim3((uint32_t)((slots + tokens - 1) / tokens), 1, groups), 256, 0, s>>>(c, q, given, received);
         } else {
-            kv_weights_kernel<D, DT, false><<<dim3((uint32_t)((slots + 127) / 128), 1, groups), 256, 0, s>>>(c, q, given, received);
+            kv_weights_kernel<D, DT, false, 2><<<dim3((uint32_t)((slots + 127) / 128), 1, groups), 256, 0, s>>>(c, q, given, received);
         }
         PSC_HIP_TRY(hipGetLastError());
     }

@@ -58,6 +58,12 @@ def _dtype(t, name):
     return code
 
 
+def _ints(**values):
+    for name, x in values.items():
+        if not -(1 << 31) <= x < 1 << 31:
+            raise PscError(f"{name}: {x} does not fit 32 bits")
+
+
 @functools.lru_cache(maxsize=1024)
 def _attention_workspace(pages, kv_heads, head_dim, page, batch, width, *sizes):
     return _load().psc_kv_attention_workspace_bytes(_pack(0, 0, 0, 0, pages, kv_heads, head_dim, page, 0, batch, width, 0), *sizes)
@@ -102,6 +108,8 @@ class KvCache:
         return t.data_ptr(), t.stride(0), t.stride(1)
 
     def _stream(self):
+        if torch._C._cuda_getDevice() != self._index:
+            raise PscError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
         return torch._C._cuda_getCurrentRawStream(self._index)
 
     def append(self, k, v, table, lengths, offsets=None, first=None, positions=None, weights=None):
@@ -138,6 +146,7 @@ class KvCache:
         c, batch, slots = self._args(table, lengths)
         n, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
         code, device = _dtype(q, "q"), self._index
+        _ints(window=window, sinks=sinks)
         rows = self._rows(q, heads, "q")
         if offsets is None:
             max_rows = n // max(batch, 1)
@@ -184,6 +193,7 @@ class KvCache:
         `out`: those four, where `lengths`, `positions` and `weights` may be the tensors passed in."""
         c, batch, slots = self._args(table, lengths)
         device, lib = self._index, _load()
+        _ints(budget=budget, sinks=sinks, recent=recent)
         if out is None:
             shape = (batch, self.kv_heads, budget)
             whole = torch.empty((2, *shape), dtype=torch.int32, device=self.device)

@@ -304,6 +304,29 @@ def test_results_repeat_on_another_stream_and_workspace():
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
 
 
+def test_arguments_that_do_not_fit_are_refused():
+    import paper_1609_01882_amd as psc
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    q, w = torch.zeros((2, 4, 64), device="cuda"), torch.zeros((2, 2, 32), device="cuda")
+    attend = lambda **kw: cache.attend(**{**dict(q=q, table=table, lengths=lengths), **kw})  # noqa: E731
+    attend()
+    for bad in (dict(window=1 << 40), dict(window=-1), dict(scale=0.0), dict(q=q.double()), dict(q=q[:, :3]), dict(q=q.cpu()),
+                dict(q=torch.zeros((2, 4, 128), device="cuda")[..., ::2]), dict(q=torch.zeros(2 * 4 * 64 + 1, device="cuda")[1:].view(2, 4, 64)),
+                dict(table=table.long()), dict(table=table.cpu()), dict(lengths=lengths[:1]), dict(lengths=None), dict(positions=w), dict(weights=w),
+                dict(weights_out=w[..., ::2]), dict(offsets=lengths), dict(out=(q, q)), dict(workspace=w), dict(causal=False, window=3)):
+        with pytest.raises(psc.PscError):
+            attend(**bad)
+    with pytest.raises(psc.PscError):
+        cache.append(q[:, :2], q[:, :2].half(), table, lengths)
+    with pytest.raises(psc.PscError):
+        cache.evict(table, lengths, w, 1 << 40)
+    with pytest.raises(psc.PscError):
+        cache.evict(table, lengths, w, 8, sinks=5, recent=4)
+    with pytest.raises(psc.PscError):
+        psc.KvCache(cache.k_codes, cache.k_scales, cache.v_codes[:2], cache.v_scales)
+
+
 # ------------------------------------------------------------------------------------------- eviction
 def _evict_case(seed, dim, heads, page, lengths, budget, sinks=0, recent=0, evicted=False, kind="spread", inplace=False, seen=None):
     import paper_1609_01882_amd as psc
