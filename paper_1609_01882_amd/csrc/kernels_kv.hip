@@ -32,6 +32,17 @@ constexpr int kMinScale = 127 - 23, kMaxScale = 127 + 13;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.693147180559945f;
 
+// Scaled scores so large that neighbouring floats lie 2 or more apart.  A row's maximum is then rounded by so much that the
+// exponents of its probabilities come out above 0 without limit, or all so low that nothing is left.  Such a row is referred to a
+// step or two below its maximum, and exponents above 0 are cut to 0: scores that 32 bits hardly tell apart share the row.
+constexpr float kCoarse = 16777216.f;
+__device__ __forceinline__ bool is_coarse(float top) { return fabsf(top) >= kCoarse && fabsf(top) <= __FLT_MAX__; }
+__device__ __forceinline__ float reference_below(float top)
+{
+    return is_coarse(top) ? fmaxf(__builtin_fmaf(fabsf(top), -0x1p-23f, top), -__FLT_MAX__) : top;
+}
+__device__ __forceinline__ float most_exponent(float reference) { return is_coarse(reference) ? 0.f : -kNegInf; }
+
 template <int DT>
 struct Element;  // what a row's coordinates are stored as
 template <>
@@ -447,6 +458,8 @@ struct Attention {
     float top[RT], sum[RT];  // of the scaled scores in units of log 2; the sum is the lane's own share
     Rows<D, DT> rows[RT];
 
+    // kFar: rows whose scores are coarse may be among them
+    template <bool kFar>
     __device__ void block(const KvView &c, const KvQueries &q, const Raw<D> &raw, const RowMask (&mask)[RT], int slot, int lim0,
                           int lim1, int n, bool whole, float factor, int i, int g, float *scores)
     {
@@ -488,7 +501,7 @@ struct Attention {
                 for (int r = 0; r < 4; ++r) m = __builtin_elementwise_maximum(m, s[t][h][r]);
             m = column_max(m) * factor;
             if (__any(m > top[t])) {
-                const float now = fmaxf(top[t], m);
+                const float now = fmaxf(top[t], kFar ? reference_below(m) : m);
                 const float shrink = now == kNegInf ? 1.f : exp2_fast(top[t] - now);
                 top[t] = now;
                 sum[t] *= shrink;
@@ -500,8 +513,14 @@ struct Attention {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; r += 2) {
-                    const float e0 = exp2_fast(__builtin_fmaf(s[t][h][r], factor, -base));
-                    const float e1 = exp2_fast(__builtin_fmaf(s[t][h][r + 1], factor, -base));
+                    float e0 = __builtin_fmaf(s[t][h][r], factor, -base), e1 = __builtin_fmaf(s[t][h][r + 1], factor, -base);
+                    if constexpr (kFar) {
+                        const float most = most_exponent(base);
+                        e0 = __builtin_elementwise_minimum(e0, most);  // (NaN stays)
+                        e1 = __builtin_elementwise_minimum(e1, most);
+                    }
+                    e0 = exp2_fast(e0);
+                    e1 = exp2_fast(e1);
                     sum[t] += e0 + e1;
                     const h16x2 hi = {(_Float16)e0, (_Float16)e1};
                     p[t][0][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, hi);
@@ -674,10 +693,6 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
         const int m = min(m0 + t * 16 + i, m_all - 1), place = m / q.group;  // (rows past the last: the last one again)
         load_rows<D, DT>(q, s.first_row + place, head * q.group + m - place * q.group, g, a.rows[t]);
         mask[t] = row_mask(q, s.first_pos + place);
-        a.top[t] = kNegInf;
-        a.sum[t] = 0.f;
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) a.acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int64_t dense = ((int64_t)b * c.heads + head) * ((int64_t)c.width << c.page_shift);
 
@@ -706,7 +721,15 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
     float *scores = nullptr;
     if constexpr (RT == 1)
         if (q.scores && i < m_all) scores = q.scores + (((int64_t)b * c.heads + head) * q.scores_rows + i) * ((int64_t)c.width << c.page_shift);
-    if (mine > 0) {
+    const auto all_blocks = [&](auto far) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            a.top[t] = kNegInf;
+            a.sum[t] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) a.acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (mine <= 0) return;
         // (two sets of registers in turn: copying the next block's costs 8 % of a block of 32 rows)
         Raw<D> raw[2];
         int ids = pages_from(0), pages[2][2] = {{__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)}, {-1, -1}};
@@ -726,7 +749,7 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
                 const bool there = slot + 32 <= s.n && now_pages[0] >= 0 && now_pages[1] >= 0 && !kPos;
                 const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
                                    (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-                a.block(c, q, now, mask, slot, now_pages[0] >= 0 ? s.n : 0, now_pages[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
+                a.template block<far.value>(c, q, now, mask, slot, now_pages[0] >= 0 ? s.n : 0, now_pages[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
             };
             for (int k = 0; k < k_end; k += 2) {  // (32 is even: a set's turn does not change from one 32 to the next)
                 turn(k, raw[0], pages[0], raw[1], pages[1]);
@@ -734,7 +757,13 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
             }
             ids = ids_then;
         }
-    }
+    };
+    all_blocks(std::false_type());
+    // (decided once at the end, and all done again: a look at every block costs 2 to 3 % of a large chunk)
+    bool far = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) far = far || is_coarse(a.top[t]);
+    if (__any(far)) all_blocks(std::true_type());
 #pragma unroll
     for (int t = 0; t < RT; ++t) a.sum[t] = column_sum(a.sum[t]);
     if (g == 0) {
@@ -904,10 +933,10 @@ __global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQ
             for (int m = 0; m < N; ++m) {
                 const int mm = min(m, m_all - 1);
                 const float2 st = *(const float2 *)(q.stat + ((int64_t)(s.first_row + mm / q.group) * q.q_heads + head * q.group + mm % q.group) * 2);
-                const float inv = m < m_all ? st.y : 0.f;
+                const float inv = m < m_all ? st.y : 0.f, most = most_exponent(st.x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)  // (the larger of NaN and 0 is 0: rows that came out NaN add nothing)
-                    sum[j] += fmaxf(exp2_fast(__builtin_fmaf(x[m][j], q.factor, -st.x)) * inv, 0.f);
+                    sum[j] += fmaxf(exp2_fast(fminf(__builtin_fmaf(x[m][j], q.factor, -st.x), most)) * inv, 0.f);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) total[j] += slot + j < s.n ? sum[j] : 0.f;
@@ -990,7 +1019,7 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
 #pragma unroll
                 for (int h = 0; h < kTiles; ++h) x[h] = scores_of<D, DT>(a[h], rows);
                 const int pos_q = s.first_pos + at;
-                const bool mine = there && (!q.causal || pos_q >= slot + 16 * kTiles - 1) && (q.window <= 0 || (int64_t)pos_q - slot < q.window || slot + 16 * kTiles <= q.sinks);
+                const bool coarse = is_coarse(st.x), mine = there && !coarse && (!q.causal || pos_q >= slot + 16 * kTiles - 1) && (q.window <= 0 || (int64_t)pos_q - slot < q.window || slot + 16 * kTiles <= q.sinks);
                 if (!__all(mine)) {
                     const RowMask mask = row_mask(q, pos_q);
 #pragma unroll
@@ -998,6 +1027,14 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             if (!(places[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]))) x[h][r] = kNegInf;
+                    if (__any(coarse)) {  // such rows' scores become their exponents over the factor
+                        const float inverse = 1.f / q.factor;
+#pragma unroll
+                        for (int h = 0; h < kTiles; ++h)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) x[h][r] = coarse ? fminf(__builtin_fmaf(x[h][r], q.factor, -st.x), 0.f) * inverse : x[h][r];
+                        st.x = coarse ? 0.f : st.x;
+                    }
                 }
 #pragma unroll
                 for (int h = 0; h < kTiles; ++h)

@@ -1,0 +1,67 @@
+"""Attention memory in 4 bits (`psc_kv_*`, needs an MI355X) where it is easy to get wrong: tails of a softmax, very large
+scores, calls without rows, rows and slots that nothing stands behind."""
+import numpy as np
+import pytest
+import torch
+
+import kv_util as U
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+
+
+def _cuda(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def _softmax_case(dtype, scores, v, q, buffers, n, scale, score_error, rows, group, page, weights):
+    """attend against the softmax of `scores` [rows * group, n] (float64, what the held keys and q give), values v [n, dim].
+    Tolerances: a probability is off by score_error [rows * group, 1] (relative), by its two float16 or one and by half a
+    step of 2^-39 of the largest; a sum of n float32 terms by sqrt(n) + n / 64 roundings, exp2 and the rest by 8."""
+    import paper_1609_01882_amd as psc
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    table = torch.arange(buffers[0].shape[0], dtype=torch.int32, device="cuda")[None]
+    received = torch.full((1, 1, buffers[0].shape[0] * page), np.nan, device="cuda") if weights else None
+    out, lse = cache.attend(q.cuda().view(rows, group, -1), table, torch.tensor([n], dtype=torch.int32, device="cuda"), causal=False,
+                            scale=scale, weights_out=received)
+    top = scores.max(-1, keepdims=True)
+    e = np.exp(scores - top)
+    p = e / e.sum(-1, keepdims=True)
+    want, size, least = p @ v, p @ np.abs(v), 2.0 ** -40 * np.abs(v).sum(0) / e.sum(-1, keepdims=True)
+    unit_p = U.UNIT["f16"] ** 2 if dtype == "f32" else U.UNIT["f16"]
+    off = score_error + (8 + np.sqrt(n) + n / 64) * EPS
+    tol = U.UNIT[dtype] * np.abs(want) + (unit_p + off) * size + least
+    worst = np.max(np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / (1.01 * tol))
+    assert worst <= 1.0, f"out: {worst} times the tolerance"
+    want = (top + np.log(e.sum(-1, keepdims=True)))[:, 0]
+    worst = np.max(np.abs(lse.double().cpu().numpy().reshape(-1) - want) / (off[:, 0] + 16 * EPS * np.abs(want)))
+    assert worst <= 1.0, f"lse: {worst} times the tolerance"
+    if weights:
+        got, want = received.double().cpu().numpy()[0, 0, :n], p.sum(0)
+        worst = np.max(np.abs(got - want) / ((p * off).sum(0) + 4 * EPS * want + 2.0 ** -125))
+        assert worst <= 1.0, f"weights: {worst} times the tolerance"
+
+
+# ------------------------------------------------------------------------------------------- very large scores
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n,rows,group", [(100, 1, 1), (100, 5, 3), (4096, 1, 8), (700, 90, 1)])
+def test_scores_beyond_the_integers_of_a_float(dtype, sign, n, rows, group):
+    """Scores up to 2^40 (float16: 2^29), whose products with the scale are rounded by more than exp2 can take: the largest
+    ones share the row.  Rows with ordinary scores beside them stay as exact as ever."""
+    rng = np.random.default_rng(n + rows)
+    dim, page, scale = 64, 64, 0.125
+    pages = -(-n // page)
+    buffers = [np.zeros((pages, 1, page, dim // d), np.uint8) for d in (2, 32, 2, 32)]
+    k, ks, v, vs = (b[:, 0].reshape(pages * page, -1) for b in buffers)
+    ks[:], vs[:] = 127 + 10, 126
+    k[:, 0] = rng.integers(1, 8, pages * page)
+    v[:] = rng.integers(0, 256, v.shape)
+    sizes = 2.0 ** np.array([-13, 18, 5, 20, 14, 3, 30, 24, 27] if dtype != "f16" else [-13, 13, 5, 15, 14, 3, 12, 11, 10])
+    q = torch.zeros((rows * group, dim), dtype=U.TYPES[dtype])
+    q[:, 0] = torch.from_numpy(sign * 1.3671875 * np.resize(sizes if rows * group > 1 else sizes[3:], rows * group)).to(q.dtype)
+    scores = scale * q[:, :1].double().numpy() * U.values(k, ks)[None, :n, 0]
+    size = np.abs(scores).max(-1, keepdims=True)
+    # (from 2^10 on two different scores are so far apart that only the largest remains)
+    print(f"large {dtype} n={n} rows={rows}x{group} sign={sign}", flush=True)
+    _softmax_case(dtype, scores, U.values(v, vs)[:n], q, buffers, n, scale, np.where(size < 1024, 8 * EPS * size, 0.0), rows, group, page, True)
