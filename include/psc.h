@@ -427,7 +427,8 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
  * weights_out_dev (may be NULL), per slot: weights_in_dev (NULL: 0) + the sum of p over the sequence's rows and the kv
  * head's query heads; 0 is added in slots that no row sees, rows that come out NaN add nothing.  The two may be the same.
  * Held values enter the products exactly, rows as they are; scores, sums and softmax are float32; probabilities are
- * rounded to float16 for the second product (float32 rows: to 22 bits).  Results do not depend on timing: nothing is
+ * rounded for the second product, by at most 2^-11 of each (float32 rows, of whatever origin: 2^-22) or 2^-40 of the
+ * row's largest, whichever is more; not for the weights.  Results do not depend on timing: nothing is
  * added atomically.  Where slots are positions (positions_dev NULL), tokens that a window hides are not read.
  * Workspace: psc_kv_attention_workspace_bytes (may be 0: workspace_dev may then be NULL). */
 size_t psc_kv_attention_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,

@@ -350,7 +350,7 @@ struct KvQueries {
     int unit_rows;                // rows (times query heads) of a unit
     uint32_t workgroups, least_blocks;
     float *part_stat, *part_acc;  // [most_parts][unit_rows][2], [...][dim]
-    float *stat;                  // [nrows][q_heads][2]: maximum (units of log 2), 1 / sum
+    float *stat;                  // [nrows][q_heads][2]: reference (units of log 2), 1 / sum over it
     float *scores;                // [batch][kv_heads][scores_rows][slots], or null
     int scores_rows;
 };

@@ -32,16 +32,24 @@ constexpr int kMinScale = 127 - 23, kMaxScale = 127 + 13;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.693147180559945f;
 
+// A row's probabilities are held as 2^kLift p / (the largest p so far) until the row is done: float16 keeps 11 bits of those down
+// to 2^-29 of the largest, and steps of 2^-39 of it below, where 1 as the largest would leave 2^-14 and 2^-24 (a long
+// tail that far below one token was lost from the output and not from the sum).  What a row is referred to (its maximum less
+// kLift) takes the lift into sums and accumulators alike, and quotients are free of it.
+constexpr float kLift = 15.f;
+
 // Scaled scores so large that neighbouring floats lie 2 or more apart.  A row's maximum is then rounded by so much that the
-// exponents of its probabilities come out above 0 without limit, or all so low that nothing is left.  Such a row is referred to a
-// step or two below its maximum, and exponents above 0 are cut to 0: scores that 32 bits hardly tell apart share the row.
+// exponents of its probabilities come out above kLift without limit, or all so low that nothing is left.  Such a row is referred
+// to a step or two further down, and exponents above kLift are cut to it: scores that 32 bits hardly tell apart share the row.
 constexpr float kCoarse = 16777216.f;
 __device__ __forceinline__ bool is_coarse(float top) { return fabsf(top) >= kCoarse && fabsf(top) <= __FLT_MAX__; }
-__device__ __forceinline__ float reference_below(float top)
+__device__ __forceinline__ float reference_below(float top)  // (coarse as well)
 {
-    return is_coarse(top) ? fmaxf(__builtin_fmaf(fabsf(top), -0x1p-23f, top), -__FLT_MAX__) : top;
+    return is_coarse(top) ? fmaxf(__builtin_fmaf(fabsf(top), -0x1p-23f, top), top > 0.f ? kCoarse : -__FLT_MAX__) : top;
 }
-__device__ __forceinline__ float most_exponent(float reference) { return is_coarse(reference) ? 0.f : -kNegInf; }
+__device__ __forceinline__ float most_exponent(float reference) { return is_coarse(reference) ? kLift : -kNegInf; }
+// log(sum of exp s) from a row's reference and the sum over it (the lift leaves both first: near 0 it would cost bits).
+__device__ __forceinline__ float log_sum(float reference, float sum) { return (reference + kLift + __log2f(sum * 0x1p-15f)) * kLn2; }
 
 template <int DT>
 struct Element;  // what a row's coordinates are stored as
@@ -450,12 +458,13 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // What it is bound by: a few rows read the cache at 5.7 TB/s (8 sequences of 53 to 131 thousand tokens x 8 heads x 128, 825 MB
 // in 145 us); many rows are bound by vector instructions (32 rows x 32 tokens: 16 exp2 of four issue slots each, 64 conversions,
 // 32 permutations, 110 others for 32 products): 2048 rows of 4 x 8 heads over 16384 tokens 653 us, 800 TFLOP/s.
-// Scores, maximum, sum and output are 32-bit floats.  Probabilities are rounded to float16 (at most 2^-11 of each, an
-// eighth of what the output's own rounding to bfloat16 may add); for float32 rows two float16 hold 22 bits.
+// Scores, maximum, sum and output are 32-bit floats.  Probabilities are rounded to float16: by at most 2^-11 of each, an
+// eighth of what the output's own rounding to bfloat16 may add (float32 rows: two float16, 2^-22 of each down to 2^-18 of the
+// largest), and never by more than 2^-40 of the row's largest beyond that (kLift).
 template <int D, int DT, int RT, bool kPos>
 struct Attention {
     f32x4 acc[RT][D / 16];
-    float top[RT], sum[RT];  // of the scaled scores in units of log 2; the sum is the lane's own share
+    float top[RT], sum[RT];  // of the scaled scores in units of log 2, the maximum less kLift; the sum is the lane's own share
     Rows<D, DT> rows[RT];
 
     // kFar: rows whose scores are coarse may be among them
@@ -499,7 +508,7 @@ struct Attention {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) m = __builtin_elementwise_maximum(m, s[t][h][r]);
-            m = column_max(m) * factor;
+            m = __builtin_fmaf(column_max(m), factor, -kLift);
             if (__any(m > top[t])) {
                 const float now = fmaxf(top[t], kFar ? reference_below(m) : m);
                 const float shrink = now == kNegInf ? 1.f : exp2_fast(top[t] - now);
@@ -811,7 +820,7 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
                 const int64_t row = (int64_t)(s.first_row + m / q.group) * q.q_heads + head * q.group + m % q.group;
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 if (run == 0) {
-                    if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (best + __log2f(sum)) * kLn2;
+                    if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : log_sum(best, sum);
                     if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(best == kNegInf ? 0.f : best, inv);
                 }
 #pragma unroll
@@ -898,7 +907,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, KvQueries q)
     for (int j = 0; j < D / 16; ++j) x[j] = column_sum(x[j]);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     if (lane == 0) {
-        if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : (top + __log2f(sum)) * kLn2;
+        if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : log_sum(top, sum);
         if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(top == kNegInf ? 0.f : top, inv);
     }
 #pragma unroll
@@ -945,8 +954,8 @@ __global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQ
     *(f32x4 *)(received + dense + slot) = total;
 }
 
-// The same with the scores once more, from the same products as in the attention itself, so that with the row's maximum and
-// sum each probability is the one that was used.  kSplitRows: a workgroup has 16 kTiles tokens and each wave a quarter of the
+// The same with the scores once more, from the same products as in the attention itself, so that with the row's reference and
+// sum each probability is the one that was used, before it was rounded.  kSplitRows: a workgroup has 16 kTiles tokens and each wave a quarter of the
 // rows that can see one; otherwise a wave has 16 kTiles tokens and all rows.  The next 16 rows are on their way while 16 are worked on,
 // their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.  Bound by
 // vector instructions (16 exp2 and some 90 others for 16 rows x 64 tokens): up to 701 rows of 3 x 4 heads x 64 over 5003, 40 us
@@ -1032,7 +1041,7 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
 #pragma unroll
                         for (int h = 0; h < kTiles; ++h)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) x[h][r] = coarse ? fminf(__builtin_fmaf(x[h][r], q.factor, -st.x), 0.f) * inverse : x[h][r];
+                            for (int r = 0; r < 4; ++r) x[h][r] = coarse ? fminf(__builtin_fmaf(x[h][r], q.factor, -st.x), kLift) * inverse : x[h][r];
                         st.x = coarse ? 0.f : st.x;
                     }
                 }

@@ -65,3 +65,32 @@ def test_scores_beyond_the_integers_of_a_float(dtype, sign, n, rows, group):
     # (from 2^10 on two different scores are so far apart that only the largest remains)
     print(f"large {dtype} n={n} rows={rows}x{group} sign={sign}", flush=True)
     _softmax_case(dtype, scores, U.values(v, vs)[:n], q, buffers, n, scale, np.where(size < 1024, 8 * EPS * size, 0.0), rows, group, page, True)
+
+
+# ------------------------------------------------------------------------------------------- tails
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("gap", [14, 16, 18])
+@pytest.mark.parametrize("n,rows,group", [(2000, 1, 1), (4096, 1, 4), (131_072, 1, 2), (2000, 20, 2), (5000, 3, 8)])
+@pytest.mark.parametrize("sink_at", [0, -1])
+def test_a_long_tail_far_below_one_token(dtype, gap, n, rows, group, sink_at):
+    """One token without a value scores `gap` above thousands of others, which are all that comes out: their probabilities,
+    some 2^-20 to 2^-26 of the largest, have to be held as well as the largest is."""
+    rng = np.random.default_rng(n + gap)
+    dim, page = 64, 64
+    pages = -(-n // page)
+    buffers = [np.zeros((pages, 1, page, dim // d), np.uint8) for d in (2, 32, 2, 32)]
+    k, ks, v, vs = (b[:, 0].reshape(pages * page, -1) for b in buffers)
+    ks[:, 0], ks[:, 1], vs[:] = 129, 124, 126
+    k[:, dim // 4:] = rng.integers(0, 256, (pages * page, dim // 4))
+    v[:] = rng.integers(1, 8, v.shape) | rng.integers(1, 8, v.shape) << 4          # all above zero: nothing cancels
+    sink = sink_at % n
+    k[sink], v[sink] = 0, 0
+    k[sink, 0] = 6                                                                 # 4 * 2^2
+    q = torch.from_numpy(0.5 * rng.normal(size=(rows * group, dim))).to(U.TYPES[dtype])
+    q[:, :dim // 2] = 0.0
+    q[:, 0] = gap / 16
+    kv, qv = U.values(k, ks)[:n], q.double().numpy()
+    scores = qv @ kv.T
+    span = (np.abs(qv) @ np.abs(kv).T).max(-1, keepdims=True)
+    print(f"tail {dtype} gap={gap} n={n} rows={rows}x{group}", flush=True)
+    _softmax_case(dtype, scores, U.values(v, vs)[:n], q, buffers, n, 1.0, 2 * (dim + 4) * EPS * span + 4 * EPS * gap, rows, group, page, True)
