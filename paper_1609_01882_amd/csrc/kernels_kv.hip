@@ -299,7 +299,6 @@ struct Raw {
     uint32_t k[2][D / 32], ks[2];
     uint32_t v[8][D == 256 ? 2 : 1];
     uint32_t vs[2][4];  // of the tokens' scale bytes the words that hold the lane's (value_scale)
-    int pos[8];         // positions of the value tokens, where they have some of their own
 };
 // The lane's scale byte of token r of four, in the place of a float's exponent.  The conversions look at these eight bits
 // alone, so the others may hold what they like.
@@ -469,7 +468,7 @@ struct Attention {
 
     // kFar: rows whose scores are coarse may be among them
     template <bool kFar>
-    __device__ void block(const KvView &c, const KvQueries &q, const Raw<D> &raw, const RowMask (&mask)[RT], int slot, int lim0,
+    __device__ void block(const KvView &c, const KvQueries &q, const Raw<D> &raw, const int (&positions)[8], const RowMask (&mask)[RT], int slot, int lim0,
                           int lim1, int n, bool whole, float factor, int i, int g, float *scores)
     {
         f32x4 s[RT][2];
@@ -487,7 +486,7 @@ struct Attention {
                 for (int r = 0; r < 4; ++r) {
                     const int at = slot + 16 * h + 4 * g + r;
                     const bool there = at < (h ? lim1 : lim0);
-                    const int pos = kPos ? raw.pos[4 * h + r] : at;
+                    const int pos = kPos ? positions[4 * h + r] : at;
 #pragma unroll
                     for (int t = 0; t < RT; ++t)
                         if (!(there && sees(q, mask[t], pos))) s[t][h][r] = kNegInf;
@@ -697,12 +696,19 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
 
     Attention<D, DT, RT, kPos> a;
     RowMask mask[RT];
+    const auto start = [&] {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int m = min(m0 + t * 16 + i, m_all - 1), place = m / q.group;  // (rows past the last: the last one again)
-        load_rows<D, DT>(q, s.first_row + place, head * q.group + m - place * q.group, g, a.rows[t]);
-        mask[t] = row_mask(q, s.first_pos + place);
-    }
+        for (int t = 0; t < RT; ++t) {
+            const int m = min(m0 + t * 16 + i, m_all - 1), place = m / q.group;  // (rows past the last: the last one again)
+            load_rows<D, DT>(q, s.first_row + place, head * q.group + m - place * q.group, g, a.rows[t]);
+            mask[t] = row_mask(q, s.first_pos + place);
+            a.top[t] = kNegInf;
+            a.sum[t] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) a.acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    start();
     const int64_t dense = ((int64_t)b * c.heads + head) * ((int64_t)c.width << c.page_shift);
 
     // The places of 32 of the wave's blocks are held across the lanes; the codes of the block after the one that is worked on
@@ -716,13 +722,20 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
         for (int h = 0; h < 2; ++h) {
             load_keys<D>(c, pg[h], i, g, r.k[h], r.ks[h]);
             load_values<D>(c, pg[h], i, g, &r.v[4 * h], r.vs[h]);
-            if constexpr (kPos) {
-                const int sl = blocks.block(min(own + k * step, end - 1)) * 32;
+        }
+    };
+    // positions of the value tokens of a block, where they have some of their own (asked for when the block is worked on: held
+    // for the next one too they would not fit the registers)
+    auto load_positions = [&](int k, int (&pos)[8]) {
+        if constexpr (kPos) {
+            const int sl = blocks.block(min(own + k * step, end - 1)) * 32;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
                 const int4 x = *(const int4 *)(q.positions + dense + min(sl + 16 * h, (c.width << c.page_shift) - 16) + 4 * g);
-                r.pos[4 * h] = x.x;
-                r.pos[4 * h + 1] = x.y;
-                r.pos[4 * h + 2] = x.z;
-                r.pos[4 * h + 3] = x.w;
+                pos[4 * h] = x.x;
+                pos[4 * h + 1] = x.y;
+                pos[4 * h + 2] = x.z;
+                pos[4 * h + 3] = x.w;
             }
         }
     };
@@ -730,15 +743,14 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
     float *scores = nullptr;
     if constexpr (RT == 1)
         if (q.scores && i < m_all) scores = q.scores + (((int64_t)b * c.heads + head) * q.scores_rows + i) * ((int64_t)c.width << c.page_shift);
-    const auto all_blocks = [&](auto far) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            a.top[t] = kNegInf;
-            a.sum[t] = 0.f;
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) a.acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        if (mine <= 0) return;
+    const auto work = [&](auto far, int k, const Raw<D> &raw, const int (&pos)[8], const int (&pg)[2]) {
+        const int slot = blocks.block(own + k * step) * 32;
+        const bool there = slot + 32 <= s.n && pg[0] >= 0 && pg[1] >= 0 && !kPos;
+        const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
+                           (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
+        a.template block<far.value>(c, q, raw, pos, mask, slot, pg[0] >= 0 ? s.n : 0, pg[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
+    };
+    if (mine > 0) {
         // (two sets of registers in turn: copying the next block's costs 8 % of a block of 32 rows)
         Raw<D> raw[2];
         int ids = pages_from(0), pages[2][2] = {{__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)}, {-1, -1}};
@@ -753,12 +765,10 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
                     next_pages[0] = __builtin_amdgcn_readlane(ids_then, 0);
                     next_pages[1] = __builtin_amdgcn_readlane(ids_then, 1);
                 }
+                int pos[8];
+                load_positions(k0 + k, pos);
                 load(k0 + k + 1, next_pages, next);
-                const int slot = blocks.block(own + (k0 + k) * step) * 32;
-                const bool there = slot + 32 <= s.n && now_pages[0] >= 0 && now_pages[1] >= 0 && !kPos;
-                const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
-                                   (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-                a.template block<far.value>(c, q, now, mask, slot, now_pages[0] >= 0 ? s.n : 0, now_pages[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores);
+                work(std::false_type(), k0 + k, now, pos, now_pages);
             };
             for (int k = 0; k < k_end; k += 2) {  // (32 is even: a set's turn does not change from one 32 to the next)
                 turn(k, raw[0], pages[0], raw[1], pages[1]);
@@ -766,13 +776,24 @@ __device__ __forceinline__ void attend_unit(const KvView &c, const KvQueries &q,
             }
             ids = ids_then;
         }
-    };
-    all_blocks(std::false_type());
-    // (decided once at the end, and all done again: a look at every block costs 2 to 3 % of a large chunk)
+    }
+    // Decided at the end, and all done again: a look at every block costs 2 to 3 % of a large chunk.
     bool far = false;
 #pragma unroll
     for (int t = 0; t < RT; ++t) far = far || is_coarse(a.top[t]);
-    if (__any(far)) all_blocks(std::true_type());
+    if (__any(far)) {
+        asm volatile("" ::: "memory");  // (the rows are read again: kept, they would cost the pass above registers)
+        start();
+#pragma unroll 1
+        for (int k = 0; k < mine; ++k) {
+            const int ids = pages_from(k), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
+            int pos[8];
+            load_positions(k, pos);
+            Raw<D> raw;
+            load(k, pages, raw);
+            work(std::true_type(), k, raw, pos, pages);
+        }
+    }
 #pragma unroll
     for (int t = 0; t < RT; ++t) a.sum[t] = column_sum(a.sum[t]);
     if (g == 0) {
