@@ -158,7 +158,7 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
     PSC_REQUIRE(weights_out_dev || !weights_in_dev, "weights_in without weights_out");
     PSC_REQUIRE(aligned(first_dev, 4) && aligned(positions_dev) && aligned(weights_in_dev) && aligned(weights_out_dev) && aligned(lse_dev, 4),
                 "misaligned first, positions, weights or lse");
-    if (!offsets_dev) max_rows = nrows / v.batch;
+    if (!offsets_dev || nrows == 0) max_rows = nrows / v.batch;
     PSC_REQUIRE(nrows == 0 || max_rows >= 1, "max_rows must be at least 1");
     if (nrows > 0) {
         PSC_TRY(check_strides("q", q_dev, dtype, q_row_stride, q_head_stride));

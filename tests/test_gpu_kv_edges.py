@@ -94,3 +94,17 @@ def test_a_long_tail_far_below_one_token(dtype, gap, n, rows, group, sink_at):
     span = (np.abs(qv) @ np.abs(kv).T).max(-1, keepdims=True)
     print(f"tail {dtype} gap={gap} n={n} rows={rows}x{group}", flush=True)
     _softmax_case(dtype, scores, U.values(v, vs)[:n], q, buffers, n, 1.0, 2 * (dim + 4) * EPS * span + 4 * EPS * gap, rows, group, page, True)
+
+
+# ------------------------------------------------------------------------------------------- no rows
+def test_no_rows_of_sequences_that_could_have_some():
+    """A step in which no sequence has a row, over a table of many pages: weights go through as they are."""
+    import paper_1609_01882_amd as psc
+    cache = psc.KvCache.empty(8, 2, 128, 32)
+    table = torch.full((3, 4096), -1, dtype=torch.int32, device="cuda")
+    lengths = torch.zeros(3, dtype=torch.int32, device="cuda")
+    w, out = torch.rand((3, 2, 4096 * 32), device="cuda"), torch.full((3, 2, 4096 * 32), np.nan, device="cuda")
+    q, offsets = torch.empty((0, 4, 128), device="cuda").half(), torch.zeros(4, dtype=torch.int32, device="cuda")
+    o, lse = cache.attend(q, table, lengths, offsets=offsets, max_rows=4, weights=w, weights_out=out)
+    assert o.shape == (0, 4, 128) and lse.shape == (0, 4) and torch.equal(w, out)
+    cache.attend(q, table, lengths, offsets=offsets, max_rows=4)
