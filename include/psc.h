@@ -430,7 +430,8 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
  * rounded for the second product, by at most 2^-11 of each (float32 rows, of whatever origin: 2^-22) or 2^-40 of the
  * row's largest, whichever is more; not for the weights.  Results do not depend on timing: nothing is
  * added atomically.  Where slots are positions (positions_dev NULL), tokens that a window hides are not read.
- * Workspace: psc_kv_attention_workspace_bytes (may be 0: workspace_dev may then be NULL). */
+ * Workspace: psc_kv_attention_workspace_bytes for the same sizes, enough with offsets_dev and without (may be 0:
+ * workspace_dev may then be NULL). */
 size_t psc_kv_attention_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
                                         int window, int sinks, int has_positions, int has_weights);
 int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,

@@ -1,4 +1,5 @@
 // C ABI of the attention memory in 4 bits: argument checking and dispatch.  See include/psc.h for the contract.
+#include <algorithm>
 #include <cmath>
 #include <cstdlib>
 
@@ -139,8 +140,12 @@ size_t psc_kv_attention_workspace_bytes(const psc_kv_cache *cache, int dtype, in
 {
     KvView v{};
     if (check_cache(cache, &v) != PSC_OK || check_attention(v, dtype, nrows, max_rows, q_heads, window, sinks) != PSC_OK) return 0;
-    if (nrows == 0 || max_rows == 0) return 0;
-    return plan_kv_attention(v, dtype, q_heads / v.heads, nrows, max_rows, window, sinks, !has_positions, has_weights != 0).bytes();
+    if (nrows == 0) return 0;
+    // with offsets the call plans for max_rows, without for nrows / batch; neither plan contains the other
+    const auto bytes = [&](int most) {
+        return plan_kv_attention(v, dtype, q_heads / v.heads, nrows, most, window, sinks, !has_positions, has_weights != 0).bytes();
+    };
+    return std::max(bytes(max_rows), bytes((int)(((int64_t)nrows + v.batch - 1) / v.batch)));
 }
 
 int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,

@@ -108,3 +108,20 @@ def test_no_rows_of_sequences_that_could_have_some():
     o, lse = cache.attend(q, table, lengths, offsets=offsets, max_rows=4, weights=w, weights_out=out)
     assert o.shape == (0, 4, 128) and lse.shape == (0, 4) and torch.equal(w, out)
     cache.attend(q, table, lengths, offsets=offsets, max_rows=4)
+
+
+def test_a_workspace_sized_with_another_most_than_the_call_uses():
+    """Without offsets `max_rows` is not used by the call, so whatever it was sized with has to be enough."""
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(3)
+    cache = psc.KvCache(*(_cuda(x) for x in U.random_cache(rng, 8, 2, 32, 128)))
+    table = torch.full((3, 4096), -1, dtype=torch.int32, device="cuda")
+    table[:, :2] = torch.arange(6, dtype=torch.int32, device="cuda").view(3, 2)
+    lengths = torch.tensor([64, 50, 30], dtype=torch.int32, device="cuda")
+    for rows in (60, 3, 600):
+        q = torch.randn((rows, 4, 128), device="cuda").bfloat16()
+        want = cache.attend(q, table, lengths)
+        for most in (0, 1, rows, 5000):
+            size = cache.attend_workspace_bytes(3, 4096, rows, most, 4, q.dtype)
+            got = cache.attend(q, table, lengths, workspace=torch.empty(size, dtype=torch.uint8, device="cuda"))
+            assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])

@@ -1,0 +1,30 @@
+"""Sizes and refusals of the attention memory's calls at their limits (no GPU: nothing is launched)."""
+import ctypes as C
+import os
+
+import pytest
+
+from test_kv_host import A, _append, _attend, _cache, _evict
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_1609_01882_amd as p
+    from paper_1609_01882_amd import binding
+    if not os.path.exists(p.lib_path()):
+        import __graft_entry__ as g
+        g.build()
+    return binding._load()
+
+
+def _size(lib, rows, most, heads=4, weights=0, window=0, **cache):
+    return lib.psc_kv_attention_workspace_bytes(C.byref(_cache(**cache)), 0, rows, most, heads, window, 0, 0, weights)
+
+
+def test_sizes_hold_whether_or_not_the_rows_have_offsets(lib):
+    """Without offsets the call takes rows / batch for max_rows, whatever the size was asked with."""
+    for width in (4, 100, 4096):
+        for rows in (3, 60, 600, 60_000):
+            need = _size(lib, rows, rows // 3, table_width=width)
+            for most in (0, 1, rows, 100 * rows):
+                assert _size(lib, rows, most, table_width=width) >= need, (width, rows, most)
