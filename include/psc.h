@@ -416,7 +416,7 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
                 psc_stream stream);
 
 /* Attention of nrows rows of q_heads heads (a multiple of kv_heads: query head h looks at kv head h / (q_heads /
- * kv_heads)); no sequence has more than max_rows rows (offsets_dev NULL: not used).
+ * kv_heads)); no sequence has more than max_rows rows (offsets_dev NULL: not used; nrows <= batch * max_rows).
  *   scores s = scale * q . k (scale > 0) over the tokens that a row sees, p = softmax(s), out = sum p v.
  * Row r of sequence b stands at position first_dev[b] + r (first_dev NULL: its rows are its last tokens); a token at
  * positions_dev (per slot, >= 0; NULL: its slot).  A row sees the tokens of its sequence

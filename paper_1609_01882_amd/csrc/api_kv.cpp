@@ -165,6 +165,7 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
                 "misaligned first, positions, weights or lse");
     if (!offsets_dev || nrows == 0) max_rows = nrows / v.batch;
     PSC_REQUIRE(nrows == 0 || max_rows >= 1, "max_rows must be at least 1");
+    PSC_REQUIRE((int64_t)max_rows * v.batch >= nrows, "%d rows are more than max_rows (%d) of each of %d sequences", nrows, max_rows, v.batch);
     if (nrows > 0) {
         PSC_TRY(check_strides("q", q_dev, dtype, q_row_stride, q_head_stride));
         PSC_TRY(check_strides("out", out_dev, dtype, 0, 0));

@@ -65,7 +65,10 @@ def _ints(**values):
 
 
 @functools.lru_cache(maxsize=1024)
-def _attention_workspace(pages, kv_heads, head_dim, page, batch, width, *sizes):
+def _attention_workspace(pages, kv_heads, head_dim, page, batch, width, dtype, rows, max_rows, q_heads, window, sinks, *has):
+    sizes = dict(rows=rows, max_rows=max_rows, q_heads=q_heads, window=window, sinks=sinks)
+    _ints(batch=batch, width=width, **sizes)
+    sizes = dtype, *sizes.values(), *has
     return _load().psc_kv_attention_workspace_bytes(_pack(0, 0, 0, 0, pages, kv_heads, head_dim, page, 0, batch, width, 0), *sizes)
 
 
@@ -139,19 +142,19 @@ class KvCache:
     def attend(self, q, table, lengths, offsets=None, max_rows=None, first=None, positions=None, scale=None, causal=True, window=0,
                sinks=0, weights=None, weights_out=None, out=None, workspace=None):
         """Attention of the rows q [n, q_heads, head_dim]: (out, lse), [n, q_heads, head_dim] and [n, q_heads].
-        The rows of a sequence are its last tokens, or stand at first[b], first[b] + 1, ...  `max_rows`: the most rows of
-        a sequence (with `offsets`; None: n).  `window` > 0: rows see that many positions back from their own, and the
+        The rows of a sequence are its last tokens, or stand at first[b], first[b] + 1, ...  `max_rows`: no sequence has
+        more rows (with `offsets`; None: n).  `window` > 0: rows see that many positions back from their own, and the
         positions below `sinks`.  `scale` None: 1 / sqrt(head_dim).  `weights_out`, per slot (float32), receives
         `weights` (None: 0) plus the weight that each token was given; they may be the same tensor."""
         c, batch, slots = self._args(table, lengths)
         n, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
         code, device = _dtype(q, "q"), self._index
-        _ints(window=window, sinks=sinks)
         rows = self._rows(q, heads, "q")
         if offsets is None:
             max_rows = n // max(batch, 1)
         elif max_rows is None:
             max_rows = n
+        _ints(max_rows=max_rows, window=window, sinks=sinks)
         if out is None:
             out = (torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device),
                    torch.empty((n, heads), dtype=torch.float32, device=self.device))
@@ -184,6 +187,7 @@ class KvCache:
                                         q_heads, window, sinks, positions, weights))
 
     def evict_workspace_bytes(self, batch: int, width: int, budget: int) -> int:
+        _ints(batch=batch, width=width, budget=budget)
         return int(_load().psc_kv_evict_workspace_bytes(_pack(0, 0, 0, 0, self.pages, self.kv_heads, self.head_dim, self.page, 0, batch, width, 0), budget))
 
     def evict(self, table, lengths, weights, budget: int, sinks: int = 0, recent: int = 0, positions=None, seen=None, out=None, workspace=None):

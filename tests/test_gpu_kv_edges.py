@@ -125,3 +125,20 @@ def test_a_workspace_sized_with_another_most_than_the_call_uses():
             size = cache.attend_workspace_bytes(3, 4096, rows, most, 4, q.dtype)
             got = cache.attend(q, table, lengths, workspace=torch.empty(size, dtype=torch.uint8, device="cuda"))
             assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+# ------------------------------------------------------------------------------------------- sizes, rows of no sequence
+def test_a_most_that_does_not_fit_is_refused():
+    import paper_1609_01882_amd as psc
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    q, offsets = torch.zeros((6, 4, 64), device="cuda"), torch.tensor([0, 1, 6], dtype=torch.int32, device="cuda")
+    for bad in ((1 << 32) + 5, 1 << 31, -1 << 40):
+        with pytest.raises(psc.PscError):
+            cache.attend(q, table, lengths, offsets=offsets, max_rows=bad)
+    with pytest.raises(psc.PscError):
+        cache.attend_workspace_bytes(2, 2, 6, (1 << 32) + 5, 4, q.dtype)
+    with pytest.raises(psc.PscError):
+        cache.attend_workspace_bytes(2, 2, 6, 5, 4, q.dtype, window=1 << 32)
+    with pytest.raises(psc.PscError):
+        cache.evict_workspace_bytes(2, 2, (1 << 32) + 5)

@@ -28,3 +28,8 @@ def test_sizes_hold_whether_or_not_the_rows_have_offsets(lib):
             need = _size(lib, rows, rows // 3, table_width=width)
             for most in (0, 1, rows, 100 * rows):
                 assert _size(lib, rows, most, table_width=width) >= need, (width, rows, most)
+
+
+def test_more_rows_than_the_sequences_may_have_are_refused(lib):
+    for bad in (dict(n=60, most=19), dict(n=60, most=1), dict(n=4, most=1)):
+        assert _attend(lib, offsets=A, **bad) == -1 and b"max_rows" in lib.psc_last_error()
