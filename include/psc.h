@@ -423,7 +423,8 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
  *   - at its own position and before it, if `causal`;
  *   - of those, if window > 0, the ones fewer than `window` positions back and the ones at positions below `sinks`.
  * out_dev [nrows][q_heads][head_dim] (dtype), lse_dev (may be NULL) [nrows][q_heads] float32: log of the sum of exp s.
- * A row that sees nothing: zeros and -infinity.  window > 0 needs causal.
+ * A row that sees nothing: zeros and -infinity.  Rows that no sequence has (outside offsets_dev, or past max_rows of
+ * theirs): NaN.  window > 0 needs causal.
  * weights_out_dev (may be NULL), per slot: weights_in_dev (NULL: 0) + the sum of p over the sequence's rows and the kv
  * head's query heads; 0 is added in slots that no row sees, rows that come out NaN add nothing.  The two may be the same.
  * Held values enter the products exactly, rows as they are; scores, sums and softmax are float32; probabilities are

@@ -259,12 +259,28 @@ __device__ __forceinline__ RowSet rows_of(const KvView &c, const KvQueries &q, i
 {
     RowSet s;
     s.first_row = q.offsets ? q.offsets[b] : b * q.each;
-    s.rows = q.offsets ? q.offsets[b + 1] - s.first_row : q.each;
-    if (s.first_row < 0 || s.first_row > q.nrows) s.rows = 0;
-    s.rows = max(0, min(min(s.rows, q.max_rows), q.nrows - s.first_row));
+    int all = q.offsets ? q.offsets[b + 1] - s.first_row : q.each;
+    if (s.first_row < 0 || s.first_row > q.nrows) all = 0;
+    all = max(0, min(all, q.nrows - s.first_row));
+    s.rows = min(all, q.max_rows);
     s.n = (int)max((int64_t)0, min((int64_t)c.lengths[b], (int64_t)c.width << c.page_shift));
-    s.first_pos = q.first ? q.first[b] : s.n - s.rows;
+    s.first_pos = q.first ? q.first[b] : s.n - all;
     return s;
+}
+
+// The output of rows from .. to - 1, NaN: no sequence has them, and what the memory held is not to pass for a result.
+template <int D, int DT>
+__device__ void rows_of_nobody(const KvQueries &q, int head, int from, int to)
+{
+    for (int64_t x = (int64_t)max(from, 0) * q.group + (threadIdx.x >> 4); x < (int64_t)min(to, q.nrows) * q.group; x += blockDim.x >> 4) {
+        const int64_t row = x / q.group * q.q_heads + head * q.group + x % q.group;
+        const int run = (int)threadIdx.x & 15;
+        float nan[D / 16];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) nan[j] = __builtin_nanf("");
+        store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + run * (D / 16), nan);
+        if (run == 0 && q.lse) q.lse[row] = nan[0];
+    }
 }
 
 // Blocks of 32 slots that some row at positions lo_pos .. hi_pos can see: those below `sink_blocks`, then
@@ -859,6 +875,10 @@ __global__ __launch_bounds__(256, (attention_waves<D, DT, RT>())) void kv_attent
     if constexpr (!kParts) {
         const int b = (int)blockIdx.z / c.heads, head = (int)blockIdx.z % c.heads, m0 = (int)blockIdx.x * 16 * RT;
         const RowSet s = rows_of(c, q, b);
+        if (q.offsets && m0 == 0) {
+            if (b == 0) rows_of_nobody<D, DT>(q, head, 0, s.first_row);
+            rows_of_nobody<D, DT>(q, head, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
+        }
         if (m0 >= s.rows * q.group) return;
         const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
         attend_unit<D, DT, RT, kPos>(c, q, s, b, head, m0, blocks, 0, blocks.count(), -1, joined);
@@ -888,7 +908,14 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, KvQueries q)
     const int r = (int)(row / q.q_heads), q_head = (int)(row % q.q_heads), b = __builtin_amdgcn_readfirstlane(sequence_of_row(q.offsets, c.batch, q.each, r));
     const RowSet s = rows_of(c, q, b);
     const int place = r - s.first_row;
-    if (place < 0 || place >= s.rows) return;
+    if (place < 0 || place >= s.rows) {  // nobody's
+        float nan[D / 16];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) nan[j] = __builtin_nanf("");
+        if (quarter == 0) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + row * D + run * (D / 16), nan);
+        if (lane == 0 && q.lse) q.lse[row] = nan[0];
+        return;
+    }
     const int m = place * q.group + q_head % q.group, in_unit = m % q.unit_rows;
     const uint32_t unit = (uint32_t)(m / q.unit_rows * c.heads + q_head / q.group);
     Parts all(c, q);

@@ -142,3 +142,33 @@ def test_a_most_that_does_not_fit_is_refused():
         cache.attend_workspace_bytes(2, 2, 6, 5, 4, q.dtype, window=1 << 32)
     with pytest.raises(psc.PscError):
         cache.evict_workspace_bytes(2, 2, (1 << 32) + 5)
+
+
+@pytest.mark.parametrize("width", [4, 200])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_no_sequence_has_come_out_nan(width, dtype):
+    """Rows outside `offsets` and those past `max_rows` are nobody's: NaN, not what the memory held before.  The others are
+    what they would be alone, at the places that they have among all rows of their sequence."""
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(width)
+    cache = psc.KvCache(*(_cuda(x) for x in U.random_cache(rng, 2 * width, 2, 32, 128)))
+    table = _cuda(rng.permutation(2 * width).reshape(2, width).astype(np.int32))
+    lengths = torch.tensor([32 * width - 1, 100], dtype=torch.int32, device="cuda")
+    q = torch.randn((50, 6, 128), device="cuda").to(U.TYPES[dtype])
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for offsets, most, first, there in (((1, 4, 48), 44, None, range(1, 48)), ((0, 20, 50), 25, None, range(45)), ((0, 3, 50), 25, (7, 20), range(28)),
+                                        ((0, 0, 50), 49, None, range(49)), ((50, 50, 50), 25, None, range(0)), ((0, 0, 0), 30, (0, 0), range(0))):
+        out = torch.full((50, 6, 128), 7.0, device="cuda", dtype=q.dtype), torch.full((50, 6), 7.0, device="cuda")
+        cache.attend(q, table, lengths, offsets=ints(*offsets), max_rows=most, first=None if first is None else ints(*first), out=out)
+        mine = torch.zeros(50, dtype=torch.bool, device="cuda")
+        mine[list(there)] = True
+        assert bool(out[0][~mine].isnan().all()) and bool(out[1][~mine].isnan().all()), (offsets, most)
+        for b in range(2):
+            lo, hi = offsets[b], offsets[b + 1]
+            if lo < hi:
+                at = ints(int(lengths[b]) - (hi - lo) if first is None else first[b])
+                want = cache.attend(q[lo:hi], table[b:b + 1], lengths[b:b + 1], first=at)
+                n = min(hi - lo, most)
+                # (parts of another number are joined in another order: a rounding or two)
+                for x, y in zip((o[lo:lo + n] for o in out), want):
+                    assert torch.allclose(x.float(), y[:n].float(), rtol=2.0 ** -7 if dtype == "bf16" else 2.0 ** -15, atol=2.0 ** -8 if dtype == "bf16" else 2.0 ** -16)
