@@ -400,6 +400,7 @@ typedef struct psc_kv_cache {
 
 /* Rows of several sequences lie one after another: sequence b has the rows offsets_dev[b] .. offsets_dev[b + 1] - 1
  * (int32 [batch + 1], ascending, from 0 to nrows), or, offsets_dev NULL, nrows / batch each (nrows a multiple of batch).
+ * Rows before offsets_dev[0] or from offsets_dev[batch] on are nobody's: not written, read as zeros.
  * Coordinates of a head are contiguous; the strides, in elements, lead from row to row and from head to head (a
  * product's output that holds queries, keys and values side by side is taken as it is).  Rows and heads start at
  * multiples of 16 bytes.  dtype: PSC_BF16, PSC_F16 or PSC_F32.

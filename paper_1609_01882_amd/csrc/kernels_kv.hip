@@ -166,7 +166,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRows r)
     const int b = sequence_of_row(r.offsets, c.batch, r.each, row);
     const int place = row - (r.offsets ? r.offsets[b] : b * r.each);
     const int64_t slot = (int64_t)c.lengths[b] + place;
-    const int page = place < 0 ? -1 : page_of(c, b, slot);
+    const bool nobodys = place < 0 || (r.offsets && row >= r.offsets[c.batch]);
+    const int page = nobodys ? -1 : page_of(c, b, slot);
     typedef typename Element<DT>::type T;
     float x[2][8];
     load_row<DT, 8>((const T *)r.k + row * r.k_stride + head * r.k_head_stride + part * 8, x[0]);
@@ -225,7 +226,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, KvRows r, void *
     const int b = sequence_of_row(r.offsets, c.batch, r.each, row);
     const int place = row - (r.offsets ? r.offsets[b] : b * r.each);
     const int64_t slot = (int64_t)c.lengths[b] + place;
-    const int page = place < 0 ? -1 : page_of(c, b, slot);
+    const bool nobodys = place < 0 || (r.offsets && row >= r.offsets[c.batch]);
+    const int page = nobodys ? -1 : page_of(c, b, slot);
     typedef typename Element<DT>::type T;
     const int64_t at = page < 0 ? 0 : ((int64_t)page * c.heads + head) << c.page_shift | (slot & ((1 << c.page_shift) - 1));
 #pragma unroll

@@ -172,3 +172,26 @@ def test_rows_that_no_sequence_has_come_out_nan(width, dtype):
                 # (parts of another number are joined in another order: a rounding or two)
                 for x, y in zip((o[lo:lo + n] for o in out), want):
                     assert torch.allclose(x.float(), y[:n].float(), rtol=2.0 ** -7 if dtype == "bf16" else 2.0 ** -15, atol=2.0 ** -8 if dtype == "bf16" else 2.0 ** -16)
+
+
+def test_rows_that_no_sequence_has_are_not_written():
+    import paper_1609_01882_amd as psc
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32, device="cuda"), torch.tensor([3, 15], dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([1, 3, 5], dtype=torch.int32, device="cuda")
+    w = torch.full((2, 2, 32), 3.0, device="cuda")
+    x = torch.ones((9, 2, 64), device="cuda")
+    cache.append(x, x, table, lengths, offsets=offsets, weights=w)
+    want = torch.full((2, 32), 3.0, device="cuda")
+    want[0, 3:5] = want[1, 15:17] = 0.0
+    assert torch.equal(w, want[:, None].expand(2, 2, 32))
+    k, _ = cache.read(table, torch.zeros_like(lengths), 64)
+    assert torch.equal(k[:, 0, 0], (want == 0).float().flatten())
+    k, v = cache.read(table, lengths, 9, offsets=offsets)
+    there = torch.tensor([0, 1, 1, 1, 1, 0, 0, 0, 0], dtype=torch.float32, device="cuda")
+    assert torch.equal(k, there.view(9, 1, 1).expand_as(k)) and torch.equal(v, k)
+    cache.append(x, x, table, torch.tensor([20, 20], dtype=torch.int32, device="cuda"), offsets=offsets)
+    k, v = cache.read(table, torch.full_like(lengths, 20), 9, offsets=offsets)      # 20, 21 of both; the rest were never written
+    assert torch.equal(k, there.view(9, 1, 1).expand_as(k))
+    k, _ = cache.read(table, torch.zeros_like(lengths), 64)
+    assert int(k[:, 0, 0].sum()) == 8
