@@ -145,7 +145,8 @@ class KvCache:
         The rows of a sequence are its last tokens, or stand at first[b], first[b] + 1, ...  `max_rows`: no sequence has
         more rows (with `offsets`; None: n).  `window` > 0: rows see that many positions back from their own, and the
         positions below `sinks`.  `scale` None: 1 / sqrt(head_dim).  `weights_out`, per slot (float32), receives
-        `weights` (None: 0) plus the weight that each token was given; they may be the same tensor."""
+        `weights` (None: 0) plus the weight that each token was given; they may be the same tensor.  Nothing flows back:
+        a `q` that wants a gradient is refused."""
         c, batch, slots = self._args(table, lengths)
         n, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
         code, device = _dtype(q, "q"), self._index
@@ -155,6 +156,8 @@ class KvCache:
         elif max_rows is None:
             max_rows = n
         _ints(max_rows=max_rows, window=window, sinks=sinks)
+        if q.requires_grad and torch.is_grad_enabled():
+            raise PscError("q: attention over a memory in 4 bits has no gradient; detach q, or call under torch.no_grad()")
         if out is None:
             out = (torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device),
                    torch.empty((n, heads), dtype=torch.float32, device=self.device))

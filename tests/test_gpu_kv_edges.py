@@ -195,3 +195,17 @@ def test_rows_that_no_sequence_has_are_not_written():
     assert torch.equal(k, there.view(9, 1, 1).expand_as(k))
     k, _ = cache.read(table, torch.zeros_like(lengths), 64)
     assert int(k[:, 0, 0].sum()) == 8
+
+
+# ------------------------------------------------------------------------------------------- gradients
+def test_queries_that_want_a_gradient_are_refused():
+    """Attention over codes has no backward pass: silence would train on a gradient of nothing."""
+    import paper_1609_01882_amd as psc
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    q = torch.zeros((2, 4, 64), device="cuda", requires_grad=True)
+    with pytest.raises(psc.PscError, match="gradient"):
+        cache.attend(q, table, lengths)
+    with torch.no_grad():
+        cache.attend(q, table, lengths)
+    cache.attend(q.detach(), table, lengths)
