@@ -385,7 +385,8 @@ int psc_imi_search(const psc_index *idx, const float *q_dev, int64_t nq, int max
  *             read as zeros and are seen by no row.  No page may stand twice among those written by one call.
  *   lengths_dev [batch] (int32): tokens of each sequence; what exceeds table_width * page does not exist.
  * Arrays "per slot" are dense: [batch][kv_heads][table_width * page], 16-byte aligned.
- * batch * kv_heads <= 65535, table_width * page < 2^30, pages * kv_heads * page < 2^35. */
+ * batch * kv_heads <= 65535, table_width * page < 2^30, pages * kv_heads * page < 2^35; a call writes or reads fewer than
+ * 2^35 - 2^11 coordinates of keys (append, read), or keeps as many of 2^37 - 2^13 (evict). */
 #define PSC_BF16 0
 #define PSC_F16 1
 #define PSC_F32 2

@@ -9,6 +9,7 @@ namespace psc {
 namespace {
 
 constexpr int64_t kMostSlots = (int64_t)1 << 30, kMostGroups = 65535;
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 24) - 1;  // of 256 lanes: a dimension of a grid has under 2^32 lanes
 
 bool aligned(const void *p, uintptr_t to = 16) { return (uintptr_t)p % to == 0; }
 
@@ -111,7 +112,7 @@ int psc_kv_append(const psc_kv_cache *cache, int dtype, const void *k_dev, int64
     PSC_TRY(check_strides("k", k_dev, dtype, k_row_stride, k_head_stride));
     PSC_TRY(check_strides("v", v_dev, dtype, v_row_stride, v_head_stride));
     PSC_REQUIRE(aligned(first_dev, 4) && aligned(positions_dev) && aligned(weights_dev), "misaligned first, positions or weights");
-    PSC_REQUIRE((int64_t)nrows * v.heads * (v.dim / 8) < (int64_t)1 << 38, "%d rows are too many", nrows);
+    PSC_REQUIRE((int64_t)nrows * v.heads * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows, v.heads, v.dim);
     const KvRows r{k_dev, v_dev, k_row_stride, k_head_stride, v_row_stride, v_head_stride, nrows, nrows / v.batch, offsets_dev, first_dev,
                    positions_dev, weights_dev};
     return launch_kv_append(v, dtype, r, (hipStream_t)stream);
@@ -127,7 +128,7 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
     if (nrows == 0) return PSC_OK;
     PSC_TRY(check_strides("k", k_dev, dtype, 0, 0));
     PSC_TRY(check_strides("v", v_dev, dtype, 0, 0));
-    PSC_REQUIRE((int64_t)nrows * v.heads * (v.dim / 8) < (int64_t)1 << 38, "%d rows are too many", nrows);
+    PSC_REQUIRE((int64_t)nrows * v.heads * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows, v.heads, v.dim);
     KvRows r{};
     r.nrows = nrows;
     r.each = nrows / v.batch;
@@ -174,7 +175,8 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
     }
     const int group = q_heads / v.heads;
     const KvPlan p = plan_kv_attention(v, dtype, group, nrows, max_rows, window, sinks, !positions_dev, weights_out_dev != nullptr);
-    PSC_REQUIRE(p.row_groups * v.heads < kMostSlots, "%d rows of a sequence are too many", max_rows);
+    PSC_REQUIRE(p.row_groups <= kMostWorkgroups, "%d rows of a sequence are too many for a launch", max_rows);
+    PSC_REQUIRE(p.weights_groups <= kMostWorkgroups, "%lld slots are too many for the weights of %d rows", (long long)v.width << v.page_shift, max_rows);
     PSC_REQUIRE(workspace_bytes >= p.bytes() && (p.bytes() == 0 || workspace_dev), "workspace too small: %zu bytes, %zu needed", workspace_bytes, p.bytes());
     PSC_REQUIRE(aligned(workspace_dev), "workspace must be 16-byte aligned");
     KvQueries q{};
@@ -234,7 +236,8 @@ int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int3
                 "misaligned array");
     const KvEvictPlan p = plan_kv_evict(v, budget);
     const size_t need = p.bytes();
-    PSC_REQUIRE((int64_t)v.batch * v.heads * budget * (v.dim / 32) < (int64_t)1 << 38, "budget %d is too large for %d x %d memories", budget, v.batch, v.heads);
+    PSC_REQUIRE((int64_t)v.batch * v.heads * budget * (v.dim / 32) <= kMostWorkgroups * 256, "budget %d of %d x %d memories is too large for a launch", budget,
+                v.batch, v.heads);
     PSC_REQUIRE(workspace_dev && workspace_bytes >= need && aligned(workspace_dev), "workspace too small or misaligned: %zu bytes, %zu needed", workspace_bytes, need);
     KvEvict e{};
     e.weights = weights_dev;

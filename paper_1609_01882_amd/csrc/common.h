@@ -360,7 +360,9 @@ struct KvPlan {
     int64_t workgroups = 0;  // units are cut into parts, about so many together; 0: a workgroup has a unit
     int64_t most_parts = 0;
     int least_blocks = 0;    // of a part
-    int scores_rows = 0;        // the scores of so many rows are kept for the weights (0: they are computed again)
+    int scores_rows = 0;     // the scores of so many rows are kept for the weights (0: they are computed again)
+    bool split_rows = false;     // and then a workgroup's waves take rows each, not tokens
+    int64_t weights_groups = 0;  // workgroups of the weights to a (sequence, kv head)
     size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0, scores_bytes = 0;
     size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes + scores_bytes; }
 };

@@ -1584,6 +1584,9 @@ constexpr int most_row_tiles()
     return DT == PSC_F32 || D == 256 ? 1 : 2;
 }
 
+// Sixteens of tokens of a workgroup that shares out rows for the weights: as many as leave room for two waves' registers.
+constexpr int split_tiles(int dim) { return dim == 256 ? 2 : 4; }
+
 template <int DT, int D>
 int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const float *given, float *received, hipStream_t s)
 {
@@ -1607,19 +1610,15 @@ int run_attention(const KvView &c, const KvQueries &q, const KvPlan &p, const fl
         }
     }
     if (received) {
-        const int64_t slots = (int64_t)c.width << c.page_shift;
-        const uint32_t groups = (uint32_t)(c.batch * c.heads);
+        const dim3 grid((uint32_t)p.weights_groups, 1, (uint32_t)(c.batch * c.heads));
         if (p.scores_rows > 0) {
-            const dim3 grid((uint32_t)((slots + 1023) / 1024), 1, groups);
             if (p.scores_rows == 1) kv_weights_of_scores_kernel<1><<<grid, 256, 0, s>>>(c, q, given, received);
             else if (p.scores_rows <= 4) kv_weights_of_scores_kernel<4><<<grid, 256, 0, s>>>(c, q, given, received);
             else kv_weights_of_scores_kernel<kScoreRows><<<grid, 256, 0, s>>>(c, q, given, received);
-        } else if (q.max_rows * (int64_t)q.group > 64) {
-            constexpr int kTiles = D == 256 ? 2 : 4;  // sixteens of tokens: as many as leave room for two waves' registers
-            const int64_t tokens = 16 * kTiles;
-            kv_weights_kernel<D, DT, true, kTiles><<<dim3((uint32_t)((slots + tokens - 1) / tokens), 1, groups), 256, 0, s>>>(c, q, given, received);
+        } else if (p.split_rows) {
+            kv_weights_kernel<D, DT, true, split_tiles(D)><<<grid, 256, 0, s>>>(c, q, given, received);
         } else {
-            kv_weights_kernel<D, DT, false, 2><<<dim3((uint32_t)((slots + 127) / 128), 1, groups), 256, 0, s>>>(c, q, given, received);
+            kv_weights_kernel<D, DT, false, 2><<<grid, 256, 0, s>>>(c, q, given, received);
         }
         PSC_HIP_TRY(hipGetLastError());
     }
@@ -1652,11 +1651,11 @@ int launch_kv_read(const KvView &c, int dtype, const KvRows &r, void *k_out, voi
 KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered, bool weights)
 {
     KvPlan p;
-    const int64_t m = (int64_t)max_rows * group, rows = nrows * group * c.heads;
+    const int64_t m = (int64_t)max_rows * group, rows = nrows * group * c.heads, slots = (int64_t)c.width << c.page_shift;
     p.row_tiles = m <= 16 || dtype == PSC_F32 || c.dim == 256 ? 1 : 2;
     p.row_groups = (m + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
     // blocks of 32 tokens that a group of rows can see at most
-    int64_t blocks = (((int64_t)c.width << c.page_shift) + 31) / 32;
+    int64_t blocks = (slots + 31) / 32;
     if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
     const int64_t units = p.row_groups * c.batch * c.heads;
     // workgroups that run at a time (attention_waves of them to a compute unit)
@@ -1671,10 +1670,13 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
         p.part_acc_bytes = (size_t)(p.most_parts * 16 * p.row_tiles * c.dim * 4 + 255) / 256 * 256;
     }
     p.least_blocks = kLeastBlocks;
+    p.split_rows = m > 64;
+    const int64_t tokens = weights && nrows > 0 && m <= kScoreRows ? 1024 : p.split_rows ? 16 * split_tiles(c.dim) : 128;
+    p.weights_groups = weights ? (slots + tokens - 1) / tokens : 0;
     p.stat_bytes = weights ? (size_t)(rows * 8 + 255) / 256 * 256 : 0;
     if (weights && nrows > 0 && m <= kScoreRows) {
         p.scores_rows = (int)m;
-        p.scores_bytes = (size_t)((int64_t)c.batch * c.heads * m * ((int64_t)c.width << c.page_shift) * 4 + 255) / 256 * 256;
+        p.scores_bytes = (size_t)((int64_t)c.batch * c.heads * m * slots * 4 + 255) / 256 * 256;
     }
     return p;
 }

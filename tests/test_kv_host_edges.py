@@ -33,3 +33,28 @@ def test_sizes_hold_whether_or_not_the_rows_have_offsets(lib):
 def test_more_rows_than_the_sequences_may_have_are_refused(lib):
     for bad in (dict(n=60, most=19), dict(n=60, most=1), dict(n=4, most=1)):
         assert _attend(lib, offsets=A, **bad) == -1 and b"max_rows" in lib.psc_last_error()
+
+
+LANES = 1 << 32    # a dimension of a grid has fewer
+
+
+def test_more_rows_than_a_grid_has_lanes_for_are_refused(lib):
+    for dim, heads in ((128, 2), (256, 1), (64, 48)):
+        kw = dict(head_dim=dim, kv_heads=heads)
+        n = -(-LANES // (heads * dim // 8 * 3)) * 3                  # (a multiple of the three sequences)
+        assert _append(lib, _cache(**kw), n=n) == -1 and b"rows" in lib.psc_last_error()
+        assert lib.psc_kv_read(C.byref(_cache(**kw)), 0, n, None, A, A, None) == -1 and b"rows" in lib.psc_last_error()
+
+
+def test_a_budget_that_a_grid_has_no_lanes_for_is_refused(lib):
+    budget = -(-LANES // (3 * 2 * 4))
+    assert _evict(lib, budget=budget, stride=budget, size=1 << 60) == -1 and b"budget" in lib.psc_last_error()
+
+
+def test_attention_that_a_grid_has_no_lanes_for_is_refused(lib):
+    one = dict(batch=1, kv_heads=1)
+    n = (1 << 30) - 32                                               # units of 32 rows, a workgroup of 256 to each
+    assert _attend(lib, _cache(**one), n=n, most=n, heads=1, size=1 << 60) == -1 and b"rows" in lib.psc_last_error()
+    # weights of many rows: a workgroup to 32 slots of 256 coordinates
+    wide = _cache(**one, head_dim=256, page=256, table_width=1 << 21)
+    assert _attend(lib, wide, n=100, most=100, heads=1, w_out=A, size=1 << 60) == -1 and b"weights" in lib.psc_last_error()
