@@ -445,7 +445,8 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
 
 /* Cuts every (sequence, kv head) with more than `budget` tokens down to the budget.  Kept are the tokens at positions
  * below `sinks` and at seen_dev[b] - recent and later (seen_dev NULL: lengths_dev; sinks + recent <= budget), then
- * those of the largest weights_dev (per slot; NaN counts as the smallest); the lower slot on equal weight.  The slots
+ * those of the largest weights_dev (per slot; NaN counts as the smallest); the lower slot on equal weight.  Slots without
+ * a page hold no token: those below the budget stay as they are and count, those behind it are not kept.  The slots
  * below the budget that fall free take, in ascending order, the kept tokens of the slots behind it, in ascending order;
  * nothing else moves, and slots behind the budget stay as they are until they are written again.
  *   kept_dev [batch][kv_heads][budget] (int32): the slot that the token now in this slot had; -1 past the length

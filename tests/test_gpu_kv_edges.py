@@ -209,3 +209,74 @@ def test_queries_that_want_a_gradient_are_refused():
     with torch.no_grad():
         cache.attend(q, table, lengths)
     cache.attend(q.detach(), table, lengths)
+
+
+# ------------------------------------------------------------------------------------------- eviction
+def _evict_reference(lengths, weights, positions, seen, budget, sinks, recent, paged):
+    """kept as in kv_util.evict, where paged [batch][slots] says which slots have a page."""
+    batch, heads = weights.shape[:2]
+    kept = np.full((batch, heads, budget), -1, np.int32)
+    for b in range(batch):
+        n = min(max(int(lengths[b]), 0), weights.shape[2])
+        for h in range(heads):
+            w, there = weights[b, h, :n].astype(np.float64), paged[b, :n]
+            pos = np.arange(n) if positions is None else positions[b, h, :n].astype(np.int64)
+            stays = (pos < sinks) | (pos >= (n if seen is None else int(seen[b])) - recent) | (~there & (np.arange(n) < budget))
+            stays &= there | (np.arange(n) < budget)
+
+            def order(s):
+                if stays[s]:
+                    return (0, 0.0, s)
+                if not there[s]:
+                    return (3, 0.0, s)
+                return (2, 0.0, s) if np.isnan(w[s]) else (1, -w[s], s)
+            keep = np.zeros(n, bool)
+            keep[sorted(range(n), key=order)[:budget]] = True
+            source = np.arange(min(n, budget), dtype=np.int32)
+            source[~keep[:budget]] = np.flatnonzero(keep[budget:]) + budget
+            kept[b, h, :len(source)] = source
+    return kept
+
+
+@pytest.mark.parametrize("page,width,budget", [(16, 20, 100), (16, 200, 700), (64, 8, 200), (256, 3, 300), (16, 1300, 5000), (32, 700, 17_000), (128, 200, 9000)])
+@pytest.mark.parametrize("kind", ["spread", "ties", "nan"])
+@pytest.mark.parametrize("reordered", [False, True])
+def test_slots_without_a_page_neither_keep_a_token_nor_take_one(page, width, budget, kind, reordered):
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(page + width)
+    batch, heads, dim, slots = 3, 2, 64, width * page
+    lengths = np.array([slots, slots - page // 2 - 1, min(slots, budget + 5)], np.int32)
+    pages = batch * width + 1
+    table = rng.permutation(pages)[:batch * width].reshape(batch, width).astype(np.int32)
+    lost = rng.random((batch, width)) < 0.2
+    lost[0, 0] = lost[1, (budget - 1) // page] = True
+    lost[2, : (budget - 1) // page] = False
+    table[lost] = rng.choice([-1, pages, 1 << 30, -9], int(lost.sum()))
+    paged = np.repeat(~lost, page, 1)
+    w = np.exp(rng.normal(size=(batch, heads, slots))).astype(np.float32)
+    if kind == "ties":
+        w = rng.integers(0, 2, w.shape).astype(np.float32)
+    elif kind == "nan":
+        w[rng.random(w.shape) < 0.9] = np.nan
+    positions = seen = None
+    if reordered:
+        positions = np.stack([np.stack([rng.permutation(2 * slots)[:slots] for _ in range(heads)]) for _ in range(batch)]).astype(np.int32)
+        seen = np.full(batch, 2 * slots, np.int32)
+    want = _evict_reference(lengths, w, positions, seen, budget, 4, budget // 3, paged)
+    buffers = U.random_cache(rng, pages, heads, page, dim)
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    print(f"evict without pages: page={page} slots={slots} budget={budget} {kind}", flush=True)
+    kept, out_len, pos, out_w = (t.cpu().numpy() for t in cache.evict(_cuda(table), _cuda(lengths), _cuda(w), budget, sinks=4, recent=budget // 3,
+                                                                     positions=_cuda(positions), seen=_cuda(seen)))
+    assert np.array_equal(kept, want) and np.array_equal(out_len, np.minimum(lengths, budget))
+    b, h = np.arange(batch)[:, None, None], np.arange(heads)[None, :, None]
+    assert np.array_equal(out_w, np.where(want < 0, np.float32(0), w[b, h, want]), equal_nan=True)
+    assert np.array_equal(pos, np.where(want < 0, -1, want if positions is None else positions[b, h, want]))
+    ref = [x.copy() for x in buffers]
+    for bi, hi, to in np.argwhere((want >= 0) & (want != np.arange(budget))):
+        src = want[bi, hi, to]
+        assert paged[bi, src] and paged[bi, to]
+        for x, y in zip(ref, buffers):
+            x[table[bi, to // page], hi, to % page] = y[table[bi, src // page], hi, src % page]
+    for x, t in zip(ref, (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)):
+        assert np.array_equal(x, t.cpu().numpy())
