@@ -67,9 +67,12 @@ int check_rows(const KvView &v, int nrows, const int32_t *offsets)
     return PSC_OK;
 }
 
-int check_strides(const char *what, const void *p, int dtype, int64_t row, int64_t head)
+// (A stride that leads to no second row or head may be anything.)
+int check_strides(const char *what, const void *p, int dtype, int nrows, int64_t row, int heads, int64_t head)
 {
     const int64_t unit = dtype == PSC_F32 ? 4 : 8;  // elements in 16 bytes
+    row = nrows > 1 ? row : 0;
+    head = heads > 1 ? head : 0;
     PSC_REQUIRE(p != nullptr, "null %s", what);
     PSC_REQUIRE(aligned(p) && row % unit == 0 && head % unit == 0, "%s: rows and heads must start at multiples of 16 bytes", what);
     PSC_REQUIRE(std::llabs(row) < (1ll << 40) && std::llabs(head) < (1ll << 40), "%s: stride too large", what);
@@ -109,8 +112,8 @@ int psc_kv_append(const psc_kv_cache *cache, int dtype, const void *k_dev, int64
     PSC_TRY(check_dtype(dtype));
     PSC_TRY(check_rows(v, nrows, offsets_dev));
     if (nrows == 0) return PSC_OK;
-    PSC_TRY(check_strides("k", k_dev, dtype, k_row_stride, k_head_stride));
-    PSC_TRY(check_strides("v", v_dev, dtype, v_row_stride, v_head_stride));
+    PSC_TRY(check_strides("k", k_dev, dtype, nrows, k_row_stride, v.heads, k_head_stride));
+    PSC_TRY(check_strides("v", v_dev, dtype, nrows, v_row_stride, v.heads, v_head_stride));
     PSC_REQUIRE(aligned(first_dev, 4) && aligned(positions_dev) && aligned(weights_dev), "misaligned first, positions or weights");
     PSC_REQUIRE((int64_t)nrows * v.heads * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows, v.heads, v.dim);
     const KvRows r{k_dev, v_dev, k_row_stride, k_head_stride, v_row_stride, v_head_stride, nrows, nrows / v.batch, offsets_dev, first_dev,
@@ -126,8 +129,8 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
     PSC_TRY(check_dtype(dtype));
     PSC_TRY(check_rows(v, nrows, offsets_dev));
     if (nrows == 0) return PSC_OK;
-    PSC_TRY(check_strides("k", k_dev, dtype, 0, 0));
-    PSC_TRY(check_strides("v", v_dev, dtype, 0, 0));
+    PSC_TRY(check_strides("k", k_dev, dtype, 0, 0, 0, 0));
+    PSC_TRY(check_strides("v", v_dev, dtype, 0, 0, 0, 0));
     PSC_REQUIRE((int64_t)nrows * v.heads * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows, v.heads, v.dim);
     KvRows r{};
     r.nrows = nrows;
@@ -168,8 +171,8 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
     PSC_REQUIRE(nrows == 0 || max_rows >= 1, "max_rows must be at least 1");
     PSC_REQUIRE((int64_t)max_rows * v.batch >= nrows, "%d rows are more than max_rows (%d) of each of %d sequences", nrows, max_rows, v.batch);
     if (nrows > 0) {
-        PSC_TRY(check_strides("q", q_dev, dtype, q_row_stride, q_head_stride));
-        PSC_TRY(check_strides("out", out_dev, dtype, 0, 0));
+        PSC_TRY(check_strides("q", q_dev, dtype, nrows, q_row_stride, q_heads, q_head_stride));
+        PSC_TRY(check_strides("out", out_dev, dtype, 0, 0, 0, 0));
     } else if (!weights_out_dev) {
         return PSC_OK;
     }

@@ -280,3 +280,29 @@ def test_slots_without_a_page_neither_keep_a_token_nor_take_one(page, width, bud
             x[table[bi, to // page], hi, to % page] = y[table[bi, src // page], hi, src % page]
     for x, t in zip(ref, (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)):
         assert np.array_equal(x, t.cpu().numpy())
+
+
+# ------------------------------------------------------------------------------------------- strides
+def test_strides_of_one_row_and_of_one_head_are_never_used():
+    """A single row out of a buffer of odd pitch begins where it has to; what leads to a next one does not matter."""
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(5)
+    for dtype in (torch.bfloat16, torch.float32):
+        cache = psc.KvCache.empty(2, 1, 64, 16)
+        table, lengths = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        x = torch.from_numpy(rng.normal(size=(5, 64))).cuda().to(dtype)
+        k = x[:1].clone().as_strided((1, 1, 64), (3, 5, 1))
+        v = x[1:2].clone().as_strided((1, 1, 64), (67, 1, 1))
+        cache.append(k, v, table, lengths)
+        rows = torch.zeros((3, 2 * 64), device="cuda", dtype=dtype)
+        rows[:, :64] = x[2:]
+        lengths += 1
+        cache.append(rows.as_strided((3, 1, 64), (128, 7, 1)), rows.as_strided((3, 1, 64), (128, 1, 1)), table, lengths)
+        lengths += 3
+        other = psc.KvCache.empty(2, 1, 64, 16)
+        other.append(torch.cat([x[:1], x[2:]])[:, None], torch.cat([x[1:2], x[2:]])[:, None], table, torch.zeros_like(lengths))
+        for a, b in zip((cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales), (other.k_codes, other.k_scales, other.v_codes, other.v_scales)):
+            assert torch.equal(a, b)
+        want = cache.attend(x[:1, None], table, lengths)
+        got = cache.attend(x[:1].clone().as_strided((1, 1, 64), (9, 11, 1)), table, lengths)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
