@@ -434,7 +434,8 @@ int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *
  * row's largest, whichever is more; not for the weights.  Results do not depend on timing: nothing is
  * added atomically.  Where slots are positions (positions_dev NULL), tokens that a window hides are not read.
  * Workspace: psc_kv_attention_workspace_bytes for the same sizes, enough with offsets_dev and without (may be 0:
- * workspace_dev may then be NULL). */
+ * workspace_dev may then be NULL).  With weights of up to 8 rows of a kv head it holds their scores, 4 bytes for a row and slot
+ * of each kv head, where these are no more than 4 GiB. */
 size_t psc_kv_attention_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
                                         int window, int sinks, int has_positions, int has_weights);
 int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,

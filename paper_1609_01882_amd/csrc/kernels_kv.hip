@@ -967,8 +967,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, KvQueries q)
 
 // The weight that every token received, from the scores that the attention left: a thread to four slots.  For up to
 // kScoreRows rows (query heads times rows of a sequence): the scores' 4 bytes to a row, written and read, are then less than
-// the keys' bytes and what comes with expanding them (32 x 4k tokens, 4 rows: 31 us with the keys once more).
+// the keys' bytes and what comes with expanding them (32 x 4k tokens, 4 rows: 31 us with the keys once more).  They are kept up to a
+// size that a caller can spare (whole calls of 8 rows x 128, kept and not: 8 x 8 x 131k tokens, 0.27 GB of scores, 269 and 355 us;
+// 16 x 8 x 262k, 1.1 GB, 1118 and 1426).
 constexpr int kScoreRows = 8;
+constexpr int64_t kMostScoreBytes = (int64_t)4 << 30;
 template <int N>
 __global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQueries q, const float *given, float *received)
 {
@@ -1686,13 +1689,15 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
         p.part_acc_bytes = (size_t)(p.most_parts * 16 * p.row_tiles * c.dim * 4 + 255) / 256 * 256;
     }
     p.least_blocks = kLeastBlocks;
+    const int64_t scores_bytes = (int64_t)c.batch * c.heads * m * slots * 4;
+    const bool keep_scores = weights && nrows > 0 && m <= kScoreRows && scores_bytes <= kMostScoreBytes;
     p.split_rows = m > 64;
-    const int64_t tokens = weights && nrows > 0 && m <= kScoreRows ? 1024 : p.split_rows ? 16 * split_tiles(c.dim) : 128;
+    const int64_t tokens = keep_scores ? 1024 : p.split_rows ? 16 * split_tiles(c.dim) : 128;
     p.weights_groups = weights ? (slots + tokens - 1) / tokens : 0;
     p.stat_bytes = weights ? (size_t)(rows * 8 + 255) / 256 * 256 : 0;
-    if (weights && nrows > 0 && m <= kScoreRows) {
+    if (keep_scores) {
         p.scores_rows = (int)m;
-        p.scores_bytes = (size_t)((int64_t)c.batch * c.heads * m * slots * 4 + 255) / 256 * 256;
+        p.scores_bytes = (size_t)(scores_bytes + 255) / 256 * 256;
     }
     return p;
 }

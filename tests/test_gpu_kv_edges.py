@@ -306,3 +306,22 @@ def test_strides_of_one_row_and_of_one_head_are_never_used():
         want = cache.attend(x[:1, None], table, lengths)
         got = cache.attend(x[:1].clone().as_strided((1, 1, 64), (9, 11, 1)), table, lengths)
         assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+# ------------------------------------------------------------------------------------------- what a call keeps
+@pytest.mark.parametrize("rows,group", [(1, 8), (2, 4)])
+def test_weights_of_memories_whose_tables_are_very_wide(rows, group):
+    """Too many slots to keep every score of: the weights come from the keys once more, and are the same."""
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(rows)
+    batch, heads, page, dim, width = 4, 32, 256, 64, 4352
+    cache = psc.KvCache(*(_cuda(x) for x in U.random_cache(rng, 3 * batch, heads, page, dim)))
+    table = torch.full((batch, width), -1, dtype=torch.int32, device="cuda")
+    table[:, :3] = _cuda(rng.permutation(3 * batch).reshape(batch, 3).astype(np.int32))
+    lengths = torch.tensor([700, 3, 512, 768], dtype=torch.int32, device="cuda")
+    q = torch.randn((batch * rows, heads * group, dim), device="cuda").bfloat16()
+    narrow, wide = torch.empty((batch, heads, 3 * page), device="cuda"), torch.full((batch, heads, width * page), np.nan, device="cuda")
+    a = cache.attend(q, table[:, :3].contiguous(), lengths, weights_out=narrow)
+    b = cache.attend(q, table, lengths, weights_out=wide)
+    assert torch.allclose(a[0].float(), b[0].float(), rtol=2.0 ** -7, atol=2.0 ** -8) and torch.allclose(a[1], b[1], rtol=2.0 ** -18, atol=2.0 ** -18)
+    assert torch.allclose(narrow, wide[..., :3 * page], rtol=2.0 ** -17, atol=2.0 ** -60) and bool((wide[..., 3 * page:] == 0).all())

@@ -58,3 +58,10 @@ def test_attention_that_a_grid_has_no_lanes_for_is_refused(lib):
     # weights of many rows: a workgroup to 32 slots of 256 coordinates
     wide = _cache(**one, head_dim=256, page=256, table_width=1 << 21)
     assert _attend(lib, wide, n=100, most=100, heads=1, w_out=A, size=1 << 60) == -1 and b"weights" in lib.psc_last_error()
+
+
+def test_kept_scores_are_bounded(lib):
+    """Eight rows of 64 x 8 memories of a million slots: their scores would take 17 GB."""
+    small = _size(lib, 64, 1, heads=64, weights=1, batch=64, kv_heads=8, page=64, table_width=64)
+    assert small >= 64 * 8 * 8 * 4096 * 4
+    assert _size(lib, 64, 1, heads=64, weights=1, batch=64, kv_heads=8, page=64, table_width=16_384) < 9 << 29
