@@ -25,6 +25,10 @@ PSC_BF16, PSC_F16, PSC_F32 = 0, 1, 2
 _DTYPES = {torch.bfloat16: PSC_BF16, torch.float16: PSC_F16, torch.float32: PSC_F32}
 
 
+# The address of a device's current stream: 0.1 us where torch has a function that gives it alone, 1.1 through a stream object.
+_stream_address = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _Cache(C.Structure):
     _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
                 ("pages", C.c_int64), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("page", C.c_int), ("table", C.c_void_p),
@@ -111,9 +115,9 @@ class KvCache:
         return t.data_ptr(), t.stride(0), t.stride(1)
 
     def _stream(self):
-        if torch._C._cuda_getDevice() != self._index:
+        if torch.cuda.current_device() != self._index:
             raise PscError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
-        return torch._C._cuda_getCurrentRawStream(self._index)
+        return _stream_address(self._index)
 
     def append(self, k, v, table, lengths, offsets=None, first=None, positions=None, weights=None):
         """Round the rows k, v [n, kv_heads, head_dim] to 4 bits and write them to slots lengths[b], lengths[b] + 1, ...

@@ -325,3 +325,27 @@ def test_weights_of_memories_whose_tables_are_very_wide(rows, group):
     b = cache.attend(q, table, lengths, weights_out=wide)
     assert torch.allclose(a[0].float(), b[0].float(), rtol=2.0 ** -7, atol=2.0 ** -8) and torch.allclose(a[1], b[1], rtol=2.0 ** -18, atol=2.0 ** -18)
     assert torch.allclose(narrow, wide[..., :3 * page], rtol=2.0 ** -17, atol=2.0 ** -60) and bool((wide[..., 3 * page:] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------- streams
+def test_the_current_stream_is_found_without_torchs_private_names(monkeypatch):
+    import importlib.util
+
+    from paper_1609_01882_amd import kv
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    spec = importlib.util.spec_from_file_location("paper_1609_01882_amd.kv_of_another_torch", kv.__file__)
+    other = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(other)
+    rng = np.random.default_rng(8)
+    buffers = [_cuda(x) for x in U.random_cache(rng, 4, 2, 64, 128)]
+    table, lengths = _cuda(np.arange(4, dtype=np.int32)[None]), torch.tensor([200], dtype=torch.int32, device="cuda")
+    q = torch.randn((1, 8, 128), device="cuda").bfloat16()
+    want = kv.KvCache(*buffers).attend(q, table, lengths)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        cache = other.KvCache(*buffers)
+        assert cache._stream() == side.cuda_stream
+        got = cache.attend(q, table, lengths)
+    side.synchronize()
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
