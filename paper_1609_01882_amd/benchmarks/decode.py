@@ -34,7 +34,7 @@ def main():
     from ._common import graph_replay_ms, time_ms
 
     batch, heads, dim, group = args.batch, args.kv_heads, args.dim, args.group
-    width = -(-max(args.prompt, args.budget + args.slack) // args.page)
+    width = -(-max(args.prompt, args.budget + max(args.slack, 1)) // args.page)    # a token is written before the cut
     slots = width * args.page
     cache = psc.KvCache.empty(batch * width, heads, dim, args.page)
     table = torch.randperm(batch * width, device="cuda").int().view(batch, width)

@@ -349,3 +349,22 @@ def test_the_current_stream_is_found_without_torchs_private_names(monkeypatch):
         got = cache.attend(q, table, lengths)
     side.synchronize()
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+# ------------------------------------------------------------------------------------------- the example
+def test_the_example_has_room_for_the_token_that_is_cut_at_once(monkeypatch, capsys):
+    import json
+    import sys
+
+    import paper_1609_01882_amd as psc
+    from paper_1609_01882_amd.benchmarks import decode
+    append = psc.KvCache.append
+
+    def fits(self, k, v, table, lengths, **kw):
+        assert int(lengths.max()) + k.shape[0] // table.shape[0] <= table.shape[1] * self.page
+        return append(self, k, v, table, lengths, **kw)
+    monkeypatch.setattr(psc.KvCache, "append", fits)
+    monkeypatch.setattr("paper_1609_01882_amd.benchmarks._common.graph_replay_ms", lambda fn, steps: 0.0)    # (the check above is no work for a graph)
+    monkeypatch.setattr(sys, "argv", "decode --batch 1 --kv-heads 1 --group 2 --page 32 --prompt 60 --chunk 50 --budget 64 --recent 30 --slack 0 --tokens 9".split())
+    decode.main()
+    assert json.loads(capsys.readouterr().out)["token_ms"] > 0
