@@ -154,7 +154,7 @@ __device__ __forceinline__ int sixteen_of(const KvView &c, int b, int head, int 
 // ------------------------------------------------------------------------------------------- append, read
 // D / 8 lanes to a (row, head), 8 coordinates of its key and of its value to a lane; four lanes share a scale, whose largest
 // magnitude they find as integers.  Bound by HBM: 27 thousand rows of 8 heads x 128 float16 (141 MB) in 33 us, 4.3 TB/s;
-// kv_read_kernel gives the same back in 28 us, 5.1 TB/s.
+// kv_read_kernel gives the same back in 30 us, 4.7 TB/s.
 template <int DT, int D>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRows r)
 {
@@ -474,7 +474,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // coordinates of 8 tokens and pairs up the tokens' values of one coordinate with one permutation each.
 // What it is bound by: a few rows read the cache at 5.7 TB/s (8 sequences of 53 to 131 thousand tokens x 8 heads x 128, 825 MB
 // in 145 us); many rows are bound by vector instructions (32 rows x 32 tokens: 16 exp2 of four issue slots each, 64 conversions,
-// 32 permutations, 110 others for 32 products): 2048 rows of 4 x 8 heads over 16384 tokens 653 us, 800 TFLOP/s.
+// 32 permutations, 110 others for 32 products): 2048 rows of 4 x 8 heads over 16384 tokens 656 us, 795 TFLOP/s.
 // Scores, maximum, sum and output are 32-bit floats.  Probabilities are rounded to float16: by at most 2^-11 of each, an
 // eighth of what the output's own rounding to bfloat16 may add (float32 rows: two float16, 2^-22 of each down to 2^-18 of the
 // largest), and never by more than 2^-40 of the row's largest beyond that (kLift).
@@ -1010,9 +1010,9 @@ __global__ __launch_bounds__(256) void kv_weights_of_scores_kernel(KvView c, KvQ
 // The same with the scores once more, from the same products as in the attention itself, so that with the row's reference and
 // sum each probability is the one that was used, before it was rounded.  kSplitRows: a workgroup has 16 kTiles tokens and each wave a quarter of the
 // rows that can see one; otherwise a wave has 16 kTiles tokens and all rows.  The next 16 rows are on their way while 16 are worked on,
-// their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.  Bound by
-// vector instructions (16 exp2 and some 90 others for 16 rows x 64 tokens): up to 701 rows of 3 x 4 heads x 64 over 5003, 40 us
-// (with 32 tokens 52).
+// their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.  16 exp2
+// and some 90 other vector instructions for 16 rows x 64 tokens: up to 701 rows of 3 x 4 heads x 64 over 5003, 40 us (with 32
+// tokens 52), in which a compute unit works 58 % of the time and issues vector instructions in 81 % of the cycles that it works.
 template <int D, int DT, bool kSplitRows, int kTiles>
 __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
 {
@@ -1153,7 +1153,7 @@ __device__ __forceinline__ uint32_t claim_of(const KvEvict &e, int seen, float w
 //   kv_list_kernel    the lists
 // One workgroup per kv head for all of it took 231 us for 8 x 8 memories of up to 131072 tokens, five passes of which each
 // waits for memory; the four
-// kernels take 64 (whole call 121.6; with 8, 12, 24, 32 claims to a thread 127, 123, 131, 146): issue of the ballots and the
+// kernels take 65 (whole call 123; when it was 121.6, with 8, 12, 24, 32 claims to a thread 127, 123, 131, 146): issue of the ballots and the
 // counts' conflicts in LDS, then what each waits for at its start.
 constexpr int kSegmentKeys = 16, kSegment = kEvictThreads * kSegmentKeys, kBins = 2048;
 
@@ -1340,7 +1340,7 @@ __global__ __launch_bounds__(kEvictThreads) void kv_select_kernel(KvView c, KvEv
     if (tid == 0) e.free_slots[bh] = all_holes;
 }
 
-// (8 waves to a SIMD here and in the next: two workgroups to a compute unit, 110.8 us for 114.1)
+// (8 waves to a SIMD here and in the next, two workgroups to a compute unit: 8 x 8 memories of 131072 tokens cut to 8192 3 % faster)
 __global__ __launch_bounds__(kEvictThreads, 8) void kv_count_kernel(KvView c, KvEvict e)
 {
     const int bh = (int)blockIdx.y, tid = (int)threadIdx.x;
@@ -1677,7 +1677,8 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
     int64_t blocks = (slots + 31) / 32;
     if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
     const int64_t units = p.row_groups * c.batch * c.heads;
-    // workgroups that run at a time (attention_waves of them to a compute unit)
+    // workgroups to a compute unit that attention_waves leaves registers for (of 64 coordinates with 32 rows or float32 the
+    // compiler makes kernels small enough for three; two are counted)
     const int waves = dtype == PSC_F32 ? (c.dim == 256 ? 1 : 2) : c.dim == 256 || p.row_tiles == 2 ? 2 : c.dim == 64 ? 4 : 3;
     // As many units as that, or memories of a few blocks to a wave: parts and their join would cost more than they save.
     if (units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31)
