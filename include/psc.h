@@ -413,6 +413,41 @@ int psc_kv_append(const psc_kv_cache *cache, int dtype, const void *k_dev, int64
                   const void *v_dev, int64_t v_row_stride, int64_t v_head_stride, int nrows, const int32_t *offsets_dev,
                   const int32_t *first_dev, int32_t *positions_dev, float *weights_dev, psc_stream stream);
 
+/* Rotary positions.  The first `dims` coordinates of a head (even; 2 .. head_dim) form dims / 2 pairs (a, b): neighbours if
+ * `interleaved`, else dims / 2 apart.  At position t the i-th pair turns by t times its frequency,
+ *   a' = factor (a cos - b sin)      b' = factor (b cos + a sin)
+ * and what lies behind them stays as it is.  turns_dev [dims / 2]: the frequencies as the share of a turn that one
+ * position adds, in units of 2^-64 (psc_rotary_turns makes them, on the host, from radians between -1024 and 1024), so
+ * that the angle of a far position is as exact as that of a near one.  Frequencies scaled for long contexts are
+ * frequencies like others, and their factor on queries and keys is `factor`. */
+typedef struct psc_rotary {
+    const uint64_t *turns_dev;
+    int dims, interleaved;
+    float factor;
+} psc_rotary;
+int psc_rotary_turns(const double *radians, int n, uint64_t *turns);
+
+/* Rows x_dev [nrows][heads][head_dim] turned (transposed != 0: by the opposite angles, which is the gradient) into
+ * out_dev, which may be x_dev with the same strides.  A row stands at positions_dev[row], or, positions_dev NULL, at
+ * first_dev[b] + its place in its sequence b (offsets_dev as above; first_dev NULL: 0).  Rows that no sequence has are
+ * copied.  Sines and cosines are computed in 64 bits and rounded to 32, products and sums are float32.  head_dim 2 .. 65536,
+ * any even dims; strides in elements, any alignment of the type (16-byte aligned rows and heads with dims a multiple of
+ * 16 and head_dim one of 8 go faster). */
+int psc_rotary_rows(const psc_rotary *rotary, int transposed, int dtype, const void *x_dev, int64_t row_stride,
+                    int64_t head_stride, int nrows, int heads, int head_dim, const int32_t *positions_dev, int batch,
+                    const int32_t *offsets_dev, const int32_t *first_dev, void *out_dev, int64_t out_row_stride,
+                    int64_t out_head_stride, psc_stream stream);
+
+/* psc_kv_append with the keys turned first: row r of sequence b by the angles of first_dev[b] + r (first_dev NULL: its
+ * slot).  Keys are turned in 64 bits and rounded to float32, then to 4 bits.  The queries of the same rows (q_heads may be
+ * 0) are turned into q_out_dev [nrows][q_heads][head_dim], which is another array than q_dev; those of rows that no sequence
+ * has are copied.  dims is a multiple of 16 here. */
+int psc_kv_append_rotary(const psc_kv_cache *cache, const psc_rotary *rotary, int dtype, const void *k_dev,
+                         int64_t k_row_stride, int64_t k_head_stride, const void *v_dev, int64_t v_row_stride,
+                         int64_t v_head_stride, const void *q_dev, int64_t q_row_stride, int64_t q_head_stride,
+                         int q_heads, void *q_out_dev, int nrows, const int32_t *offsets_dev, const int32_t *first_dev,
+                         int32_t *positions_dev, float *weights_dev, psc_stream stream);
+
 /* The values that the cache holds in the slots lengths_dev[b] + r: k_dev, v_dev [nrows][kv_heads][head_dim]. */
 int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *offsets_dev, void *k_dev, void *v_dev,
                 psc_stream stream);
@@ -444,6 +479,25 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
                      int sinks, void *out_dev, float *lse_dev, const float *weights_in_dev, float *weights_out_dev,
                      void *workspace_dev, size_t workspace_bytes, psc_stream stream);
 
+/* Differential attention: kv heads 2j and 2j + 1 are a pair (kv_heads even, head_dim 64 or 128), whose values lie side by side,
+ * 2 head_dim wide, and each of whose keys makes a map of its own.  With g = q_heads / kv_heads, output head j g + i is
+ *   o = softmax(scale q1 K1) V - lam softmax(scale q2 K2) V      of the query heads 2j g + i and (2j + 1) g + i
+ * and, norm_dev [2 head_dim] (float32) given, o / sqrt(mean o^2 + eps) * norm; times `factor` in the end.
+ * lam_dev (float32): that of row r and output head h is lam_dev[r * lam_row_stride + h] (stride 0: the same for all
+ * rows).  out_dev [nrows][q_heads / 2][2 head_dim] (dtype), lse_dev (may be NULL) [nrows][q_heads] of both maps.
+ * Both heads of a pair hold the same tokens in the same slots: positions_dev is read for the even one.  weights_out_dev:
+ * both heads of a pair receive the sum of both maps' probabilities, so that psc_kv_evict cuts them alike where
+ * they began alike.  A map that comes out NaN adds nothing to the weights; its output head is NaN.  Rows that see
+ * nothing come out 0.  Everything else as for psc_kv_attention, the precision of a map's products too. */
+size_t psc_kv_difference_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
+                                         int window, int sinks, int has_positions, int has_weights);
+int psc_kv_difference(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,
+                      int64_t q_head_stride, int nrows, int max_rows, int q_heads, const int32_t *offsets_dev,
+                      const int32_t *first_dev, const int32_t *positions_dev, float scale, int causal, int window,
+                      int sinks, const float *lam_dev, int64_t lam_row_stride, const float *norm_dev, float eps,
+                      float factor, void *out_dev, float *lse_dev, const float *weights_in_dev, float *weights_out_dev,
+                      void *workspace_dev, size_t workspace_bytes, psc_stream stream);
+
 /* Cuts every (sequence, kv head) with more than `budget` tokens down to the budget.  Kept are the tokens at positions
  * below `sinks` and at seen_dev[b] - recent and later (seen_dev NULL: lengths_dev; sinks + recent <= budget), then
  * those of the largest weights_dev (per slot; NaN counts as the smallest); the lower slot on equal weight.  Slots without
@@ -461,6 +515,47 @@ int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int3
                  const int32_t *seen_dev, int budget, int sinks, int recent, int32_t *kept_dev,
                  int32_t *lengths_out_dev, int32_t *positions_out_dev, float *weights_out_dev, int64_t out_stride,
                  void *workspace_dev, size_t workspace_bytes, psc_stream stream);
+
+/* ------------------------------------------------------------------ norms around a block */
+/* What stands between two blocks of a layer, in one pass over a residual stream x [rows][width] and a block's output y:
+ *   u = rms(y) * after * act(gate)      rms(t) = t / sqrt(mean t^2 + eps)
+ *   h = residual_scale x + block_scale u      z = rms(h) * before
+ * x_dev or y_dev may be NULL (that share is 0), as may be after_dev (then u has y itself), gate_dev (then no gate) and
+ * before_dev (then no z).  x and h are of stream_dtype, y, gate and z of block_dtype (stream_dtype float32 or the same), the
+ * weights after_dev, before_dev [width] of weight_dtype (float32 or the block's).  Rows x_stride, y_stride, gate_stride
+ * elements apart, coordinates contiguous, no alignment beyond the type's.  gate_dev has gate_rows rows, of
+ * which each serves rows / gate_rows consecutive rows: one to a row, to a sequence of equal lengths, or one to all.
+ * width 1 .. 16384.  Everything between loads and stores is float32. */
+#define PSC_GATE_PLAIN 0
+#define PSC_GATE_SIGMOID 1
+#define PSC_GATE_SILU 2
+#define PSC_MAX_NORM_WIDTH 16384
+typedef struct psc_residual_norm {
+    int rows, width;
+    int stream_dtype, block_dtype, weight_dtype;
+    const void *x_dev;
+    int64_t x_stride;
+    const void *y_dev;
+    int64_t y_stride;
+    const void *gate_dev;
+    int64_t gate_stride;
+    int gate_rows, activation;
+    const void *after_dev, *before_dev;
+    float residual_scale, block_scale, eps;
+} psc_residual_norm;
+
+/* h_dev, z_dev [rows][width] (either may be NULL: not wanted); stat_dev (may be NULL) [rows][2] float32: what the backward
+ * pass takes. */
+int psc_residual_norm_forward(const psc_residual_norm *norm, void *h_dev, void *z_dev, float *stat_dev, psc_stream stream);
+
+/* Gradients from dh_dev and dz_dev [rows][width] (NULL: zero), of the same inputs with the forward pass's stat_dev:
+ * dx_dev, dy_dev [rows][width], dgate_dev [gate_rows][width], dafter_dev, dbefore_dev [width], of the types of x, y, gate
+ * and the weights; each may be NULL (not wanted).  Sums over rows are float32 and added in one order: results repeat bit
+ * for bit. */
+size_t psc_residual_norm_workspace_bytes(const psc_residual_norm *norm);
+int psc_residual_norm_backward(const psc_residual_norm *norm, const float *stat_dev, const void *dh_dev, const void *dz_dev,
+                               void *dx_dev, void *dy_dev, void *dgate_dev, void *dafter_dev, void *dbefore_dev,
+                               void *workspace_dev, size_t workspace_bytes, psc_stream stream);
 
 /* Synchronise `stream` and report whether any scan that used this workspace since
  * the last call gave up on an internal wait (never expected; results of such a

@@ -1,7 +1,8 @@
 """Polysemous-code search on AMD MI355X: Python face of libpsc.so (HIP, gfx950).
 
 The compute lives in `csrc/` behind the C ABI declared in `include/psc.h`; this package only
-marshals arguments (see `binding.py`; `kv.py` for attention over a memory held in 4 bits).
+marshals arguments (see `binding.py`; `kv.py` for attention over a memory held in 4 bits, `layer.py` for rotary
+positions and norms around a block).
 """
 from .binding import (  # noqa: F401
     Index,
@@ -22,3 +23,4 @@ from .binding import (  # noqa: F401
     workspace_status,
 )
 from .kv import KvCache  # noqa: F401
+from .layer import Rotary, residual_norm, rotary_frequencies  # noqa: F401

@@ -80,11 +80,20 @@ def _load():
         "psc_imi_search": (i32, [vp, vp, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
         "psc_workspace_status": (i32, [vp, vp]),
         "psc_kv_append": (i32, [vp, i32, vp, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp]),
+        "psc_kv_append_rotary": (i32, [vp, vp, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, vp, i32, vp, vp, vp, vp, vp]),
         "psc_kv_read": (i32, [vp, i32, i32, vp, vp, vp, vp]),
         "psc_kv_attention_workspace_bytes": (sz, [vp, i32, i32, i32, i32, i32, i32, i32, i32]),
         "psc_kv_attention": (i32, [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, C.c_float, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
+        "psc_kv_difference_workspace_bytes": (sz, [vp, i32, i32, i32, i32, i32, i32, i32, i32]),
+        "psc_kv_difference": (i32, [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, C.c_float, i32, i32, i32, vp, i64, vp, C.c_float, C.c_float,
+                                    vp, vp, vp, vp, vp, sz, vp]),
         "psc_kv_evict_workspace_bytes": (sz, [vp, i32]),
         "psc_kv_evict": (i32, [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, i64, vp, sz, vp]),
+        "psc_rotary_turns": (i32, [vp, i32, vp]),
+        "psc_rotary_rows": (i32, [vp, i32, i32, vp, i64, i64, i32, i32, i32, vp, i32, vp, vp, vp, i64, i64, vp]),
+        "psc_residual_norm_forward": (i32, [vp, vp, vp, vp, vp]),
+        "psc_residual_norm_workspace_bytes": (sz, [vp]),
+        "psc_residual_norm_backward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -107,8 +116,10 @@ def exported_symbols():
             "psc_ivf_assign_encode", "psc_ivf_set_lists", "psc_ivf_search_workspace_bytes",
             "psc_ivf_search", "psc_imi_set_coarse", "psc_imi_assign_workspace_bytes", "psc_imi_assign_encode",
             "psc_imi_set_lists", "psc_imi_search_workspace_bytes", "psc_imi_search", "psc_workspace_status",
-            "psc_kv_append", "psc_kv_read", "psc_kv_attention_workspace_bytes", "psc_kv_attention",
-            "psc_kv_evict_workspace_bytes", "psc_kv_evict"]
+            "psc_kv_append", "psc_kv_append_rotary", "psc_kv_read", "psc_kv_attention_workspace_bytes", "psc_kv_attention",
+            "psc_kv_difference_workspace_bytes", "psc_kv_difference", "psc_kv_evict_workspace_bytes", "psc_kv_evict",
+            "psc_rotary_turns", "psc_rotary_rows", "psc_residual_norm_forward", "psc_residual_norm_workspace_bytes",
+            "psc_residual_norm_backward"]
 
 
 def _check(rc: int):

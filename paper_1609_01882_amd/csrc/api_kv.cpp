@@ -3,15 +3,12 @@
 #include <cmath>
 #include <cstdlib>
 
-#include "common.h"
+#include "api_checks.h"
 
 namespace psc {
 namespace {
 
 constexpr int64_t kMostSlots = (int64_t)1 << 30, kMostGroups = 65535;
-constexpr int64_t kMostWorkgroups = ((int64_t)1 << 24) - 1;  // of 256 lanes: a dimension of a grid has under 2^32 lanes
-
-bool aligned(const void *p, uintptr_t to = 16) { return (uintptr_t)p % to == 0; }
 
 // The cache's own fields; what a call does not touch may be null (tables and lengths are always needed).
 int check_cache(const psc_kv_cache *c, KvView *v)
@@ -53,29 +50,11 @@ int check_buffers(const psc_kv_cache *c, KvView *v)
     return PSC_OK;
 }
 
-int check_dtype(int dtype)
-{
-    PSC_REQUIRE(dtype == PSC_BF16 || dtype == PSC_F16 || dtype == PSC_F32, "dtype must be PSC_BF16, PSC_F16 or PSC_F32, got %d", dtype);
-    return PSC_OK;
-}
-
 int check_rows(const KvView &v, int nrows, const int32_t *offsets)
 {
     PSC_REQUIRE(nrows >= 0, "%d rows", nrows);
     PSC_REQUIRE(offsets || nrows % v.batch == 0, "%d rows are no multiple of %d sequences, and there are no offsets", nrows, v.batch);
     PSC_REQUIRE(aligned(offsets, 4), "misaligned offsets");
-    return PSC_OK;
-}
-
-// (A stride that leads to no second row or head may be anything.)
-int check_strides(const char *what, const void *p, int dtype, int nrows, int64_t row, int heads, int64_t head)
-{
-    const int64_t unit = dtype == PSC_F32 ? 4 : 8;  // elements in 16 bytes
-    row = nrows > 1 ? row : 0;
-    head = heads > 1 ? head : 0;
-    PSC_REQUIRE(p != nullptr, "null %s", what);
-    PSC_REQUIRE(aligned(p) && row % unit == 0 && head % unit == 0, "%s: rows and heads must start at multiples of 16 bytes", what);
-    PSC_REQUIRE(std::llabs(row) < (1ll << 40) && std::llabs(head) < (1ll << 40), "%s: stride too large", what);
     return PSC_OK;
 }
 
@@ -90,16 +69,89 @@ int check_attention(const KvView &v, int dtype, int nrows, int max_rows, int q_h
     return PSC_OK;
 }
 
+int check_pairs(const KvView &v)
+{
+    PSC_REQUIRE(v.heads % 2 == 0, "differential attention takes pairs of kv heads, got %d", v.heads);
+    PSC_REQUIRE(v.dim == 64 || v.dim == 128, "differential attention takes a head_dim of 64 or 128, got %d", v.dim);
+    return PSC_OK;
+}
+
+// What both attentions take alike.
+struct QueryCall {
+    int dtype;
+    const void *q;
+    int64_t row_stride, head_stride;
+    int nrows, max_rows, q_heads;
+    const int32_t *offsets, *first, *positions;
+    float scale;
+    int causal, window, sinks;
+    void *out;
+    float *lse;
+    const float *weights_in;
+    float *weights_out;
+};
+
+int check_query_call(const KvView &v, const QueryCall &a, KvQueries *q)
+{
+    int rc = check_attention(v, a.dtype, a.nrows, a.max_rows, a.q_heads, a.window, a.sinks);
+    if (rc == PSC_OK) rc = check_rows(v, a.nrows, a.offsets);
+    if (rc != PSC_OK) return rc;
+    PSC_REQUIRE(a.scale > 0.f && std::isfinite(a.scale), "scale must be positive and finite");
+    PSC_REQUIRE(a.window == 0 || a.causal, "a window needs causal attention");
+    PSC_REQUIRE(a.weights_out || !a.weights_in, "weights_in without weights_out");
+    PSC_REQUIRE(aligned(a.first, 4) && aligned(a.positions) && aligned(a.weights_in) && aligned(a.weights_out) && aligned(a.lse, 4),
+                "misaligned first, positions, weights or lse");
+    const int max_rows = a.offsets && a.nrows > 0 ? a.max_rows : a.nrows / v.batch;
+    PSC_REQUIRE(a.nrows == 0 || max_rows >= 1, "max_rows must be at least 1");
+    PSC_REQUIRE((int64_t)max_rows * v.batch >= a.nrows, "%d rows are more than max_rows (%d) of each of %d sequences", a.nrows, max_rows, v.batch);
+    if (a.nrows > 0) {
+        rc = check_strides("q", a.q, a.dtype, a.nrows, a.row_stride, a.q_heads, a.head_stride);
+        if (rc == PSC_OK) rc = check_strides("out", a.out, a.dtype, 0, 0, 0, 0);
+        if (rc != PSC_OK) return rc;
+    }
+    q->q = a.q;
+    q->row_stride = a.row_stride;
+    q->head_stride = a.head_stride;
+    q->nrows = a.nrows;
+    q->each = a.nrows / v.batch;
+    q->max_rows = max_rows;
+    q->q_heads = a.q_heads;
+    q->group = a.q_heads / v.heads;
+    q->unit_heads = v.heads;
+    q->offsets = a.offsets;
+    q->first = a.first;
+    q->positions = a.positions;
+    q->factor = (float)((double)a.scale * 1.4426950408889634);
+    q->causal = a.causal != 0;
+    q->window = a.window;
+    q->sinks = a.sinks;
+    q->out = a.out;
+    q->lse = a.lse;
+    return PSC_OK;
+}
+
+int use_plan(const KvView &v, const KvPlan &p, void *workspace, size_t bytes, KvQueries *q)
+{
+    PSC_REQUIRE(p.row_groups <= kMostWorkgroups, "%d rows of a sequence are too many for a launch", q->max_rows);
+    PSC_REQUIRE(p.weights_groups <= kMostWorkgroups, "%lld slots are too many for the weights of %d rows", (long long)v.width << v.page_shift, q->max_rows);
+    PSC_REQUIRE(bytes >= p.bytes() && (p.bytes() == 0 || workspace), "workspace too small: %zu bytes, %zu needed", bytes, p.bytes());
+    PSC_REQUIRE(aligned(workspace), "workspace must be 16-byte aligned");
+    char *ws = (char *)workspace;
+    q->unit_rows = 16 * p.row_tiles;
+    q->workgroups = (uint32_t)p.workgroups;
+    q->least_blocks = (uint32_t)p.least_blocks;
+    q->part_stat = (float *)ws;
+    q->part_acc = (float *)(ws + p.part_stat_bytes);
+    q->stat = p.stat_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes) : nullptr;
+    q->scores = p.scores_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes + p.stat_bytes) : nullptr;
+    q->scores_rows = p.scores_rows;
+    return PSC_OK;
+}
+
 }  // namespace
 }  // namespace psc
 
 using namespace psc;
-
-#define PSC_TRY(expr)                  \
-    do {                               \
-        const int rc_ = (expr);        \
-        if (rc_ != PSC_OK) return rc_; \
-    } while (0)
 
 extern "C" {
 
@@ -119,6 +171,42 @@ int psc_kv_append(const psc_kv_cache *cache, int dtype, const void *k_dev, int64
     const KvRows r{k_dev, v_dev, k_row_stride, k_head_stride, v_row_stride, v_head_stride, nrows, nrows / v.batch, offsets_dev, first_dev,
                    positions_dev, weights_dev};
     return launch_kv_append(v, dtype, r, (hipStream_t)stream);
+}
+
+int psc_kv_append_rotary(const psc_kv_cache *cache, const psc_rotary *rotary, int dtype, const void *k_dev,
+                         int64_t k_row_stride, int64_t k_head_stride, const void *v_dev, int64_t v_row_stride,
+                         int64_t v_head_stride, const void *q_dev, int64_t q_row_stride, int64_t q_head_stride,
+                         int q_heads, void *q_out_dev, int nrows, const int32_t *offsets_dev, const int32_t *first_dev,
+                         int32_t *positions_dev, float *weights_dev, psc_stream stream)
+{
+    KvView v{};
+    PSC_TRY(check_buffers(cache, &v));
+    PSC_TRY(check_dtype(dtype));
+    PSC_TRY(check_rows(v, nrows, offsets_dev));
+    Rotary t{};
+    PSC_TRY(check_rotary(rotary, v.dim, &t));
+    PSC_REQUIRE(t.dims % 16 == 0, "keys of a memory are turned in multiples of 16 coordinates, got %d", t.dims);
+    PSC_REQUIRE(q_heads >= 0 && q_heads <= 65536, "%d query heads: 0 to 65536", q_heads);
+    if (nrows == 0) return PSC_OK;
+    PSC_TRY(check_strides("k", k_dev, dtype, nrows, k_row_stride, v.heads, k_head_stride));
+    PSC_TRY(check_strides("v", v_dev, dtype, nrows, v_row_stride, v.heads, v_head_stride));
+    if (q_heads > 0) {
+        PSC_TRY(check_strides("q", q_dev, dtype, nrows, q_row_stride, q_heads, q_head_stride));
+        PSC_TRY(check_strides("q_out", q_out_dev, dtype, 0, 0, 0, 0));
+        PSC_REQUIRE(q_out_dev != q_dev, "queries cannot be turned in place while keys are appended");
+    }
+    PSC_REQUIRE(aligned(first_dev, 4) && aligned(positions_dev) && aligned(weights_dev), "misaligned first, positions or weights");
+    PSC_REQUIRE((int64_t)nrows * (v.heads + q_heads) * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows,
+                v.heads + q_heads, v.dim);
+    const KvRows r{k_dev, v_dev, k_row_stride, k_head_stride, v_row_stride, v_head_stride, nrows, nrows / v.batch, offsets_dev, first_dev,
+                   positions_dev, weights_dev};
+    RotaryQueries q{};
+    q.q = q_dev;
+    q.out = q_out_dev;
+    q.row_stride = q_row_stride;
+    q.head_stride = q_head_stride;
+    q.heads = q_heads;
+    return launch_kv_append_rotary(v, dtype, r, t, q, (hipStream_t)stream);
 }
 
 int psc_kv_read(const psc_kv_cache *cache, int dtype, int nrows, const int32_t *offsets_dev, void *k_dev, void *v_dev,
@@ -160,56 +248,53 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
 {
     KvView v{};
     PSC_TRY(check_buffers(cache, &v));
-    PSC_TRY(check_attention(v, dtype, nrows, max_rows, q_heads, window, sinks));
-    PSC_TRY(check_rows(v, nrows, offsets_dev));
-    PSC_REQUIRE(scale > 0.f && std::isfinite(scale), "scale must be positive and finite");
-    PSC_REQUIRE(window == 0 || causal, "a window needs causal attention");
-    PSC_REQUIRE(weights_out_dev || !weights_in_dev, "weights_in without weights_out");
-    PSC_REQUIRE(aligned(first_dev, 4) && aligned(positions_dev) && aligned(weights_in_dev) && aligned(weights_out_dev) && aligned(lse_dev, 4),
-                "misaligned first, positions, weights or lse");
-    if (!offsets_dev || nrows == 0) max_rows = nrows / v.batch;
-    PSC_REQUIRE(nrows == 0 || max_rows >= 1, "max_rows must be at least 1");
-    PSC_REQUIRE((int64_t)max_rows * v.batch >= nrows, "%d rows are more than max_rows (%d) of each of %d sequences", nrows, max_rows, v.batch);
-    if (nrows > 0) {
-        PSC_TRY(check_strides("q", q_dev, dtype, nrows, q_row_stride, q_heads, q_head_stride));
-        PSC_TRY(check_strides("out", out_dev, dtype, 0, 0, 0, 0));
-    } else if (!weights_out_dev) {
-        return PSC_OK;
-    }
-    const int group = q_heads / v.heads;
-    const KvPlan p = plan_kv_attention(v, dtype, group, nrows, max_rows, window, sinks, !positions_dev, weights_out_dev != nullptr);
-    PSC_REQUIRE(p.row_groups <= kMostWorkgroups, "%d rows of a sequence are too many for a launch", max_rows);
-    PSC_REQUIRE(p.weights_groups <= kMostWorkgroups, "%lld slots are too many for the weights of %d rows", (long long)v.width << v.page_shift, max_rows);
-    PSC_REQUIRE(workspace_bytes >= p.bytes() && (p.bytes() == 0 || workspace_dev), "workspace too small: %zu bytes, %zu needed", workspace_bytes, p.bytes());
-    PSC_REQUIRE(aligned(workspace_dev), "workspace must be 16-byte aligned");
+    const QueryCall a{dtype, q_dev, q_row_stride, q_head_stride, nrows, max_rows, q_heads, offsets_dev, first_dev, positions_dev, scale, causal, window,
+                      sinks, out_dev, lse_dev, weights_in_dev, weights_out_dev};
     KvQueries q{};
-    q.q = q_dev;
-    q.row_stride = q_row_stride;
-    q.head_stride = q_head_stride;
-    q.nrows = nrows;
-    q.each = nrows / v.batch;
-    q.max_rows = max_rows;
-    q.q_heads = q_heads;
-    q.group = group;
-    q.offsets = offsets_dev;
-    q.first = first_dev;
-    q.positions = positions_dev;
-    q.factor = (float)((double)scale * 1.4426950408889634);
-    q.causal = causal != 0;
-    q.window = window;
-    q.sinks = sinks;
-    q.out = out_dev;
-    q.lse = lse_dev;
-    q.unit_rows = 16 * p.row_tiles;
-    q.workgroups = (uint32_t)p.workgroups;
-    q.least_blocks = (uint32_t)p.least_blocks;
-    char *ws = (char *)workspace_dev;
-    q.part_stat = (float *)ws;
-    q.part_acc = (float *)(ws + p.part_stat_bytes);
-    q.stat = p.stat_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes) : nullptr;
-    q.scores = p.scores_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes + p.stat_bytes) : nullptr;
-    q.scores_rows = p.scores_rows;
+    PSC_TRY(check_query_call(v, a, &q));
+    if (nrows == 0 && !weights_out_dev) return PSC_OK;
+    const KvPlan p = plan_kv_attention(v, dtype, q.group, nrows, q.max_rows, window, sinks, !positions_dev, weights_out_dev != nullptr);
+    PSC_TRY(use_plan(v, p, workspace_dev, workspace_bytes, &q));
     return launch_kv_attention(v, dtype, q, p, weights_in_dev, weights_out_dev, (hipStream_t)stream);
+}
+
+size_t psc_kv_difference_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
+                                         int window, int sinks, int has_positions, int has_weights)
+{
+    KvView v{};
+    if (check_cache(cache, &v) != PSC_OK || check_pairs(v) != PSC_OK || check_attention(v, dtype, nrows, max_rows, q_heads, window, sinks) != PSC_OK) return 0;
+    if (nrows == 0) return 0;
+    const auto bytes = [&](int most) {
+        return plan_kv_difference(v, dtype, q_heads / v.heads, nrows, most, window, sinks, !has_positions, has_weights != 0).bytes();
+    };
+    return std::max(bytes(max_rows), bytes((int)(((int64_t)nrows + v.batch - 1) / v.batch)));
+}
+
+int psc_kv_difference(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,
+                      int64_t q_head_stride, int nrows, int max_rows, int q_heads, const int32_t *offsets_dev,
+                      const int32_t *first_dev, const int32_t *positions_dev, float scale, int causal, int window,
+                      int sinks, const float *lam_dev, int64_t lam_row_stride, const float *norm_dev, float eps,
+                      float factor, void *out_dev, float *lse_dev, const float *weights_in_dev, float *weights_out_dev,
+                      void *workspace_dev, size_t workspace_bytes, psc_stream stream)
+{
+    KvView v{};
+    PSC_TRY(check_buffers(cache, &v));
+    PSC_TRY(check_pairs(v));
+    const QueryCall a{dtype, q_dev, q_row_stride, q_head_stride, nrows, max_rows, q_heads, offsets_dev, first_dev, positions_dev, scale, causal, window,
+                      sinks, out_dev, lse_dev, weights_in_dev, weights_out_dev};
+    KvQueries q{};
+    PSC_TRY(check_query_call(v, a, &q));
+    PSC_REQUIRE(std::isfinite(factor), "factor must be finite");
+    PSC_REQUIRE(!norm_dev || (eps >= 0.f && std::isfinite(eps)), "eps must be finite and not negative");
+    PSC_REQUIRE(aligned(lam_dev, 4) && aligned(norm_dev, 4), "misaligned lam or norm");
+    PSC_REQUIRE(nrows == 0 || lam_dev, "null lam");
+    PSC_REQUIRE(std::llabs(lam_row_stride) < (1ll << 40), "lam: stride too large");
+    if (nrows == 0 && !weights_out_dev) return PSC_OK;
+    q.unit_heads = v.heads / 2;
+    const KvPlan p = plan_kv_difference(v, dtype, q.group, nrows, q.max_rows, window, sinks, !positions_dev, weights_out_dev != nullptr);
+    PSC_TRY(use_plan(v, p, workspace_dev, workspace_bytes, &q));
+    const KvDifference d{lam_dev, lam_row_stride, norm_dev, eps, factor};
+    return launch_kv_difference(v, dtype, q, d, p, weights_in_dev, weights_out_dev, (hipStream_t)stream);
 }
 
 size_t psc_kv_evict_workspace_bytes(const psc_kv_cache *cache, int budget)

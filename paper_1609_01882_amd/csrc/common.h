@@ -338,10 +338,82 @@ struct KvRows {
 };
 int launch_kv_append(const KvView &c, int dtype, const KvRows &r, hipStream_t s);
 int launch_kv_read(const KvView &c, int dtype, const KvRows &r, void *k_out, void *v_out, hipStream_t s);
+
+// ---- norms around a block (kernels_norm.hip)
+struct ResidualNorm {
+    const void *x, *y, *gate, *after, *before;  // each may be null (x or y is there)
+    int64_t x_stride, y_stride, gate_stride;
+    int rows, width;
+    int gate_each;  // rows that share a gate row
+    int activation, weight_f32;
+    float residual_scale, block_scale, eps;
+    int lanes;      // of a row
+};
+struct NormGradients {
+    const float *stat;     // [rows][2]: 1 / root of y, of h
+    const void *dh, *dz;   // may be null
+    void *dx, *dy, *dgate, *dafter, *dbefore;
+    int groups, split, gates_of_group;  // workgroups; workgroups of a gate row, or gate rows of a workgroup
+    float *after_parts, *before_parts, *gate_parts;  // [groups][width], or null
+};
+struct NormPlan {
+    int lanes = 0, groups = 0, split = 1, gates_of_group = 1;
+};
+NormPlan plan_residual_norm(int rows, int width, int gate_each);
+int launch_residual_norm(const ResidualNorm &p, int stream_dtype, int block_dtype, void *h, void *z, float *stat, hipStream_t s);
+int launch_residual_norm_backward(const ResidualNorm &p, int stream_dtype, int block_dtype, const NormGradients &d, hipStream_t s);
+
+// ---- rotary positions (kernels_rotary.hip)
+struct Rotary {
+    const uint64_t *turns;  // [dims / 2]: of a turn that a position adds, in units of 2^-64
+    int dims, interleaved;
+    float factor;
+};
+// Rows [nrows][heads][head_dim] at positions of their own, or first[b] + place in their sequence (first null: place).
+struct RotaryRows {
+    const void *x;
+    void *out;
+    int64_t row_stride, head_stride, out_row_stride, out_head_stride;
+    int nrows, heads, head_dim, batch, each;
+    const int32_t *positions, *offsets, *first;
+    int transposed;
+    int group;  // heads that a thread takes
+
+    __device__ int64_t position_of(int row, bool *nobodys) const
+    {
+        *nobodys = false;
+        if (positions) return positions[row];
+        int b = each ? row / each : 0, begin = b * each;
+        if (offsets) {
+            int hi = batch;
+            b = 0;
+            while (hi - b > 1) {
+                const int mid = (b + hi) >> 1;
+                if (offsets[mid] <= row) b = mid;
+                else hi = mid;
+            }
+            begin = offsets[b];
+            *nobodys = row < begin || row >= offsets[batch];
+        }
+        return (int64_t)(first ? first[b] : 0) + row - begin;
+    }
+};
+int launch_rotary(const Rotary &t, int dtype, const RotaryRows &r, bool wide, hipStream_t s);
+// Queries of the rows that are appended, turned by the same angles: out [nrows][heads][head_dim].
+struct RotaryQueries {
+    const void *q;
+    void *out;
+    int64_t row_stride, head_stride;
+    int heads;
+    int group;  // kv and query heads that a thread takes
+};
+int launch_kv_append_rotary(const KvView &c, int dtype, const KvRows &r, const Rotary &t, const RotaryQueries &q, hipStream_t s);
+
 struct KvQueries {
     const void *q;
     int64_t row_stride, head_stride;
     int nrows, each, max_rows, q_heads, group;
+    int unit_heads;               // units of work to a sequence's rows: kv heads, or pairs of them
     const int32_t *offsets, *first, *positions;
     float factor;  // scale / log 2
     int causal, window, sinks;
@@ -371,6 +443,17 @@ KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, i
 // received (or null): given (or 0) + the weight each token received.
 int launch_kv_attention(const KvView &c, int dtype, const KvQueries &q, const KvPlan &p, const float *given, float *received,
                         hipStream_t s);
+// Differential attention (kernels_difference.hip): what it takes beyond the queries.
+struct KvDifference {
+    const float *lam;    // [..][q_heads / 2], rows lam_stride apart
+    int64_t lam_stride;
+    const float *norm;   // [2 dim], or null
+    float eps, factor;
+};
+KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered,
+                          bool weights);
+int launch_kv_difference(const KvView &c, int dtype, const KvQueries &q, const KvDifference &d, const KvPlan &p, const float *given,
+                         float *received, hipStream_t s);
 struct KvSegment {  // of a long memory: see kernels_kv.hip
     uint32_t above, first, count, ties;
 };

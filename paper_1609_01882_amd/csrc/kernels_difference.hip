@@ -1,0 +1,559 @@
+// Differential attention over the attention memory in 4 bits (the format: kv_device.h).
+//
+// kv heads 2j and 2j + 1 are a pair: each has keys of its own, their values lie side by side (2 D wide), and an output head is
+//   o = softmax(s q1 K1) V - lam softmax(s q2 K2) V,   then o * rsqrt(mean o^2 + eps) * norm * factor.
+// A wave has both maps of its rows, so that the memory is read once, and values are expanded once for both.
+#include <algorithm>
+#include <type_traits>
+
+#include "kv_weights.h"
+
+namespace psc {
+namespace {
+
+// One wave attends with 16 RT rows, in both maps, over every fourth of the workgroup's blocks.  As in kv_attention_kernel: scores K Q^T leave
+// 8 scores of one row in a lane, which are the operand of V^T P^T as they are; maximum, sum and rescaling are the lane's own.
+// Tile t of map w is number w RT + t.  Accumulator (h D / 16 + j) of a tile has coordinate (4 g + r) D / 16 + j of value half h.
+template <int D, int DT, int RT, bool kPos>
+struct Difference {
+    f32x4 acc[2 * RT][D / 8];
+    float top[2 * RT], sum[2 * RT];  // of the scaled scores in units of log 2, the maximum less kLift; the sum is the lane's own share
+    Rows<D, DT> rows[2 * RT];
+
+    // kFar: rows whose scores are coarse may be among them
+    template <bool kFar>
+    __device__ __forceinline__ void block(const KvQueries &q, const Raw<D> (&raw)[2], const int (&positions)[8], const RowMask (&mask)[RT], int slot, int lim0, int lim1,
+                                          int n, bool whole, float factor, int i, int g, float *scores, int64_t scores_stride)
+    {
+        f32x4 s[2 * RT][2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 a[D / 32];
+                expand_keys<D, DT>(raw[w].k[h], raw[w].ks[h], a);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) s[w * RT + t][h] = scores_of<D, DT>(a, rows[w * RT + t]);
+            }
+        if (!whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = slot + 16 * h + 4 * g + r;
+                    const bool there = at < (h ? lim1 : lim0);
+                    const int pos = kPos ? positions[4 * h + r] : at;
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+                        if (!(there && sees(q, mask[t], pos))) s[t][h][r] = s[RT + t][h][r] = kNegInf;
+                }
+        }
+        if constexpr (RT == 1) {
+            if (scores) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (slot + 16 * h < n) *(f32x4 *)(scores + w * scores_stride + slot + 16 * h + 4 * g) = s[w][h];
+            }
+        }
+        uint32_t p[2 * RT][2][4];  // float16 pairs (the second array: what the first leaves of float32 rows' probabilities)
+#pragma unroll
+        for (int t = 0; t < 2 * RT; ++t) {
+            float m = kNegInf;  // (NaN where a score is: the row is lost then, whatever the maximum)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) m = __builtin_elementwise_maximum(m, s[t][h][r]);
+            m = __builtin_fmaf(column_max(m), factor, -kLift);
+            if (__any(m > top[t])) {
+                const float now = fmaxf(top[t], kFar ? reference_below(m) : m);
+                const float shrink = now == kNegInf ? 1.f : exp2_fast(top[t] - now);
+                top[t] = now;
+                sum[t] *= shrink;
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) acc[t][j] *= shrink;
+            }
+            const float base = top[t] == kNegInf ? 0.f : top[t];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    float e0 = __builtin_fmaf(s[t][h][r], factor, -base), e1 = __builtin_fmaf(s[t][h][r + 1], factor, -base);
+                    if constexpr (kFar) {
+                        const float most = most_exponent(base);
+                        e0 = __builtin_elementwise_minimum(e0, most);  // (NaN stays)
+                        e1 = __builtin_elementwise_minimum(e1, most);
+                    }
+                    e0 = exp2_fast(e0);
+                    e1 = exp2_fast(e1);
+                    sum[t] += e0 + e1;
+                    const h16x2 hi = {(_Float16)e0, (_Float16)e1};
+                    p[t][0][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, hi);
+                    if constexpr (DT == PSC_F32) {
+                        const h16x2 lo = {(_Float16)(e0 - (float)hi.x), (_Float16)(e1 - (float)hi.y)};
+                        p[t][1][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, lo);
+                    }
+                }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            // tokens 0..7 of the lane: 4 g + r, then 16 + 4 g + r
+            uint32_t held[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) held[t] = value_scale<D>(raw[half].vs[t >> 2], t & 3, i);
+            if (!whole) {  // what lies past the end may be NaN: with the scale 2^-127 it is zeros in float16
+#pragma unroll
+                for (int t = 0; t < 8; ++t) held[t] = slot + (t < 4 ? 4 * g + t : 12 + 4 * g + t) < (t < 4 ? lim0 : lim1) ? held[t] : 0u;
+            }
+            constexpr int kBytes = D / 32;  // code bytes of a token in this lane
+#pragma unroll
+            for (int y = 0; y < kBytes; ++y) {
+                uint32_t w[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    const float sc = __uint_as_float(held[t]);
+                    const uint32_t x = raw[half].v[t][0];
+                    w[t] = y == 0 ? two_h16<0>(x, sc) : y == 1 ? two_h16<1>(x, sc) : y == 2 ? two_h16<2>(x, sc) : two_h16<3>(x, sc);
+                }
+                u32x4 lo, hi;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    lo[t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x05040100u);
+                    hi[t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x07060302u);
+                }
+#pragma unroll
+                for (int t = 0; t < 2 * RT; ++t) {
+#pragma unroll
+                    for (int term = DT == PSC_F32 ? 1 : 0; term >= 0; --term) {
+                        const h16x8 pr = __builtin_bit_cast(h16x8, (u32x4){p[t][term][0], p[t][term][1], p[t][term][2], p[t][term][3]});
+                        f32x4 &a = acc[t][half * (D / 16) + 2 * y], &b = acc[t][half * (D / 16) + 2 * y + 1];
+                        a = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, lo), pr, a, 0, 0, 0);
+                        b = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, hi), pr, b, 0, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+};
+
+// Waves of a SIMD that the registers are to leave room for.
+template <int D, int DT, int RT>
+constexpr int difference_waves()
+{
+    return D == 64 && DT != PSC_F32 && RT == 1 ? 2 : 1;
+}
+
+// From a row's sums over both maps, D / 16 coordinates of both value halves to each of 16 lanes that stand in a row: the output.
+template <int D, int DT>
+__device__ __forceinline__ void finish_row(const KvQueries &q, const KvDifference &d, int row, int out_head, int run, const float (&x)[2][2][D / 16], const float (&inv)[2])
+{
+    const float lam = d.lam[(int64_t)row * d.lam_stride + out_head];
+    float o[2][D / 16], squares = 0.f;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            o[half][j] = x[0][half][j] * inv[0] - lam * (x[1][half][j] * inv[1]);
+            squares += o[half][j] * o[half][j];
+        }
+    float scale = d.factor;
+    if (d.norm) {
+#pragma unroll
+        for (int k = 1; k < 16; k *= 2) squares += __shfl_xor(squares, k);
+        scale *= 1.f / sqrtf(squares * (1.f / (2 * D)) + d.eps);
+    }
+    typename Element<DT>::type *out = (typename Element<DT>::type *)q.out + ((int64_t)row * (q.q_heads / 2) + out_head) * (2 * D);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int at = half * D + run * (D / 16);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) o[half][j] *= d.norm ? d.norm[at + j] * scale : scale;
+        store_row<DT, D / 16>(out + at, o[half]);
+    }
+}
+
+// The output of rows from .. to - 1, NaN: no sequence has them.
+template <int D, int DT>
+__device__ void difference_of_nobody(const KvQueries &q, int pair, int from, int to)
+{
+    for (int64_t x = (int64_t)max(from, 0) * q.group + (threadIdx.x >> 4); x < (int64_t)min(to, q.nrows) * q.group; x += blockDim.x >> 4) {
+        const int64_t row = x / q.group;
+        const int in_group = (int)(x % q.group), run = (int)threadIdx.x & 15;
+        float nan[D / 16];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) nan[j] = __builtin_nanf("");
+        typename Element<DT>::type *out = (typename Element<DT>::type *)q.out + (row * (q.q_heads / 2) + pair * q.group + in_group) * (2 * D) + run * (D / 16);
+        store_row<DT, D / 16>(out, nan);
+        store_row<DT, D / 16>(out + D, nan);
+        if (run < 2 && q.lse) q.lse[row * q.q_heads + (2 * pair + run) * q.group + in_group] = nan[0];
+    }
+}
+
+template <int D, int RT>
+struct JoinedPair {  // of a workgroup's four waves
+    static constexpr int kStride = 2 * D + 4;
+    float acc[4][16 * kStride];
+    float tops[4][32 * RT], sums[4][32 * RT];
+};
+
+// Blocks begin .. end - 1 of the rows from m0 on of (b, pair): the workgroup's four waves take every fourth each and are joined in LDS.
+// part < 0: these are all blocks, and the result is final.
+template <int D, int DT, int RT, bool kPos>
+__device__ __forceinline__ void attend_pair(const KvView &c, const KvQueries &q, const KvDifference &d, const RowSet &s, int b, int pair, int m0, const Blocks &blocks,
+                                            int begin, int end, int64_t part, JoinedPair<D, RT> &joined)
+{
+    const int lane = lane_id(), i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int m_all = s.rows * q.group, m_end = min(m0 + 16 * RT, m_all);
+    const int lo_pos = s.first_pos + m0 / q.group, hi_pos = s.first_pos + (m_end - 1) / q.group;
+    constexpr int step = 4;
+
+    Difference<D, DT, RT, kPos> a;
+    RowMask mask[RT];
+    const auto start = [&] {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int m = min(m0 + t * 16 + i, m_all - 1), place = m / q.group;  // (rows past the last: the last one again)
+            mask[t] = row_mask(q, s.first_pos + place);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int n = w * RT + t;
+                load_rows<D, DT>(q, s.first_row + place, (2 * pair + w) * q.group + m - place * q.group, g, a.rows[n]);
+                a.top[n] = kNegInf;
+                a.sum[n] = 0.f;
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) a.acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+    };
+    start();
+    const int64_t slots = (int64_t)c.width << c.page_shift, dense = ((int64_t)b * c.heads + 2 * pair) * slots;
+    const int next_head = 1 << (c.page_shift - 4);  // sixteens from a head's slots to the next head's
+
+    // The places of 32 of the wave's blocks are held across the lanes; the codes of the block after the one that is worked on
+    // are on their way, without a branch around their loads (past the last block: of a page that is there).
+    const int own = begin + wave, mine = end > own ? (end - own + step - 1) / step : 0;
+    auto pages_from = [&](int k) {
+        return sixteen_of(c, b, 2 * pair, s.n, blocks.block(min(own + (k + (lane >> 1)) * step, end - 1)) * 32 + (lane & 1) * 16);
+    };
+    auto load = [&](const int (&pg)[2], Raw<D> (&r)[2]) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = max(pg[h], 0) + w * next_head;
+                load_keys<D>(c, at, i, g, r[w].k[h], r[w].ks[h]);
+                load_values<D>(c, at, i, g, &r[w].v[4 * h], r[w].vs[h]);
+            }
+    };
+    auto load_positions = [&](int k, int (&pos)[8]) {
+        if constexpr (kPos) {
+            const int sl = blocks.block(min(own + k * step, end - 1)) * 32;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int4 x = *(const int4 *)(q.positions + dense + min(sl + 16 * h, (c.width << c.page_shift) - 16) + 4 * g);
+                pos[4 * h] = x.x;
+                pos[4 * h + 1] = x.y;
+                pos[4 * h + 2] = x.z;
+                pos[4 * h + 3] = x.w;
+            }
+        }
+    };
+    // where the scores of the lane's row are left for kv_weights_of_scores_kernel
+    float *scores = nullptr;
+    if constexpr (RT == 1)
+        if (q.scores && i < m_all) scores = q.scores + (((int64_t)b * c.heads + 2 * pair) * q.scores_rows + i) * slots;
+    const auto work = [&](auto far, int k, const Raw<D> (&raw)[2], const int (&pos)[8], const int (&pg)[2]) {
+        const int slot = blocks.block(own + k * step) * 32;
+        const bool there = slot + 32 <= s.n && pg[0] >= 0 && pg[1] >= 0 && !kPos;
+        const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
+                           (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
+        a.template block<far.value>(q, raw, pos, mask, slot, pg[0] >= 0 ? s.n : 0, pg[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores, q.scores_rows * slots);
+    };
+    if (mine > 0) {
+        Raw<D> raw[2][2];
+        int ids = pages_from(0), pages[2][2] = {{__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)}, {-1, -1}};
+        load(pages[0], raw[0]);
+        for (int k0 = 0; k0 < mine; k0 += 32) {
+            const int ids_then = pages_from(k0 + 32), k_end = min(32, mine - k0);
+            const auto turn = [&](int k, const Raw<D> (&now)[2], const int (&now_pages)[2], Raw<D> (&next)[2], int (&next_pages)[2]) {
+                if (k < 31) {
+                    next_pages[0] = __builtin_amdgcn_readlane(ids, 2 * k + 2);
+                    next_pages[1] = __builtin_amdgcn_readlane(ids, 2 * k + 3);
+                } else {
+                    next_pages[0] = __builtin_amdgcn_readlane(ids_then, 0);
+                    next_pages[1] = __builtin_amdgcn_readlane(ids_then, 1);
+                }
+                int pos[8];
+                load_positions(k0 + k, pos);
+                load(next_pages, next);
+                work(std::false_type(), k0 + k, now, pos, now_pages);
+            };
+            for (int k = 0; k < k_end; k += 2) {  // (32 is even: a set's turn does not change from one 32 to the next)
+                turn(k, raw[0], pages[0], raw[1], pages[1]);
+                if (k + 1 < k_end) turn(k + 1, raw[1], pages[1], raw[0], pages[0]);
+            }
+            ids = ids_then;
+        }
+    }
+    // Decided at the end, and all done again, as in kv_attention_kernel.
+    bool far = false;
+#pragma unroll
+    for (int t = 0; t < 2 * RT; ++t) far = far || is_coarse(a.top[t]);
+    if (__any(far)) {
+        asm volatile("" ::: "memory");  // (the rows are read again: kept, they would cost the pass above registers)
+        start();
+#pragma unroll 1
+        for (int k = 0; k < mine; ++k) {
+            const int ids = pages_from(k), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
+            int pos[8];
+            load_positions(k, pos);
+            Raw<D> raw[2];
+            load(pages, raw);
+            work(std::true_type(), k, raw, pos, pages);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 2 * RT; ++t) a.sum[t] = column_sum(a.sum[t]);
+    if (g == 0) {
+#pragma unroll
+        for (int t = 0; t < 2 * RT; ++t) {
+            joined.tops[wave][t * 16 + i] = a.top[t];
+            joined.sums[wave][t * 16 + i] = a.sum[t];
+        }
+    }
+    __syncthreads();
+    const int local = (int)threadIdx.x >> 4, run = (int)threadIdx.x & 15;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int m = m0 + t * 16 + local;
+        float x[2][2][D / 16], inv[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int n = w * RT + t;
+            float top = kNegInf;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, joined.tops[k][n * 16 + i]);
+            const float shrink = top == kNegInf ? 1.f : exp2_fast(a.top[n] - top);
+            if (t > 0 || w > 0) __syncthreads();
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float y[D / 16];
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) y[j] = a.acc[n][half * (D / 16) + j][r] * shrink;
+                    store_row<PSC_F32, D / 16>(&joined.acc[wave][i * joined.kStride + half * D + (g * 4 + r) * (D / 16)], y);
+                }
+            __syncthreads();
+            float best = kNegInf, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) best = fmaxf(best, joined.tops[k][n * 16 + local]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum += joined.sums[k][n * 16 + local] * (best == kNegInf ? 1.f : exp2_fast(joined.tops[k][n * 16 + local] - best));
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    x[w][half][j] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[w][half][j] += joined.acc[k][local * joined.kStride + half * D + run * (D / 16) + j];
+                }
+            inv[w] = sum == 0.f ? 0.f : 1.f / sum;
+            if (m >= m_all) continue;
+            if (part >= 0) {
+                const int64_t at = (part * 2 + w) * (16 * RT) + t * 16 + local;
+                if (run == 0) *(float2 *)(q.part_stat + at * 2) = make_float2(best, sum);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) store_row<PSC_F32, D / 16>(q.part_acc + at * (2 * D) + half * D + run * (D / 16), x[w][half]);
+            } else if (run == 0) {
+                const int64_t row = (int64_t)(s.first_row + m / q.group) * q.q_heads + (2 * pair + w) * q.group + m % q.group;
+                if (q.lse) q.lse[row] = sum == 0.f ? kNegInf : log_sum(best, sum);
+                if (q.stat) *(float2 *)(q.stat + row * 2) = make_float2(best == kNegInf ? 0.f : best, inv[w]);
+            }
+        }
+        if (part < 0 && m < m_all) finish_row<D, DT>(q, d, s.first_row + m / q.group, pair * q.group + m % q.group, run, x, inv);
+    }
+}
+
+template <int D, int DT, int RT, bool kPos, bool kParts>
+__global__ __launch_bounds__(256, (difference_waves<D, DT, RT>())) void kv_difference_kernel(KvView c, KvQueries q, KvDifference d)
+{
+    __shared__ JoinedPair<D, RT> joined;
+    const int pairs = c.heads / 2;
+    if constexpr (!kParts) {
+        const int b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, m0 = (int)blockIdx.x * 16 * RT;
+        const RowSet s = rows_of(c, q, b);
+        if (q.offsets && m0 == 0) {
+            if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
+            difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
+        }
+        if (m0 >= s.rows * q.group) return;
+        const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
+        attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, 0, blocks.count(), -1, joined);
+    } else {
+        Parts all(c, q);
+        if (blockIdx.x >= all.total) return;
+        uint32_t first;
+        const int b = all.find(c, q, blockIdx.x, &first);
+        const RowSet s = rows_of(c, q, b);
+        const uint32_t each = Parts::blocks_of_unit(q, s), parts = all.parts_of_unit(each);
+        const uint32_t unit = (blockIdx.x - first) / parts, part = blockIdx.x - first - unit * parts;
+        const int pair = (int)unit % pairs, m0 = (int)unit / pairs * 16 * RT;
+        const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
+        const int count = blocks.count(), from = (int)((uint64_t)part * each / parts), to = (int)((uint64_t)(part + 1) * each / parts);
+        attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, min(count, from), min(count, to), parts == 1 ? -1 : (int64_t)blockIdx.x, joined);
+    }
+}
+
+// Joins the parts of an output head's two maps, a wave to a (row, output head): each lane takes a part's maximum and sum (64 parts at a
+// time), then the lanes take D / 16 coordinates of both halves of every fourth part each.  Sequences without a block have no part:
+// zeros.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQueries q, KvDifference d)
+{
+    const int lane = lane_id(), run = lane & 15, quarter = lane >> 4, out_heads = q.q_heads / 2;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (item >= (int64_t)q.nrows * out_heads) return;
+    const int r = (int)(item / out_heads), out_head = (int)(item % out_heads), pair = out_head / q.group, in_group = out_head % q.group;
+    const int b = __builtin_amdgcn_readfirstlane(sequence_of_row(q.offsets, c.batch, q.each, r));
+    const RowSet s = rows_of(c, q, b);
+    const int place = r - s.first_row;
+    const int64_t row0 = (int64_t)r * q.q_heads + 2 * pair * q.group + in_group;  // of the first map; the second: q.group further
+    if (place < 0 || place >= s.rows) {  // nobody's
+        float nan[D / 16];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) nan[j] = __builtin_nanf("");
+        if (quarter < 2) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + item * (2 * D) + quarter * D + run * (D / 16), nan);
+        if (lane < 2 && q.lse) q.lse[row0 + lane * q.group] = nan[0];
+        return;
+    }
+    const int m = place * q.group + in_group, in_unit = m % q.unit_rows;
+    const uint32_t unit = (uint32_t)(m / q.unit_rows * q.unit_heads + pair);
+    Parts all(c, q);
+    const int parts = (int)all.parts_of_unit(Parts::blocks_of_unit(q, s));
+    if (parts == 1) return;  // (final already)
+    const int64_t begin = (int64_t)all.first_of(c, q, b) + (int64_t)unit * parts;
+    float x[2][2][D / 16], inv[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const int64_t at = (begin * 2 + w) * q.unit_rows + in_unit;  // and every 2 unit_rows further
+        float top = kNegInf, sum = 0.f;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) x[w][half][j] = 0.f;
+        for (int p0 = 0; p0 < parts; p0 += 64) {
+            float2 st = make_float2(kNegInf, 0.f);
+            if (p0 + lane < parts) st = *(const float2 *)(q.part_stat + (at + (int64_t)(p0 + lane) * 2 * q.unit_rows) * 2);
+            float now = top;
+            if (st.y != 0.f) now = fmaxf(now, st.x);
+#pragma unroll
+            for (int k = 1; k < 64; k *= 2) now = fmaxf(now, __shfl_xor(now, k));
+            const float shrink = now == kNegInf ? 1.f : exp2_fast(top - now);
+            const float theirs = st.y == 0.f ? 0.f : now == kNegInf ? 1.f : exp2_fast(st.x - now);
+            float add = st.y * theirs;  // (a part that saw nothing: 0)
+#pragma unroll
+            for (int k = 1; k < 64; k *= 2) add += __shfl_xor(add, k);
+            sum = __builtin_fmaf(sum, shrink, add);
+            top = now;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) x[w][half][j] *= shrink;
+            const int last = min(64, parts - p0);
+            for (int k = 0; k < last; k += 4) {  // (all lanes to the end: a lane's weight is asked of another one)
+                const int p = k + quarter;
+                const float weight = __shfl(theirs, p);  // past the last: 0
+                const float *from = q.part_acc + (at + (int64_t)(p0 + min(p, last - 1)) * 2 * q.unit_rows) * (2 * D) + run * (D / 16);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float y[D / 16];
+                    load_row<PSC_F32, D / 16>(from + half * D, y);
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) x[w][half][j] = __builtin_fmaf(y[j], weight, x[w][half][j]);
+                }
+            }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) x[w][half][j] = column_sum(x[w][half][j]);
+        inv[w] = sum == 0.f ? 0.f : 1.f / sum;
+        if (lane == 0) {
+            if (q.lse) q.lse[row0 + w * q.group] = sum == 0.f ? kNegInf : log_sum(top, sum);
+            if (q.stat) *(float2 *)(q.stat + (row0 + w * q.group) * 2) = make_float2(top == kNegInf ? 0.f : top, inv[w]);
+        }
+    }
+    if (quarter == 0) finish_row<D, DT>(q, d, r, out_head, run, x, inv);
+}
+
+// Blocks of a part at least, and blocks of a memory up to which a unit stays whole (a block is 32 tokens of both heads).
+constexpr int64_t kLeastBlocks = 8, kFewBlocks = 32;
+
+// Rows of a wave, in sixteens, at most.
+constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || dim == 128 ? 1 : 2; }
+
+template <int DT, int D>
+int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, const KvPlan &p, const float *given, float *received, hipStream_t s)
+{
+    constexpr int kMost = most_row_tiles(DT, D);
+    if (q.nrows > 0) {
+        const uint32_t groups = (uint32_t)(c.batch * (c.heads / 2));
+        const auto launch = [&](auto rt, auto pos) {
+            if (p.workgroups) kv_difference_kernel<D, DT, rt.value, pos.value, true><<<(uint32_t)p.most_parts, 256, 0, s>>>(c, q, d);
+            else kv_difference_kernel<D, DT, rt.value, pos.value, false><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, d);
+        };
+        const auto launch_rows = [&](auto pos) {
+            if (p.row_tiles == 1) launch(std::integral_constant<int, 1>(), pos);
+            else launch(std::integral_constant<int, kMost>(), pos);
+        };
+        if (q.positions) launch_rows(std::true_type());
+        else launch_rows(std::false_type());
+        PSC_HIP_TRY(hipGetLastError());
+        if (p.workgroups) {
+            kv_difference_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * (q.q_heads / 2) + 3) / 4), 256, 0, s>>>(c, q, d);
+            PSC_HIP_TRY(hipGetLastError());
+        }
+    }
+    if (received) return run_weights<DT, D, 2>(c, q, p, given, received, s);
+    return PSC_OK;
+}
+
+}  // namespace
+
+KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered, bool weights)
+{
+    KvPlan p;
+    const int64_t m = (int64_t)max_rows * group, slots = (int64_t)c.width << c.page_shift, pairs = c.heads / 2;
+    p.row_tiles = m <= 16 ? 1 : most_row_tiles(dtype, c.dim);
+    p.row_groups = (m + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
+    // blocks of 32 tokens that a group of rows can see at most
+    int64_t blocks = (slots + 31) / 32;
+    if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
+    const int64_t units = p.row_groups * c.batch * pairs;
+    const int waves = c.dim == 64 && dtype != PSC_F32 && p.row_tiles == 1 ? 2 : 1;  // workgroups to a compute unit: difference_waves
+    if (units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31) p.workgroups = 256 * waves;
+    if (p.workgroups) {
+        // at most one part more to a unit than `wanted` of Parts, which is half of the workgroups or more
+        p.most_parts = std::min(p.workgroups + units, units * ((blocks + kLeastBlocks - 1) / kLeastBlocks));
+        p.part_stat_bytes = (size_t)(p.most_parts * 32 * p.row_tiles * 8 + 255) / 256 * 256;
+        p.part_acc_bytes = (size_t)(p.most_parts * 32 * p.row_tiles * 2 * c.dim * 4 + 255) / 256 * 256;
+    }
+    p.least_blocks = kLeastBlocks;
+    if (weights) plan_weights(c, m, nrows * group * c.heads, &p);
+    return p;
+}
+
+int launch_kv_difference(const KvView &c, int dtype, const KvQueries &q, const KvDifference &d, const KvPlan &p, const float *given, float *received, hipStream_t s)
+{
+    return c.dim == 64 ? (dtype == PSC_BF16  ? run_difference<PSC_BF16, 64>(c, q, d, p, given, received, s)
+                          : dtype == PSC_F16 ? run_difference<PSC_F16, 64>(c, q, d, p, given, received, s)
+                                             : run_difference<PSC_F32, 64>(c, q, d, p, given, received, s))
+                       : (dtype == PSC_BF16  ? run_difference<PSC_BF16, 128>(c, q, d, p, given, received, s)
+                          : dtype == PSC_F16 ? run_difference<PSC_F16, 128>(c, q, d, p, given, received, s)
+                                             : run_difference<PSC_F32, 128>(c, q, d, p, given, received, s));
+}
+
+}  // namespace psc

@@ -1,0 +1,264 @@
+// Rotary positions: pairs (a, b) of a head's first `dims` coordinates turned by an angle that grows with the row's position,
+//   a' = f (a cos t - b sin t)   b' = f (b cos t + a sin t)   t = position * frequency of the pair
+// alone (the transposed, which is the gradient, turns by -t), and for keys on their way into the memory in 4 bits.
+//
+// Angles.  A frequency is held as the share of a turn that a position adds, in 64 bits: position * frequency modulo 2^64 is then
+// the angle without its whole turns, exactly, in one integer product, however far the position.  What is left of a
+// quarter turn after the nearest quarters are taken off goes into Taylor's series in 64 bits (|t| <= pi/4: sine to t^15, off by
+// 5e-17, cosine to t^16, off by 2e-18).  64-bit operations issue at the rate of single 32-bit ones here, and a thread uses its sines and
+// cosines for several heads.
+#include "kv_device.h"
+
+namespace psc {
+namespace {
+
+__device__ __forceinline__ void sincos_of_turns(uint64_t turns, double *sine, double *cosine)
+{
+    const uint64_t quarters = ((turns >> 61) + 1) >> 1;
+    const double t = (double)(int64_t)(turns - (quarters << 62)) * (0x1.921fb54442d18p+2 * 0x1p-64), tt = t * t;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = __builtin_fma(s, tt, 1.0 / 6227020800.0);
+    s = __builtin_fma(s, tt, -1.0 / 39916800.0);
+    s = __builtin_fma(s, tt, 1.0 / 362880.0);
+    s = __builtin_fma(s, tt, -1.0 / 5040.0);
+    s = __builtin_fma(s, tt, 1.0 / 120.0);
+    s = __builtin_fma(s, tt, -1.0 / 6.0);
+    s = __builtin_fma(s * tt, t, t);
+    c = __builtin_fma(c, tt, -1.0 / 87178291200.0);
+    c = __builtin_fma(c, tt, 1.0 / 479001600.0);
+    c = __builtin_fma(c, tt, -1.0 / 3628800.0);
+    c = __builtin_fma(c, tt, 1.0 / 40320.0);
+    c = __builtin_fma(c, tt, -1.0 / 720.0);
+    c = __builtin_fma(c, tt, 1.0 / 24.0);
+    c = __builtin_fma(c, tt, -0.5);
+    c = __builtin_fma(c, tt, 1.0);
+    const double s0 = quarters & 1 ? c : s, c0 = quarters & 1 ? s : c;
+    *sine = quarters & 2 ? -s0 : s0;
+    *cosine = (quarters + 1) & 2 ? -c0 : c0;
+}
+
+// Sine and cosine of a pair times the factor (the rows that nobody has: as they are).
+__device__ __forceinline__ void turn_of(const Rotary &t, int pair, int64_t position, bool nobodys, double *sine, double *cosine)
+{
+    sincos_of_turns((uint64_t)position * t.turns[pair], sine, cosine);
+    *sine = nobodys ? 0.0 : *sine * t.factor;
+    *cosine = nobodys ? 1.0 : *cosine * t.factor;
+}
+
+// ------------------------------------------------------------------------------------------- rows on their own
+// A thread takes 8 pairs (or 16 coordinates behind the turned ones, which are copied) of a row, in every head of a group.
+template <int DT, bool kInterleaved>
+__global__ __launch_bounds__(256) void rotary_kernel(Rotary t, RotaryRows r)
+{
+    typedef typename Element<DT>::type T;
+    const int turned = t.dims / 16, chunks = turned + (r.head_dim - t.dims + 15) / 16;
+    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int chunk = (int)(item % chunks);
+    const int64_t rest = item / chunks;
+    const int row = (int)(rest % r.nrows), group = (int)(rest / r.nrows), from = group * r.group, to = min(from + r.group, r.heads);
+    if (from >= r.heads) return;
+    const T *x = (const T *)r.x + row * r.row_stride;
+    T *y = (T *)r.out + row * r.out_row_stride;
+    if (chunk >= turned) {
+        const int at = t.dims + (chunk - turned) * 16;
+        const bool second = at + 8 < r.head_dim;
+        for (int h = from; h < to; ++h) {
+            float a[8], b[8];
+            load_row<DT, 8>(x + h * r.head_stride + at, a);
+            if (second) load_row<DT, 8>(x + h * r.head_stride + at + 8, b);
+            store_row<DT, 8>(y + h * r.out_head_stride + at, a);
+            if (second) store_row<DT, 8>(y + h * r.out_head_stride + at + 8, b);
+        }
+        return;
+    }
+    bool nobodys;
+    const int64_t position = r.position_of(row, &nobodys);
+    float s[8], c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        double sine, cosine;
+        turn_of(t, chunk * 8 + i, position, nobodys, &sine, &cosine);
+        s[i] = r.transposed ? -(float)sine : (float)sine;
+        c[i] = (float)cosine;
+    }
+    const int at0 = kInterleaved ? chunk * 16 : chunk * 8, at1 = kInterleaved ? at0 + 8 : at0 + t.dims / 2;
+#pragma unroll 4
+    for (int h = from; h < to; ++h) {
+        float u[8], v[8], p[8], q[8];
+        load_row<DT, 8>(x + h * r.head_stride + at0, u);
+        load_row<DT, 8>(x + h * r.head_stride + at1, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (kInterleaved) {
+                const float a = i < 4 ? u[2 * i] : v[2 * i - 8], b = i < 4 ? u[2 * i + 1] : v[2 * i - 7];
+                (i < 4 ? p[2 * i] : q[2 * i - 8]) = a * c[i] - b * s[i];
+                (i < 4 ? p[2 * i + 1] : q[2 * i - 7]) = b * c[i] + a * s[i];
+            } else {
+                p[i] = u[i] * c[i] - v[i] * s[i];
+                q[i] = v[i] * c[i] + u[i] * s[i];
+            }
+        }
+        store_row<DT, 8>(y + h * r.out_head_stride + at0, p);
+        store_row<DT, 8>(y + h * r.out_head_stride + at1, q);
+    }
+}
+
+// Any number of dimensions, strides and alignment: a thread takes a pair, or a coordinate that is copied.
+template <int DT>
+__global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows r)
+{
+    typedef typename Element<DT>::type T;
+    const int half = t.dims / 2, places = half + r.head_dim - t.dims;
+    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int place = (int)(item % places);
+    const int64_t rest = item / places;
+    const int row = (int)(rest % r.nrows), group = (int)(rest / r.nrows), from = group * r.group, to = min(from + r.group, r.heads);
+    if (from >= r.heads) return;
+    const T *x = (const T *)r.x + row * r.row_stride;
+    T *y = (T *)r.out + row * r.out_row_stride;
+    if (place >= half) {
+        const int at = half + place;
+        for (int h = from; h < to; ++h) y[h * r.out_head_stride + at] = x[h * r.head_stride + at];
+        return;
+    }
+    bool nobodys;
+    const int64_t position = r.position_of(row, &nobodys);
+    double sine, cosine;
+    turn_of(t, place, position, nobodys, &sine, &cosine);
+    const float s = r.transposed ? -(float)sine : (float)sine, c = (float)cosine;
+    const int at0 = t.interleaved ? 2 * place : place, at1 = t.interleaved ? at0 + 1 : at0 + half;
+#pragma unroll 4
+    for (int h = from; h < to; ++h) {
+        const float a = Element<DT>::load(x[h * r.head_stride + at0]), b = Element<DT>::load(x[h * r.head_stride + at1]);
+        y[h * r.out_head_stride + at0] = Element<DT>::store(a * c - b * s);
+        y[h * r.out_head_stride + at1] = Element<DT>::store(b * c + a * s);
+    }
+}
+
+// ------------------------------------------------------------------------------------------- into the memory
+// D / 8 lanes to a row, 8 coordinates to a lane, in every head of a group of the kv heads (whose keys are turned, rounded and written
+// with their values) and the query heads behind them.  A key's products are made in 64 bits and rounded to 32, then to 4: a
+// coordinate next to a border between two codes comes out on the same side as in any other exact computation.
+template <int DT, int D, bool kInterleaved>
+__global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows r, Rotary t, RotaryQueries q)
+{
+    constexpr int L = D / 8;
+    typedef typename Element<DT>::type T;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int part = (int)(threadIdx.x % L);
+    const int row = (int)(item % r.nrows), group = (int)(item / r.nrows), from = group * q.group, to = min(from + q.group, c.heads + q.heads);
+    if (from >= to) return;
+    const RowPlace p = place_of(c, r, row);
+    const bool nobodys = p.place < 0 || (r.offsets && row >= r.offsets[c.batch]);
+    const int64_t position = (int64_t)(r.first ? r.first[p.b] : c.lengths[p.b]) + p.place;
+    // the lane's pairs; of pairs half of `dims` apart it has one side, and reads the other side too
+    constexpr int kPairs = kInterleaved ? 4 : 8;
+    const int at = part * 8, half = t.dims / 2;
+    const bool turned = at < t.dims, second = !kInterleaved && at >= half;
+    const int other = kInterleaved || !turned ? at : second ? at - half : at + half;
+    double s[kPairs], co[kPairs];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        s[i] = 0.0;
+        co[i] = 1.0;
+    }
+    if (turned) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            turn_of(t, kInterleaved ? part * 4 + i : second ? other + i : at + i, position, nobodys, &s[i], &co[i]);
+            if (!kInterleaved && !second) s[i] = -s[i];  // (then x cos + other sin on both sides)
+        }
+    }
+    for (int h = from; h < to; ++h) {
+        if (h < c.heads) {
+            const T *k = (const T *)r.k + row * r.k_stride + h * r.k_head_stride;
+            float x[2][8];
+            load_row<DT, 8>(k + at, x[0]);
+            load_row<DT, 8>((const T *)r.v + row * r.v_stride + h * r.v_head_stride + at, x[1]);
+            if (turned) {
+                if constexpr (kInterleaved) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double a = x[0][2 * i], b = x[0][2 * i + 1];
+                        x[0][2 * i] = (float)__builtin_fma(a, co[i], -(b * s[i]));
+                        x[0][2 * i + 1] = (float)__builtin_fma(b, co[i], a * s[i]);
+                    }
+                } else {
+                    float o[8];
+                    load_row<DT, 8>(k + other, o);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[0][i] = (float)__builtin_fma((double)x[0][i], co[i], (double)o[i] * s[i]);
+                }
+            }
+            write_token<D>(c, r, p, h, part, x);
+        } else {
+            const T *from_q = (const T *)q.q + row * q.row_stride + (h - c.heads) * q.head_stride;
+            float x[8];
+            load_row<DT, 8>(from_q + at, x);
+            if (turned) {
+                if constexpr (kInterleaved) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float a = x[2 * i], b = x[2 * i + 1], sf = (float)s[i], cf = (float)co[i];
+                        x[2 * i] = a * cf - b * sf;
+                        x[2 * i + 1] = b * cf + a * sf;
+                    }
+                } else {
+                    float o[8];
+                    load_row<DT, 8>(from_q + other, o);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = x[i] * (float)co[i] + o[i] * (float)s[i];
+                }
+            }
+            store_row<DT, 8>((T *)q.out + ((int64_t)row * q.heads + h - c.heads) * D + at, x);
+        }
+    }
+}
+
+// Heads that a thread takes: so many that enough threads are left to fill the card, 8 at most.
+constexpr int64_t kThreads = (int64_t)256 * 2048;
+int heads_of_a_thread(int64_t threads_of_a_head, int heads)
+{
+    int group = 1;
+    while (group < 8 && group < heads && threads_of_a_head * heads / (2 * group) >= kThreads) group *= 2;
+    return group;
+}
+
+template <int DT>
+int run_rotary(const Rotary &t, RotaryRows r, bool wide, hipStream_t s)
+{
+    const int64_t places = wide ? t.dims / 16 + (r.head_dim - t.dims + 15) / 16 : t.dims / 2 + r.head_dim - t.dims;
+    r.group = heads_of_a_thread(places * r.nrows, r.heads);
+    const int64_t blocks = (places * r.nrows * ((r.heads + r.group - 1) / r.group) + 255) / 256;
+    if (!wide) rotary_single_kernel<DT><<<(uint32_t)blocks, 256, 0, s>>>(t, r);
+    else if (t.interleaved) rotary_kernel<DT, true><<<(uint32_t)blocks, 256, 0, s>>>(t, r);
+    else rotary_kernel<DT, false><<<(uint32_t)blocks, 256, 0, s>>>(t, r);
+    PSC_HIP_TRY(hipGetLastError());
+    return PSC_OK;
+}
+
+template <int DT, int D>
+int run_append_rotary(const KvView &c, const KvRows &r, const Rotary &t, RotaryQueries q, hipStream_t s)
+{
+    const int heads = c.heads + q.heads;
+    q.group = heads_of_a_thread((int64_t)r.nrows * (D / 8), heads);
+    const int64_t blocks = ((int64_t)r.nrows * ((heads + q.group - 1) / q.group) * (D / 8) + 255) / 256;
+    if (t.interleaved) kv_append_rotary_kernel<DT, D, true><<<(uint32_t)blocks, 256, 0, s>>>(c, r, t, q);
+    else kv_append_rotary_kernel<DT, D, false><<<(uint32_t)blocks, 256, 0, s>>>(c, r, t, q);
+    PSC_HIP_TRY(hipGetLastError());
+    return PSC_OK;
+}
+
+}  // namespace
+
+int launch_rotary(const Rotary &t, int dtype, const RotaryRows &r, bool wide, hipStream_t s)
+{
+    return dtype == PSC_BF16 ? run_rotary<PSC_BF16>(t, r, wide, s) : dtype == PSC_F16 ? run_rotary<PSC_F16>(t, r, wide, s) : run_rotary<PSC_F32>(t, r, wide, s);
+}
+
+int launch_kv_append_rotary(const KvView &c, int dtype, const KvRows &r, const Rotary &t, const RotaryQueries &q, hipStream_t s)
+{
+    return PSC_KV_DISPATCH(run_append_rotary, dtype, c.dim, c, r, t, q, s);
+}
+
+}  // namespace psc

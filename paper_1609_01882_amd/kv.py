@@ -69,11 +69,11 @@ def _ints(**values):
 
 
 @functools.lru_cache(maxsize=1024)
-def _attention_workspace(pages, kv_heads, head_dim, page, batch, width, dtype, rows, max_rows, q_heads, window, sinks, *has):
+def _attention_workspace(call, pages, kv_heads, head_dim, page, batch, width, dtype, rows, max_rows, q_heads, window, sinks, *has):
     sizes = dict(rows=rows, max_rows=max_rows, q_heads=q_heads, window=window, sinks=sinks)
     _ints(batch=batch, width=width, **sizes)
     sizes = dtype, *sizes.values(), *has
-    return _load().psc_kv_attention_workspace_bytes(_pack(0, 0, 0, 0, pages, kv_heads, head_dim, page, 0, batch, width, 0), *sizes)
+    return getattr(_load(), call + "_workspace_bytes")(_pack(0, 0, 0, 0, pages, kv_heads, head_dim, page, 0, batch, width, 0), *sizes)
 
 
 class KvCache:
@@ -119,19 +119,51 @@ class KvCache:
             raise PscError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
         return _stream_address(self._index)
 
-    def append(self, k, v, table, lengths, offsets=None, first=None, positions=None, weights=None):
+    def append(self, k, v, table, lengths, offsets=None, first=None, positions=None, weights=None, rotary=None, q=None, q_out=None):
         """Round the rows k, v [n, kv_heads, head_dim] to 4 bits and write them to slots lengths[b], lengths[b] + 1, ...
         `lengths` stays as it is.  `positions`, per slot (int32), receives first[b], first[b] + 1, ... (`first` None: the
-        slots); `weights`, per slot (float32), receives 0."""
+        slots); `weights`, per slot (float32), receives 0.
+        `rotary` (a `Rotary`, of a multiple of 16 dimensions): keys are turned first, row r of a sequence by the angles of first[b] + r, and so
+        are the queries q [n, q_heads, head_dim] of the same rows, which are returned (in `q_out`, another tensor than q).
+        Nothing flows back: tensors that want a gradient are refused then."""
         c, batch, slots = self._args(table, lengths)
         n = k.shape[0]
         if v.dtype != k.dtype or v.shape != k.shape:
             raise PscError("k and v differ in type or shape")
+        if rotary is not None:
+            return self._append_rotary(c, batch, slots, k, v, offsets, first, positions, weights, rotary, q, q_out)
+        if q is not None or q_out is not None:
+            raise PscError("q: is turned by a rotary, and there is none")
         _check(_load().psc_kv_append(c, _dtype(k, "k"), *self._rows(k, self.kv_heads, "k"), *self._rows(v, self.kv_heads, "v"), n,
                                      _array(offsets, torch.int32, (batch + 1,), "offsets", self._index),
                                      _array(first, torch.int32, (batch,), "first", self._index),
                                      _array(positions, torch.int32, slots, "positions", self._index),
                                      _array(weights, torch.float32, slots, "weights", self._index), self._stream()))
+
+    def _append_rotary(self, c, batch, slots, k, v, offsets, first, positions, weights, rotary, q, q_out):
+        n, heads, device = k.shape[0], 0, self._index
+        if rotary._index != device:
+            raise PscError(f"rotary: expected on {self.device}, got {rotary.device}")
+        if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (k, v, q, q_out)):
+            raise PscError("k, v, q: what goes into a memory in 4 bits has no gradient; detach, or call under torch.no_grad()")
+        rows, to = (None, 0, 0), None
+        if q is not None:
+            heads = q.shape[1] if q.dim() == 3 else 0
+            if q.dtype != k.dtype or q.shape[0] != n or heads < 1:
+                raise PscError(f"q: expected {k.dtype} [{n}, q_heads, {self.head_dim}], got {q.dtype} {list(q.shape)}")
+            rows = self._rows(q, heads, "q")
+            if q_out is None:
+                q_out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            to = _array(q_out, q.dtype, (n, heads, self.head_dim), "q_out", device)
+        elif q_out is not None:
+            raise PscError("q_out: without q")
+        _check(_load().psc_kv_append_rotary(c, C.byref(rotary._struct), _dtype(k, "k"), *self._rows(k, self.kv_heads, "k"),
+                                            *self._rows(v, self.kv_heads, "v"), *rows, heads, to, n,
+                                            _array(offsets, torch.int32, (batch + 1,), "offsets", device),
+                                            _array(first, torch.int32, (batch,), "first", device),
+                                            _array(positions, torch.int32, slots, "positions", device),
+                                            _array(weights, torch.float32, slots, "weights", device), self._stream()))
+        return q_out
 
     def read(self, table, starts, rows: int, offsets=None, dtype=torch.float32):
         """The held values of the slots starts[b], starts[b] + 1, ... (`rows` of them altogether): k, v [rows, kv_heads,
@@ -151,6 +183,41 @@ class KvCache:
         positions below `sinks`.  `scale` None: 1 / sqrt(head_dim).  `weights_out`, per slot (float32), receives
         `weights` (None: 0) plus the weight that each token was given; they may be the same tensor.  Nothing flows back:
         a `q` that wants a gradient is refused."""
+        return self._attend("psc_kv_attention", (self.head_dim, 1), None, q, table, lengths, offsets, max_rows, first, positions, scale, causal,
+                            window, sinks, weights, weights_out, out, workspace)
+
+    def attend_difference(self, q, lam, table, lengths, offsets=None, max_rows=None, first=None, positions=None, scale=None, causal=True, window=0,
+                          sinks=0, norm=None, eps=1e-6, factor=1.0, weights=None, weights_out=None, out=None, workspace=None):
+        """Differential attention of the rows q [n, q_heads, head_dim]: (out, lse), [n, q_heads / 2, 2 head_dim] and [n, q_heads].
+        kv heads 2j and 2j + 1 are a pair: a map of each one's keys, both over the two heads' values side by side.  With g
+        query heads to a kv head, output head j * g + i is softmax(q1 K1) V - lam softmax(q2 K2) V of the query heads
+        2j * g + i and (2j + 1) * g + i, with `norm` [2 head_dim] (float32) divided by the root of its mean square plus
+        `eps` and multiplied by `norm`; then by `factor`.  `lam` (float32): [q_heads / 2], or [n, q_heads / 2] for each row.
+        `positions` of a pair's heads are alike (the even one's are read); both receive both maps' weights.  head_dim is
+        64 or 128, kv_heads even.  All else as for `attend`; nothing flows back."""
+        heads = q.shape[1] if q.dim() == 3 else 0
+        if self.kv_heads % 2 or self.head_dim > 128 or heads < 1 or heads % self.kv_heads:
+            raise PscError(f"differential attention takes pairs of kv heads of 64 or 128 and a multiple of {self.kv_heads} query heads, got {heads} over "
+                           f"{self.kv_heads} x {self.head_dim}")
+        n = q.shape[0]
+        if lam.dim() == 1:
+            row = 0
+            at = _array(lam, torch.float32, (heads // 2,), "lam", self._index)
+        else:
+            row = lam.stride(0)
+            if lam.shape != (n, heads // 2) or lam.dtype != torch.float32 or lam.get_device() != self._index or (heads > 2 and lam.stride(1) != 1):
+                raise PscError(f"lam: expected float32 [{heads // 2}] or [{n}, {heads // 2}] on {self.device} with contiguous heads, got {lam.dtype} "
+                               f"{list(lam.shape)} with strides {list(lam.stride())} on {lam.device}")
+            at = lam.data_ptr()
+        if torch.is_grad_enabled() and (lam.requires_grad or (norm is not None and norm.requires_grad)):
+            raise PscError("lam, norm: attention over a memory in 4 bits has no gradient; detach them, or call under torch.no_grad()")
+        more = at, row, _array(norm, torch.float32, (2 * self.head_dim,), "norm", self._index), eps, factor
+        return self._attend("psc_kv_difference", (2 * self.head_dim, 2), more, q, table, lengths, offsets, max_rows, first, positions, scale, causal,
+                            window, sinks, weights, weights_out, out, workspace)
+
+    def _attend(self, call, shape, more, q, table, lengths, offsets, max_rows, first, positions, scale, causal, window, sinks, weights, weights_out,
+                out, workspace):
+        """`shape`: width of an output head, and how many query heads it takes; `more`: what the call takes behind the sinks."""
         c, batch, slots = self._args(table, lengths)
         n, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
         code, device = _dtype(q, "q"), self._index
@@ -162,36 +229,44 @@ class KvCache:
         _ints(max_rows=max_rows, window=window, sinks=sinks)
         if q.requires_grad and torch.is_grad_enabled():
             raise PscError("q: attention over a memory in 4 bits has no gradient; detach q, or call under torch.no_grad()")
+        outs = (n, heads // shape[1], shape[0])
         if out is None:
-            out = (torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device),
+            out = (torch.empty(outs, dtype=q.dtype, device=self.device),
                    torch.empty((n, heads), dtype=torch.float32, device=self.device))
         space = None, 0
         if workspace is not None:
             space = _bytes(workspace, device)
         else:
-            need = _attention_workspace(self.pages, self.kv_heads, self.head_dim, self.page, batch, table.shape[1], code, n, max_rows, heads,
+            need = _attention_workspace(call, self.pages, self.kv_heads, self.head_dim, self.page, batch, table.shape[1], code, n, max_rows, heads,
                                         window, sinks, positions is not None, weights_out is not None)
             if need:
                 workspace = _workspace(need, self.device)
                 space = workspace.data_ptr(), need
-        _check(_load().psc_kv_attention(c, code, *rows, n, max_rows, heads,
-                                    _array(offsets, torch.int32, (batch + 1,), "offsets", device),
-                                    _array(first, torch.int32, (batch,), "first", device),
-                                    _array(positions, torch.int32, slots, "positions", device),
-                                    1.0 / math.sqrt(self.head_dim) if scale is None else scale, int(causal), window, sinks,
-                                    _array(out[0], q.dtype, (n, heads, self.head_dim), "out", device),
-                                    _array(out[1], torch.float32, (n, heads), "lse", device),
-                                    _array(weights, torch.float32, slots, "weights", device),
-                                    _array(weights_out, torch.float32, slots, "weights_out", device),
-                                    *space, self._stream()))
+        _check(getattr(_load(), call)(c, code, *rows, n, max_rows, heads,
+                                      _array(offsets, torch.int32, (batch + 1,), "offsets", device),
+                                      _array(first, torch.int32, (batch,), "first", device),
+                                      _array(positions, torch.int32, slots, "positions", device),
+                                      1.0 / math.sqrt(self.head_dim) if scale is None else scale, int(causal), window, sinks,
+                                      *(more or ()),
+                                      _array(out[0], q.dtype, outs, "out", device),
+                                      _array(out[1], torch.float32, (n, heads), "lse", device),
+                                      _array(weights, torch.float32, slots, "weights", device),
+                                      _array(weights_out, torch.float32, slots, "weights_out", device),
+                                      *space, self._stream()))
         return out
 
     def attend_workspace_bytes(self, batch: int, width: int, rows: int, max_rows: int, q_heads: int, dtype, window: int = 0, sinks: int = 0,
                                positions: bool = False, weights: bool = False) -> int:
         """What `attend` needs for `rows` rows, at most `max_rows` of a sequence, over tables [batch, width]; `positions` and
         `weights`: whether there are positions and weights_out."""
-        return int(_attention_workspace(self.pages, self.kv_heads, self.head_dim, self.page, batch, width, _DTYPES[dtype], rows, max_rows,
-                                        q_heads, window, sinks, positions, weights))
+        return int(_attention_workspace("psc_kv_attention", self.pages, self.kv_heads, self.head_dim, self.page, batch, width, _DTYPES[dtype], rows,
+                                        max_rows, q_heads, window, sinks, positions, weights))
+
+    def attend_difference_workspace_bytes(self, batch: int, width: int, rows: int, max_rows: int, q_heads: int, dtype, window: int = 0,
+                                          sinks: int = 0, positions: bool = False, weights: bool = False) -> int:
+        """What `attend_difference` needs, as for `attend`."""
+        return int(_attention_workspace("psc_kv_difference", self.pages, self.kv_heads, self.head_dim, self.page, batch, width, _DTYPES[dtype], rows,
+                                        max_rows, q_heads, window, sinks, positions, weights))
 
     def evict_workspace_bytes(self, batch: int, width: int, budget: int) -> int:
         _ints(batch=batch, width=width, budget=budget)
