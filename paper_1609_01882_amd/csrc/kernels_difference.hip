@@ -11,6 +11,99 @@
 namespace psc {
 namespace {
 
+// Codes, scales and positions of a block of 32 tokens on their way through LDS: a wave has kStages places of its own, into which loads write
+// past the registers, so that the blocks after the one that is worked on are under way whatever the registers hold.  No other wave
+// reads them: no barrier, the wave counts its loads.  Each load moves 16 bytes (scales, positions: 4) of every lane to consecutive places; which
+// bytes a lane asks for is chosen so that what it reads back lies without conflicts over the banks:
+//   keys      in the order in which the lanes read them (coordinates g D/4 ... of token i, as for kv_device.h's load_keys)
+//   values    a row of D / 2 bytes to a token, the four tokens of g turned by g (D = 64: g / 2) places
+constexpr int kStages = 2;
+template <int D, bool kPos>
+struct Stage {
+    static constexpr int kCodes = 2048 * (D / 64), kScales = 128 * (D / 64);
+    static constexpr int kKeys = 0, kValues = kCodes, kKeyScales = 2 * kCodes, kValueScales = kKeyScales + kScales, kPositions = kValueScales + kScales;
+    static constexpr int kBytes = kPositions + (kPos ? 256 : 0), kLoads = (D == 64 ? 5 : 10) + (kPos ? 1 : 0);
+};
+
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t to)  // 16 bytes of every lane
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void load_word_to_lds(const void *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_for_loads()  // but for the last N
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_for_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// What a lane reads of a stage.
+template <int D, bool kPos>
+struct StageReader {
+    typedef Stage<D, kPos> S;
+    PSC_LDS const uint8_t *keys, *key_scales, *values, *value_scales, *positions;  // of the lane, in stage 0
+    int g;
+    __device__ StageReader(PSC_LDS const uint8_t *base, int i, int lane_g) : g(lane_g)
+    {
+        keys = base + S::kKeys + (D == 128 ? (g * 16 + i) * 16 : ((g >> 1) * 16 + i) * 16 + (g & 1) * 8);
+        key_scales = base + S::kKeyScales + (D == 128 ? i * 4 + g : i * 2 + (g >> 1));
+        values = base + S::kValues + 4 * g * (D / 2) + i * (D / 32);
+        value_scales = base + S::kValueScales + g * (D / 8);
+        positions = base + S::kPositions + 16 * g;
+    }
+    __device__ __forceinline__ void read_keys(int stage, int w, int h, uint32_t (&k)[D / 32], uint32_t &ks) const
+    {
+        PSC_LDS const uint8_t *p = keys + stage * S::kBytes;
+        if constexpr (D == 128) {
+            const u32x4 t = *(PSC_LDS const u32x4 *)(p + (w * 2 + h) * 1024);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = t[j];
+            ks = (key_scales + stage * S::kBytes)[(w * 2 + h) * 64];
+        } else {
+            const u32x2 t = *(PSC_LDS const u32x2 *)(p + w * 1024 + h * 512);
+            k[0] = t.x;
+            k[1] = t.y;
+            ks = (key_scales + stage * S::kBytes)[(w * 2 + h) * 32];
+        }
+    }
+    __device__ __forceinline__ void read_values(int stage, int w, uint32_t (&v)[8], uint32_t (&vs)[2][4]) const
+    {
+        PSC_LDS const uint8_t *p = values + stage * S::kBytes, *s = value_scales + stage * S::kBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                PSC_LDS const uint8_t *token = p + (D == 128 ? (w * 2 + h) * 1024 : w * 1024 + h * 512) + ((r + (D == 128 ? g : g >> 1)) & 3) * (D / 2);
+                if constexpr (D == 128) v[4 * h + r] = *(PSC_LDS const uint32_t *)token;
+                else v[4 * h + r] = *(PSC_LDS const uint16_t *)token;
+            }
+            if constexpr (D == 128) {
+                const u32x4 t = *(PSC_LDS const u32x4 *)(s + (w * 2 + h) * 64);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vs[h][r] = t[r];
+            } else {
+                const u32x2 t = *(PSC_LDS const u32x2 *)(s + (w * 2 + h) * 32);
+                vs[h][0] = t.x;
+                vs[h][1] = t.y;
+            }
+        }
+    }
+    __device__ __forceinline__ void read_positions(int stage, int (&pos)[8]) const
+    {
+        if constexpr (kPos) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 t = *(PSC_LDS const u32x4 *)(positions + stage * S::kBytes + h * 64);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) pos[4 * h + r] = (int)t[r];
+            }
+        }
+    }
+};
+
 // One wave attends with 16 RT rows, in both maps, over every fourth of the workgroup's blocks.  As in kv_attention_kernel: scores K Q^T leave
 // 8 scores of one row in a lane, which are the operand of V^T P^T as they are; maximum, sum and rescaling are the lane's own.
 // Tile t of map w is number w RT + t.  Accumulator (h D / 16 + j) of a tile has coordinate (4 g + r) D / 16 + j of value half h.
@@ -20,22 +113,26 @@ struct Difference {
     float top[2 * RT], sum[2 * RT];  // of the scaled scores in units of log 2, the maximum less kLift; the sum is the lane's own share
     Rows<D, DT> rows[2 * RT];
 
-    // kFar: rows whose scores are coarse may be among them
-    template <bool kFar>
-    __device__ __forceinline__ void block(const KvQueries &q, const Raw<D> (&raw)[2], const int (&positions)[8], const RowMask (&mask)[RT], int slot, int lim0, int lim1,
-                                          int n, bool whole, float factor, int i, int g, float *scores, int64_t scores_stride)
+    // kFar: rows whose scores are coarse may be among them.  `refill` is called when the stage has been read.
+    template <bool kFar, class Refill>
+    __device__ __forceinline__ void block(const KvQueries &q, const StageReader<D, kPos> &from, int stage, const RowMask (&mask)[RT], int slot, int lim0, int lim1,
+                                          int n, bool whole, float factor, int i, int g, float *scores, int64_t scores_stride, const Refill &refill)
     {
         f32x4 s[2 * RT][2];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                uint32_t k[D / 32], ks;
+                from.read_keys(stage, w, h, k, ks);
                 u32x4 a[D / 32];
-                expand_keys<D, DT>(raw[w].k[h], raw[w].ks[h], a);
+                expand_keys<D, DT>(k, ks, a);
 #pragma unroll
                 for (int t = 0; t < RT; ++t) s[w * RT + t][h] = scores_of<D, DT>(a, rows[w * RT + t]);
             }
         if (!whole) {
+            int positions[8];
+            from.read_positions(stage, positions);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -98,10 +195,13 @@ struct Difference {
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
+            uint32_t v[8], vs[2][4];
+            from.read_values(stage, half, v, vs);
+            if (half == 1) refill();
             // tokens 0..7 of the lane: 4 g + r, then 16 + 4 g + r
             uint32_t held[8];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) held[t] = value_scale<D>(raw[half].vs[t >> 2], t & 3, i);
+            for (int t = 0; t < 8; ++t) held[t] = value_scale<D>(vs[t >> 2], t & 3, i);
             if (!whole) {  // what lies past the end may be NaN: with the scale 2^-127 it is zeros in float16
 #pragma unroll
                 for (int t = 0; t < 8; ++t) held[t] = slot + (t < 4 ? 4 * g + t : 12 + 4 * g + t) < (t < 4 ? lim0 : lim1) ? held[t] : 0u;
@@ -113,7 +213,7 @@ struct Difference {
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
                     const float sc = __uint_as_float(held[t]);
-                    const uint32_t x = raw[half].v[t][0];
+                    const uint32_t x = v[t];
                     w[t] = y == 0 ? two_h16<0>(x, sc) : y == 1 ? two_h16<1>(x, sc) : y == 2 ? two_h16<2>(x, sc) : two_h16<3>(x, sc);
                 }
                 u32x4 lo, hi;
@@ -138,10 +238,10 @@ struct Difference {
 };
 
 // Waves of a SIMD that the registers are to leave room for.
-template <int D, int DT, int RT>
-constexpr int difference_waves()
+constexpr int difference_waves(int dim, int dtype, int row_tiles)
 {
-    return D == 64 && DT != PSC_F32 && RT == 1 ? 2 : 1;
+    if (dtype == PSC_F32) return dim == 64 ? 2 : 1;
+    return dim == 64 && row_tiles == 1 ? 3 : 2;
 }
 
 // From a row's sums over both maps, D / 16 coordinates of both value halves to each of 16 lanes that stand in a row: the output.
@@ -196,12 +296,17 @@ struct JoinedPair {  // of a workgroup's four waves
     float acc[4][16 * kStride];
     float tops[4][32 * RT], sums[4][32 * RT];
 };
+template <int D, int RT, bool kPos>
+union PairLds {  // first the stages, then the join
+    JoinedPair<D, RT> joined;
+    uint8_t stages[4][kStages][Stage<D, kPos>::kBytes];
+};
 
 // Blocks begin .. end - 1 of the rows from m0 on of (b, pair): the workgroup's four waves take every fourth each and are joined in LDS.
 // part < 0: these are all blocks, and the result is final.
 template <int D, int DT, int RT, bool kPos>
 __device__ __forceinline__ void attend_pair(const KvView &c, const KvQueries &q, const KvDifference &d, const RowSet &s, int b, int pair, int m0, const Blocks &blocks,
-                                            int begin, int end, int64_t part, JoinedPair<D, RT> &joined)
+                                            int begin, int end, int64_t part, PairLds<D, RT, kPos> &lds)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -231,72 +336,93 @@ __device__ __forceinline__ void attend_pair(const KvView &c, const KvQueries &q,
     const int64_t slots = (int64_t)c.width << c.page_shift, dense = ((int64_t)b * c.heads + 2 * pair) * slots;
     const int next_head = 1 << (c.page_shift - 4);  // sixteens from a head's slots to the next head's
 
-    // The places of 32 of the wave's blocks are held across the lanes; the codes of the block after the one that is worked on
+    // The places of 32 of the wave's blocks are held across the lanes; the codes of the blocks after the one that is worked on
     // are on their way, without a branch around their loads (past the last block: of a page that is there).
     const int own = begin + wave, mine = end > own ? (end - own + step - 1) / step : 0;
     auto pages_from = [&](int k) {
         return sixteen_of(c, b, 2 * pair, s.n, blocks.block(min(own + (k + (lane >> 1)) * step, end - 1)) * 32 + (lane & 1) * 16);
     };
-    auto load = [&](const int (&pg)[2], Raw<D> (&r)[2]) {
+    typedef Stage<D, kPos> S;
+    PSC_LDS uint8_t *const base = (PSC_LDS uint8_t *)lds.stages[wave];
+    const uint32_t base_at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)base);
+    const StageReader<D, kPos> reader(base, i, g);
+    // what the lane asks for: of keys, values and scales (see Stage)
+    const int key_token = D == 128 ? i * 64 + g * 16 : i * 32 + (g & 1) * 16;
+    const int row = D == 128 ? lane >> 2 : lane >> 1 & 15, value_token = (row & ~3) + ((row - (D == 128 ? row >> 2 : row >> 3)) & 3);
+    const int value_at = value_token * (D / 2) + (D == 128 ? lane & 3 : lane & 1) * 16;
+    const auto load = [&](int k, const int (&pg)[2], int stage) {
+        const uint32_t to = base_at + stage * S::kBytes;
+        const int p0 = max(pg[0], 0), p1 = max(pg[1], 0);
+        if constexpr (D == 128) {
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
+            for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int at = max(pg[h], 0) + w * next_head;
-                load_keys<D>(c, at, i, g, r[w].k[h], r[w].ks[h]);
-                load_values<D>(c, at, i, g, &r[w].v[4 * h], r[w].vs[h]);
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t at = (int64_t)((h ? p1 : p0) + w * next_head) * 1024;
+                    load_to_lds(c.k_codes + at + key_token, to + S::kKeys + (w * 2 + h) * 1024);
+                    load_to_lds(c.v_codes + at + value_at, to + S::kValues + (w * 2 + h) * 1024);
+                }
+            const int64_t at = (int64_t)((lane & 16 ? p1 : p0) + (lane >> 5) * next_head) * 64 + (lane & 15) * 4;
+            load_word_to_lds(c.k_scales + at, to + S::kKeyScales);
+            load_word_to_lds(c.v_scales + at, to + S::kValueScales);
+        } else {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int64_t at = (int64_t)((lane & 32 ? p1 : p0) + w * next_head) * 512;
+                load_to_lds(c.k_codes + at + key_token, to + S::kKeys + w * 1024);
+                load_to_lds(c.v_codes + at + value_at, to + S::kValues + w * 1024);
             }
-    };
-    auto load_positions = [&](int k, int (&pos)[8]) {
+            const int64_t at = (int64_t)((lane & 8 ? p1 : p0) + (lane >> 4 & 1) * next_head) * 32 + (lane & 7) * 4;
+            load_word_to_lds((lane & 32 ? c.v_scales : c.k_scales) + at, to + S::kKeyScales);
+        }
         if constexpr (kPos) {
             const int sl = blocks.block(min(own + k * step, end - 1)) * 32;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int4 x = *(const int4 *)(q.positions + dense + min(sl + 16 * h, (c.width << c.page_shift) - 16) + 4 * g);
-                pos[4 * h] = x.x;
-                pos[4 * h + 1] = x.y;
-                pos[4 * h + 2] = x.z;
-                pos[4 * h + 3] = x.w;
-            }
+            load_word_to_lds(q.positions + dense + min(sl + (lane & 31), (int)slots - 1), to + S::kPositions);
         }
     };
     // where the scores of the lane's row are left for kv_weights_of_scores_kernel
     float *scores = nullptr;
     if constexpr (RT == 1)
         if (q.scores && i < m_all) scores = q.scores + (((int64_t)b * c.heads + 2 * pair) * q.scores_rows + i) * slots;
-    const auto work = [&](auto far, int k, const Raw<D> (&raw)[2], const int (&pos)[8], const int (&pg)[2]) {
+    const auto work = [&](auto far, int k, int stage, const int (&pg)[2], const auto &refill) {
         const int slot = blocks.block(own + k * step) * 32;
         const bool there = slot + 32 <= s.n && pg[0] >= 0 && pg[1] >= 0 && !kPos;
         const bool whole = there && (!q.causal || slot + 31 <= lo_pos) &&
                            (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-        a.template block<far.value>(q, raw, pos, mask, slot, pg[0] >= 0 ? s.n : 0, pg[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores, q.scores_rows * slots);
+        a.template block<far.value>(q, reader, stage, mask, slot, pg[0] >= 0 ? s.n : 0, pg[1] >= 0 ? s.n : 0, s.n, whole, q.factor, i, g, scores, q.scores_rows * slots,
+                                    refill);
     };
     if (mine > 0) {
-        Raw<D> raw[2][2];
-        int ids = pages_from(0), pages[2][2] = {{__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)}, {-1, -1}};
-        load(pages[0], raw[0]);
-        for (int k0 = 0; k0 < mine; k0 += 32) {
-            const int ids_then = pages_from(k0 + 32), k_end = min(32, mine - k0);
-            const auto turn = [&](int k, const Raw<D> (&now)[2], const int (&now_pages)[2], Raw<D> (&next)[2], int (&next_pages)[2]) {
-                if (k < 31) {
-                    next_pages[0] = __builtin_amdgcn_readlane(ids, 2 * k + 2);
-                    next_pages[1] = __builtin_amdgcn_readlane(ids, 2 * k + 3);
-                } else {
-                    next_pages[0] = __builtin_amdgcn_readlane(ids_then, 0);
-                    next_pages[1] = __builtin_amdgcn_readlane(ids_then, 1);
-                }
-                int pos[8];
-                load_positions(k0 + k, pos);
-                load(next_pages, next);
-                work(std::false_type(), k0 + k, now, pos, now_pages);
-            };
-            for (int k = 0; k < k_end; k += 2) {  // (32 is even: a set's turn does not change from one 32 to the next)
-                turn(k, raw[0], pages[0], raw[1], pages[1]);
-                if (k + 1 < k_end) turn(k + 1, raw[1], pages[1], raw[0], pages[0]);
+        int ids = pages_from(0), pages[kStages + 1][2], stage = 0;  // pages of the block that is worked on, and of those under way
+#pragma unroll
+        for (int k = 0; k < kStages; ++k) {
+            pages[k][0] = __builtin_amdgcn_readlane(ids, 2 * k);
+            pages[k][1] = __builtin_amdgcn_readlane(ids, 2 * k + 1);
+            load(k, pages[k], k);
+        }
+        int ids_then = pages_from(32);
+        for (int k = 0; k < mine; ++k) {
+            const int ahead = (k & 31) + kStages, from = ahead < 32 ? ids : ids_then;
+            pages[kStages][0] = __builtin_amdgcn_readlane(from, 2 * (ahead & 31));
+            pages[kStages][1] = __builtin_amdgcn_readlane(from, 2 * (ahead & 31) + 1);
+            wait_for_loads<(kStages - 1) * S::kLoads>();
+            work(std::false_type(), k, stage, pages[0], [&] {
+                wait_for_lds();
+                load(k + kStages, pages[kStages], stage);
+            });
+            stage = stage + 1 < kStages ? stage + 1 : 0;
+#pragma unroll
+            for (int j = 0; j < kStages; ++j) {
+                pages[j][0] = pages[j + 1][0];
+                pages[j][1] = pages[j + 1][1];
             }
-            ids = ids_then;
+            if ((k & 31) == 31) {
+                ids = ids_then;
+                ids_then = pages_from(k + 33);
+            }
         }
     }
+    wait_for_loads<0>();  // (of blocks past the last too: their places are used again)
     // Decided at the end, and all done again, as in kv_attention_kernel.
     bool far = false;
 #pragma unroll
@@ -307,13 +433,14 @@ __device__ __forceinline__ void attend_pair(const KvView &c, const KvQueries &q,
 #pragma unroll 1
         for (int k = 0; k < mine; ++k) {
             const int ids = pages_from(k), pages[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
-            int pos[8];
-            load_positions(k, pos);
-            Raw<D> raw[2];
-            load(pages, raw);
-            work(std::true_type(), k, raw, pos, pages);
+            wait_for_lds();
+            load(k, pages, 0);
+            wait_for_loads<0>();
+            work(std::true_type(), k, 0, pages, [] {});
         }
     }
+    JoinedPair<D, RT> &joined = lds.joined;
+    __syncthreads();
 #pragma unroll
     for (int t = 0; t < 2 * RT; ++t) a.sum[t] = column_sum(a.sum[t]);
     if (g == 0) {
@@ -378,9 +505,9 @@ __device__ __forceinline__ void attend_pair(const KvView &c, const KvQueries &q,
 }
 
 template <int D, int DT, int RT, bool kPos, bool kParts>
-__global__ __launch_bounds__(256, (difference_waves<D, DT, RT>())) void kv_difference_kernel(KvView c, KvQueries q, KvDifference d)
+__global__ __launch_bounds__(256, difference_waves(D, DT, RT)) void kv_difference_kernel(KvView c, KvQueries q, KvDifference d)
 {
-    __shared__ JoinedPair<D, RT> joined;
+    __shared__ __attribute__((aligned(16))) PairLds<D, RT, kPos> lds;
     const int pairs = c.heads / 2;
     if constexpr (!kParts) {
         const int b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, m0 = (int)blockIdx.x * 16 * RT;
@@ -391,7 +518,7 @@ __global__ __launch_bounds__(256, (difference_waves<D, DT, RT>())) void kv_diffe
         }
         if (m0 >= s.rows * q.group) return;
         const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
-        attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, 0, blocks.count(), -1, joined);
+        attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, 0, blocks.count(), -1, lds);
     } else {
         Parts all(c, q);
         if (blockIdx.x >= all.total) return;
@@ -403,7 +530,7 @@ __global__ __launch_bounds__(256, (difference_waves<D, DT, RT>())) void kv_diffe
         const int pair = (int)unit % pairs, m0 = (int)unit / pairs * 16 * RT;
         const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
         const int count = blocks.count(), from = (int)((uint64_t)part * each / parts), to = (int)((uint64_t)(part + 1) * each / parts);
-        attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, min(count, from), min(count, to), parts == 1 ? -1 : (int64_t)blockIdx.x, joined);
+        attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, min(count, from), min(count, to), parts == 1 ? -1 : (int64_t)blockIdx.x, lds);
     }
 }
 
@@ -533,7 +660,7 @@ KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, 
     int64_t blocks = (slots + 31) / 32;
     if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
     const int64_t units = p.row_groups * c.batch * pairs;
-    const int waves = c.dim == 64 && dtype != PSC_F32 && p.row_tiles == 1 ? 2 : 1;  // workgroups to a compute unit: difference_waves
+    const int waves = difference_waves(c.dim, dtype, p.row_tiles);  // workgroups to a compute unit
     if (units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31) p.workgroups = 256 * waves;
     if (p.workgroups) {
         // at most one part more to a unit than `wanted` of Parts, which is half of the workgroups or more

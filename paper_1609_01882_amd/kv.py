@@ -157,7 +157,7 @@ class KvCache:
             to = _array(q_out, q.dtype, (n, heads, self.head_dim), "q_out", device)
         elif q_out is not None:
             raise PscError("q_out: without q")
-        _check(_load().psc_kv_append_rotary(c, C.byref(rotary._struct), _dtype(k, "k"), *self._rows(k, self.kv_heads, "k"),
+        _check(_load().psc_kv_append_rotary(c, rotary._struct, _dtype(k, "k"), *self._rows(k, self.kv_heads, "k"),
                                             *self._rows(v, self.kv_heads, "v"), *rows, heads, to, n,
                                             _array(offsets, torch.int32, (batch + 1,), "offsets", device),
                                             _array(first, torch.int32, (batch,), "first", device),

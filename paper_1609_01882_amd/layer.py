@@ -10,11 +10,12 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 
 import torch
 
 from .binding import PscError, _check, _load, _workspace
-from .kv import _DTYPES, PSC_F32, _array, _dtype, _ints, _stream_address
+from .kv import _DTYPES, _array, _dtype, _stream_address
 
 
 class _Rotary(C.Structure):
@@ -28,10 +29,21 @@ class _Norm(C.Structure):
                 ("residual_scale", C.c_float), ("block_scale", C.c_float), ("eps", C.c_float)]
 
 
+_pack = struct.Struct("@5iPqPqPq2i2P3f0P").pack     # the same fields, packed at once: a call of a few microseconds notices
+assert struct.calcsize("@5iPqPqPq2i2P3f0P") == C.sizeof(_Norm)
+
+
 def _current(index, what):
     if torch.cuda.current_device() != index:
         raise PscError(f"{what} is on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
     return _stream_address(index)
+
+
+def _once(backward):
+    """A backward pass that cannot be differentiated again.  (The wrapper that says so to autograd costs a tenth of a small step, and is
+    needed only where a graph of the gradients is asked for.)"""
+    guarded = torch.autograd.function.once_differentiable(backward)
+    return staticmethod(lambda ctx, *grads: (guarded if torch.is_grad_enabled() else backward)(ctx, *grads))
 
 
 # ------------------------------------------------------------------------------------------- rotary positions
@@ -79,7 +91,7 @@ class Rotary:
         signed = [t - (1 << 64) if t >> 63 else t for t in turns]
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
         self.device, self._index = self.turns.device, self.turns.get_device()
-        self._struct = _Rotary(self.turns.data_ptr(), dims, self.interleaved, self.factor)
+        self._struct = bytes(_Rotary(self.turns.data_ptr(), dims, self.interleaved, self.factor))
 
     def __call__(self, x, positions=None, first=None, offsets=None, out=None):
         """x [rows, heads, head_dim] (or [rows, head_dim]) turned: row r at positions[r] (int32), or at first[b] + its place in
@@ -98,13 +110,18 @@ class Rotary:
         return self._turn(x, positions, first, offsets, out, True)
 
     def _turn(self, x, positions, first, offsets, out, transposed):
-        stream = _current(self._index, "the rotary")
-        code = _dtype(x, "x")
-        whole = x.unsqueeze(1) if x.dim() == 2 else x
-        if whole.dim() != 3 or x.get_device() != self._index or whole.shape[2] < self.dims or whole.stride(2) != 1:
-            raise PscError(f"x: expected [rows, heads, head_dim >= {self.dims}] on {self.device} with contiguous coordinates, got {list(x.shape)} "
+        stream, index = _current(self._index, "the rotary"), self._index
+        code, shape = _dtype(x, "x"), x.shape
+        if len(shape) == 3:
+            rows, heads, dim = shape
+            row_stride, head_stride, last = x.stride()
+        elif len(shape) == 2:
+            (rows, dim), heads, (row_stride, last), head_stride = shape, 1, x.stride(), 0
+        else:
+            rows, heads, dim, last = 0, 0, 0, 0
+        if x.get_device() != index or dim < self.dims or last != 1:
+            raise PscError(f"x: expected [rows, heads, head_dim >= {self.dims}] on {self.device} with contiguous coordinates, got {list(shape)} "
                            f"with strides {list(x.stride())} on {x.device}")
-        rows, heads, dim = whole.shape
         batch = 1
         if positions is not None and (first is not None or offsets is not None):
             raise PscError("positions: of rows, or first and offsets of sequences")
@@ -115,16 +132,16 @@ class Rotary:
         if batch < 1:
             raise PscError("first, offsets: expected [batch] and [batch + 1]")
         if out is None:
-            out = torch.empty((rows, heads, dim) if x.dim() == 3 else (rows, dim), dtype=x.dtype, device=x.device)
-        to = out.unsqueeze(1) if out.dim() == 2 and x.dim() == 2 else out
-        if to.shape != whole.shape or to.dtype != x.dtype or to.get_device() != self._index or to.stride(2) != 1:
-            raise PscError(f"out: expected {x.dtype} {list(x.shape)} on {self.device} with contiguous coordinates")
-        _ints(rows=rows, heads=heads, head_dim=dim)
-        _check(_load().psc_rotary_rows(C.byref(self._struct), int(transposed), code, whole.data_ptr(), whole.stride(0), whole.stride(1), rows, heads, dim,
-                                       _array(positions, torch.int32, (rows,), "positions", self._index), batch,
-                                       _array(offsets, torch.int32, (batch + 1,), "offsets", self._index),
-                                       _array(first, torch.int32, (batch,), "first", self._index),
-                                       to.data_ptr(), to.stride(0), to.stride(1), stream))
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            to = heads * dim, dim
+        else:
+            if out.shape != shape or out.dtype is not x.dtype or out.get_device() != index or out.stride(-1) != 1:
+                raise PscError(f"out: expected {x.dtype} {list(shape)} on {self.device} with contiguous coordinates")
+            to = out.stride(0), out.stride(1) if heads > 1 else 0
+        _check(_load().psc_rotary_rows(self._struct, transposed, code, x.data_ptr(), row_stride, head_stride, rows, heads, dim,
+                                       _array(positions, torch.int32, (rows,), "positions", index), batch,
+                                       _array(offsets, torch.int32, (batch + 1,), "offsets", index),
+                                       _array(first, torch.int32, (batch,), "first", index), out.data_ptr(), *to, stream))
         return out
 
 
@@ -135,8 +152,7 @@ class _Turned(torch.autograd.Function):
         ctx.save_for_backward(positions, first, offsets)
         return rotary._turn(x, positions, first, offsets, None, False)
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         if dy.stride(-1) != 1:
             dy = dy.contiguous()
@@ -147,44 +163,32 @@ class _Turned(torch.autograd.Function):
 _ACTIVATIONS = {"none": 0, None: 0, "sigmoid": 1, "silu": 2}
 
 
-def _matrix(t, dtype, rows, width, name, device):
-    """Address and row stride of [rows, width] with contiguous coordinates."""
-    if t is None:
-        return None, 0
-    if t.dim() != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows) or t.dtype != dtype or t.get_device() != device or \
-            (width > 1 and t.stride(1) != 1):
-        raise PscError(f"{name}: expected {dtype} [{'rows' if rows is None else rows}, {width}] on cuda:{device} with contiguous coordinates, got "
-                       f"{t.dtype} {list(t.shape)} with strides {list(t.stride())} on {t.device}")
-    return t.data_ptr(), t.stride(0)
-
-
-def _norm_struct(x, y, gate, after, before, activation, residual_scale, block_scale, eps):
+def _struct_of(x, y, gate, after, before, numbers):
+    """The call's struct; what it points to has been checked."""
     some = y if x is None else x
-    device, (rows, width) = some.get_device(), some.shape
-    block = (y if y is not None else x).dtype
+    rows, width = some.shape
     weights = after if after is not None else before
-    weight = torch.float32 if weights is None else weights.dtype
-    x_at, x_stride = _matrix(x, some.dtype, rows, width, "x", device)
-    y_at, y_stride = _matrix(y, block, rows, width, "y", device)
-    gate_at, gate_stride = _matrix(gate, block, None, width, "gate", device)
-    if gate is not None and (gate.shape[0] == 0 or rows % gate.shape[0]) and rows:
-        raise PscError(f"gate: {rows} rows are no multiple of {gate.shape[0]}")
-    after_at = _array(after, weight, (width,), "after", device)
-    before_at = _array(before, weight, (width,), "before", device)
-    _ints(rows=rows, width=width)
-    return _Norm(rows, width, _DTYPES[some.dtype], _DTYPES[block], _DTYPES.get(weight, PSC_F32), x_at, x_stride, y_at, y_stride, gate_at, gate_stride,
-                 0 if gate is None else gate.shape[0], activation, after_at, before_at, residual_scale, block_scale, eps)
+    block = some if y is None else y
+    x_at, x_stride = (0, 0) if x is None else (x.data_ptr(), x.stride(0))
+    y_at, y_stride = (0, 0) if y is None else (y.data_ptr(), y.stride(0))
+    gate_at, gate_stride, gate_rows = (0, 0, 0) if gate is None else (gate.data_ptr(), gate.stride(0), gate.shape[0])
+    activation, *scales = numbers
+    return _pack(rows, width, _DTYPES[some.dtype], _DTYPES[block.dtype], _DTYPES[torch.float32 if weights is None else weights.dtype],
+                 x_at, x_stride, y_at, y_stride, gate_at, gate_stride, gate_rows, activation, 0 if after is None else after.data_ptr(),
+                 0 if before is None else before.data_ptr(), *scales)
 
 
 def _forward(x, y, gate, after, before, numbers, want_h, want_stat):
-    n = _norm_struct(x, y, gate, after, before, *numbers)
     some = y if x is None else x
-    stream = _current(some.get_device(), "x")
-    h = torch.empty(some.shape, dtype=some.dtype, device=some.device) if want_h else None
-    z = torch.empty(some.shape, dtype=(y if y is not None else x).dtype, device=some.device) if before is not None else None
-    stat = torch.empty((n.rows, 2), dtype=torch.float32, device=some.device) if want_stat else None
-    _check(_load().psc_residual_norm_forward(C.byref(n), None if h is None else h.data_ptr(), None if z is None else z.data_ptr(),
-                                             None if stat is None else stat.data_ptr(), stream))
+    h = torch.empty_like(some, memory_format=torch.contiguous_format) if want_h else None
+    z = stat = None
+    if before is not None:
+        z = torch.empty_like(some if y is None else y, memory_format=torch.contiguous_format)
+    if want_stat:
+        stat = torch.empty((some.shape[0], 2), dtype=torch.float32, device=some.device)
+    _check(_load().psc_residual_norm_forward(_struct_of(x, y, gate, after, before, numbers), h.data_ptr() if want_h else None,
+                                             None if z is None else z.data_ptr(), stat.data_ptr() if want_stat else None,
+                                             _current(some.get_device(), "x")))
     return h, z, stat
 
 
@@ -197,25 +201,37 @@ class _ResidualNorm(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         return h, z
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dh, dz):
-        x, y, gate, after, before, stat = ctx.saved_tensors
-        given = (x, y, gate, after, before)
-        n = _norm_struct(*given, *ctx.numbers)
-        wanted = ctx.needs_input_grad[:5]
-        if n.rows == 0:
+        *given, stat = ctx.saved_tensors
+        wanted = ctx.needs_input_grad
+        if stat.shape[0] == 0:
             return (*(torch.zeros_like(t) if w else None for t, w in zip(given, wanted)), None, None)
-        device = stat.device
-        stream = _current(device.index, "x")
-        dh, dz = (None if t is None else t.contiguous() for t in (dh, dz))
-        grads = [torch.empty(t.shape, dtype=t.dtype, device=device) if w else None for t, w in zip(given, wanted)]
-        lib = _load()
-        need = lib.psc_residual_norm_workspace_bytes(C.byref(n))
-        space = _workspace(need, device)
-        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        _check(lib.psc_residual_norm_backward(C.byref(n), stat.data_ptr(), at(dh), at(dz), *map(at, grads), space.data_ptr(), need, stream))
+        norm, lib = _struct_of(*given, ctx.numbers), _load()
+        if dh is not None and not dh.is_contiguous():
+            dh = dh.contiguous()
+        if dz is not None and not dz.is_contiguous():
+            dz = dz.contiguous()
+        grads = [torch.empty_like(t, memory_format=torch.contiguous_format) if w else None for t, w in zip(given, wanted)]
+        need = lib.psc_residual_norm_workspace_bytes(norm)
+        space = _workspace(need, stat.device)
+        _check(lib.psc_residual_norm_backward(norm, stat.data_ptr(), *(None if t is None else t.data_ptr() for t in (dh, dz, *grads)), space.data_ptr(),
+                                              need, _current(stat.get_device(), "x")))
         return (*grads, None, None)
+
+
+def _rows_of(t, width, dtype, name, device):
+    """t as [rows, width] with contiguous coordinates, one stride apart."""
+    if t.dtype is not dtype or t.get_device() != device or t.dim() < 1 or t.shape[-1] != width:
+        raise PscError(f"{name}: expected {dtype} [..., {width}] on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, width)
+        except RuntimeError:
+            raise PscError(f"{name}: rows must lie at one stride, got strides {list(t.stride())}") from None
+    if width > 1 and t.stride(1) != 1:
+        raise PscError(f"{name}: expected contiguous coordinates, got strides {list(t.stride())}")
+    return t
 
 
 def residual_norm(x, y=None, *, gate=None, activation="none", after=None, before=None, residual_scale=1.0, block_scale=1.0, eps=1e-6):
@@ -230,41 +246,49 @@ def residual_norm(x, y=None, *, gate=None, activation="none", after=None, before
     some = y if x is None else x
     if some is None:
         raise PscError("x and y are None")
-    if y is None and (gate is not None or after is not None):
-        raise PscError("gate, after: without y")
-    if activation not in _ACTIVATIONS:
+    code, device = _ACTIVATIONS.get(activation), some.get_device()
+    if code is None:
         raise PscError(f"activation: expected \"none\", \"sigmoid\" or \"silu\", got {activation!r}")
-    if not some.is_cuda or some.dim() < 1:
+    if device < 0 or some.dim() < 1:
         raise PscError(f"x: expected CUDA tensors [..., width], got {list(some.shape)} on {some.device}")
-    if x is not None and y is not None and x.shape != y.shape:
-        raise PscError(f"y: expected {list(x.shape)}, got {list(y.shape)}")
-    for t, name in ((x, "x"), (y, "y")):
-        if t is not None:
-            _dtype(t, name)
-    if x is not None and y is not None and x.dtype not in (torch.float32, y.dtype):
-        raise PscError(f"x: expected float32 or y's {y.dtype}, got {x.dtype}")
-    for t, name in ((after, "after"), (before, "before")):
-        if t is not None and t.dtype not in (torch.float32, (some if y is None else y).dtype):
-            raise PscError(f"{name}: expected float32 or the block's type, got {t.dtype}")
+    _dtype(some, "x")
     shape, width = some.shape, some.shape[-1]
-
-    def rows_of(t, name):
-        if t is None or t.dim() == 2:
-            return t
-        try:
-            return t.view(-1, width)
-        except RuntimeError:
-            raise PscError(f"{name}: rows must lie at one stride, got strides {list(t.stride())}") from None
-
-    x2, y2, gate2 = rows_of(x, "x"), rows_of(y, "y"), rows_of(gate, "gate")
-    numbers = (_ACTIVATIONS[activation], residual_scale, block_scale, eps)
+    kind = some.dtype
     plain = y is None and residual_scale == 1.0
+    if x is not None:
+        x2 = _rows_of(x, width, kind, "x", device)
+    else:
+        x2 = None
+    if y is None:
+        if gate is not None or after is not None:
+            raise PscError("gate, after: without y")
+        y2 = None
+    else:
+        if y.shape != shape:
+            raise PscError(f"y: expected {list(shape)}, got {list(y.shape)}")
+        if kind is not torch.float32 and y.dtype is not kind:
+            raise PscError(f"x: expected float32 or y's {y.dtype}, got {kind}")
+        kind = y.dtype
+        _dtype(y, "y")
+        y2 = _rows_of(y, width, kind, "y", device)
+    if gate is not None:
+        gate = _rows_of(gate, width, kind, "gate", device)
+        rows, gates = y2.shape[0], gate.shape[0]
+        if rows and (gates == 0 or rows % gates):
+            raise PscError(f"gate: {rows} rows are no multiple of {gates}")
+    weights = after if after is not None else before
+    if weights is not None:
+        if weights.dtype is not torch.float32 and weights.dtype is not kind:
+            raise PscError(f"after, before: expected float32 or {kind}, got {weights.dtype}")
+        _array(after, weights.dtype, (width,), "after", device)
+        _array(before, weights.dtype, (width,), "before", device)
     if plain and before is None:
         return x, None
-    given = (x2, y2, gate2, after, before)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given):
-        h, z = _ResidualNorm.apply(*given, numbers, not plain)
+    numbers = (code, residual_scale, block_scale, eps)
+    if torch.is_grad_enabled() and any([t is not None and t.requires_grad for t in (x2, y2, gate, after, before)]):
+        h, z = _ResidualNorm.apply(x2, y2, gate, after, before, numbers, not plain)
     else:
-        h, z, _ = _forward(*given, numbers, not plain, False)
-    h = x if plain else h.view(shape)
-    return h, None if z is None else z.view(shape)
+        h, z, _ = _forward(x2, y2, gate, after, before, numbers, not plain, False)
+    if len(shape) != 2:
+        h, z = None if h is None else h.view(shape), None if z is None else z.view(shape)
+    return x if plain else h, z
