@@ -432,6 +432,7 @@ struct KvPlan {
     int64_t workgroups = 0;  // units are cut into parts, about so many together; 0: a workgroup has a unit
     int64_t most_parts = 0;
     int least_blocks = 0;    // of a part
+    bool own_rows = false;   // differential attention: a wave has rows of its own
     int scores_rows = 0;     // the scores of so many rows are kept for the weights (0: they are computed again)
     bool split_rows = false;     // and then a workgroup's waves take rows each, not tokens
     int64_t weights_groups = 0;  // workgroups of the weights to a (sequence, kv head)

@@ -241,7 +241,7 @@ struct Difference {
 constexpr int difference_waves(int dim, int dtype, int row_tiles)
 {
     if (dtype == PSC_F32) return dim == 64 ? 2 : 1;
-    return dim == 64 && row_tiles == 1 ? 3 : 2;
+    return 2;
 }
 
 // From a row's sums over both maps, D / 16 coordinates of both value halves to each of 16 lanes that stand in a row: the output.
@@ -534,6 +534,264 @@ __global__ __launch_bounds__(256, difference_waves(D, DT, RT)) void kv_differenc
     }
 }
 
+// ------------------------------------------------------------------------------------------- many rows
+// Where there are rows for it, a wave has 16 RT rows of its own and a workgroup's four waves take every block together: each expands a
+// quarter of the block's keys and values -- sixteen tokens of a head -- into LDS as the operands of the products, and all four read them.  Two
+// buffers in turn: one barrier to a block.  A wave's expansions (192 vector instructions to a block of 128 coordinates, of 390 altogether) become 48.
+// 16 RT rows past the last one take part in the expansions alone.
+template <int D>
+struct Operands {
+    u32x4 keys[2][2][D / 32][64];      // [map][sixteen][32 coordinates]: a lane's operand of a product
+    u32x2 values[2][D / 16][2][64];    // [half][16 coordinates][sixteen]: half of one
+};
+template <int D>
+struct Quarter {  // of a block, as it lies in memory
+    uint32_t k[D / 32], ks, v[4][1], vs[4];
+};
+
+template <int D, int DT, int RT, bool kPos>
+struct RowsDifference {
+    f32x4 acc[2 * RT][D / 8];  // as in Difference
+    float top[2 * RT], sum[2 * RT];
+    Rows<D, DT> rows[2 * RT];
+
+    template <bool kFar>
+    __device__ __forceinline__ void block(const KvQueries &q, const Operands<D> &from, const RowMask (&mask)[RT], const int (&pos)[8], int slot, int lim0, int lim1,
+                                          bool whole, float factor, int lane)
+    {
+        const int g = lane >> 4;
+        f32x4 s[2 * RT][2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 a[D / 32];
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) a[j] = from.keys[w][h][j][lane];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) s[w * RT + t][h] = scores_of<D, DT>(a, rows[w * RT + t]);
+            }
+        if (!whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = slot + 16 * h + 4 * g + r;
+                    const bool there = at < (h ? lim1 : lim0);
+                    const int p = kPos ? pos[4 * h + r] : at;
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+                        if (!(there && sees(q, mask[t], p))) s[t][h][r] = s[RT + t][h][r] = kNegInf;
+                }
+        }
+        uint32_t p[2 * RT][4];  // float16 pairs
+#pragma unroll
+        for (int t = 0; t < 2 * RT; ++t) {
+            float m = kNegInf;  // (NaN where a score is: the row is lost then, whatever the maximum)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) m = __builtin_elementwise_maximum(m, s[t][h][r]);
+            m = __builtin_fmaf(column_max(m), factor, -kLift);
+            if (__any(m > top[t])) {
+                const float now = fmaxf(top[t], kFar ? reference_below(m) : m);
+                const float shrink = now == kNegInf ? 1.f : exp2_fast(top[t] - now);
+                top[t] = now;
+                sum[t] *= shrink;
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) acc[t][j] *= shrink;
+            }
+            const float base = top[t] == kNegInf ? 0.f : top[t];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    float e0 = __builtin_fmaf(s[t][h][r], factor, -base), e1 = __builtin_fmaf(s[t][h][r + 1], factor, -base);
+                    if constexpr (kFar) {
+                        const float most = most_exponent(base);
+                        e0 = __builtin_elementwise_minimum(e0, most);  // (NaN stays)
+                        e1 = __builtin_elementwise_minimum(e1, most);
+                    }
+                    e0 = exp2_fast(e0);
+                    e1 = exp2_fast(e1);
+                    sum[t] += e0 + e1;
+                    p[t][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, (h16x2){(_Float16)e0, (_Float16)e1});
+                }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                const u32x2 x = from.values[half][j][0][lane], y = from.values[half][j][1][lane];
+                const h16x8 v = __builtin_bit_cast(h16x8, (u32x4){x.x, x.y, y.x, y.y});
+#pragma unroll
+                for (int t = 0; t < 2 * RT; ++t) {
+                    const h16x8 pr = __builtin_bit_cast(h16x8, (u32x4){p[t][0], p[t][1], p[t][2], p[t][3]});
+                    acc[t][half * (D / 16) + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pr, acc[t][half * (D / 16) + j], 0, 0, 0);
+                }
+            }
+    }
+};
+
+template <int D, int DT, int RT, bool kPos>
+__global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, KvQueries q, KvDifference d)
+{
+    __shared__ Operands<D> operands[2];
+    const int pairs = c.heads / 2, b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, lane = lane_id(), i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const RowSet s = rows_of(c, q, b);
+    const int group0 = (int)blockIdx.x * 64 * RT, m_all = s.rows * q.group, group_end = min(group0 + 64 * RT, m_all);
+    if (q.offsets && group0 == 0) {
+        if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
+        difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
+    }
+    if (group0 >= m_all) return;
+    const int m0 = group0 + wave * 16 * RT, m_end = min(m0 + 16 * RT, m_all);
+    const bool some = m0 < m_all;
+    const int lo_pos = s.first_pos + min(m0, m_all - 1) / q.group, hi_pos = s.first_pos + (m_end - 1) / q.group;
+    const Blocks blocks = blocks_of(q, s.n, s.first_pos + group0 / q.group, s.first_pos + (group_end - 1) / q.group);
+    const int count = blocks.count();
+    const int64_t slots = (int64_t)c.width << c.page_shift, dense = ((int64_t)b * c.heads + 2 * pair) * slots;
+    const int next_head = 1 << (c.page_shift - 4);  // sixteens from a head's slots to the next head's
+
+    RowsDifference<D, DT, RT, kPos> a;
+    RowMask mask[RT];
+    const auto start = [&] {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int m = min(m0 + t * 16 + i, m_all - 1), place = m / q.group;  // (rows past the last: the last one again)
+            mask[t] = row_mask(q, s.first_pos + place);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int n = w * RT + t;
+                load_rows<D, DT>(q, s.first_row + place, (2 * pair + w) * q.group + m - place * q.group, g, a.rows[n]);
+                a.top[n] = kNegInf;
+                a.sum[n] = 0.f;
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) a.acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+    };
+    // The places of 32 blocks are held across the lanes, a sixteen to each; a wave's quarter is sixteen `mine` of head `head`.
+    const int head = wave >> 1, mine = wave & 1;
+    const auto pages_from = [&](int k) { return sixteen_of(c, b, 2 * pair, s.n, blocks.block(min(k + (lane >> 1), count - 1)) * 32 + (lane & 1) * 16); };
+    const auto load = [&](int page, Quarter<D> &x) {
+        const int at = max(page, 0) + head * next_head;
+        load_keys<D>(c, at, i, g, x.k, x.ks);
+        load_values<D>(c, at, i, g, x.v, x.vs);
+    };
+    const auto expand = [&](const Quarter<D> &x, int slot, int page, Operands<D> &to) {
+        u32x4 k[D / 32];
+        expand_keys<D, DT>(x.k, x.ks, k);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) to.keys[head][mine][j][lane] = k[j];
+        uint32_t held[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            held[r] = value_scale<D>(x.vs, r, i);
+            // what lies past the end may be NaN: with the scale 2^-127 it is zeros in float16
+            if (page < 0 || slot + 16 * mine + 16 > s.n) held[r] = page >= 0 && slot + 16 * mine + 4 * g + r < s.n ? held[r] : 0u;
+        }
+#pragma unroll
+        for (int y = 0; y < D / 32; ++y) {
+            uint32_t w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float sc = __uint_as_float(held[r]);
+                w[r] = y == 0 ? two_h16<0>(x.v[r][0], sc) : y == 1 ? two_h16<1>(x.v[r][0], sc) : y == 2 ? two_h16<2>(x.v[r][0], sc) : two_h16<3>(x.v[r][0], sc);
+            }
+            to.values[head][2 * y][mine][lane] = u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
+            to.values[head][2 * y + 1][mine][lane] = u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
+        }
+    };
+    const auto pass = [&](auto far) {
+        start();
+        if (count == 0) return;
+        int ids = pages_from(0), ids_then = pages_from(32);
+        Quarter<D> now, next;
+        load(__builtin_amdgcn_readlane(ids, mine), now);
+        for (int k = 0; k < count; ++k) {
+            const int in = k & 31, page0 = __builtin_amdgcn_readlane(ids, 2 * in), page1 = __builtin_amdgcn_readlane(ids, 2 * in + 1);
+            load(__builtin_amdgcn_readlane(in < 31 ? ids : ids_then, 2 * ((in + 1) & 31) + mine), next);
+            const int slot = blocks.block(k) * 32;
+            int pos[8];
+            if constexpr (kPos) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int4 x = *(const int4 *)(q.positions + dense + min(slot + 16 * h, (int)slots - 16) + 4 * g);
+                    pos[4 * h] = x.x;
+                    pos[4 * h + 1] = x.y;
+                    pos[4 * h + 2] = x.z;
+                    pos[4 * h + 3] = x.w;
+                }
+            }
+            Operands<D> &buffer = operands[k & 1];
+            expand(now, slot, mine ? page1 : page0, buffer);
+            __syncthreads();
+            const bool there = slot + 32 <= s.n && page0 >= 0 && page1 >= 0 && !kPos;
+            const bool whole = there && (!q.causal || slot + 31 <= lo_pos) && (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
+            const bool hidden = !kPos && ((q.causal && slot > hi_pos) || (q.window > 0 && (int64_t)lo_pos - (slot + 31) >= q.window && slot >= q.sinks));
+            if (some && !hidden) a.template block<far.value>(q, buffer, mask, pos, slot, page0 >= 0 ? s.n : 0, page1 >= 0 ? s.n : 0, whole, q.factor, lane);
+            now = next;
+            if (in == 31) {
+                ids = ids_then;
+                ids_then = pages_from(k + 33);
+            }
+        }
+    };
+    pass(std::false_type());
+    // Decided at the end, and all done again, as in kv_attention_kernel.
+    bool coarse = false;
+#pragma unroll
+    for (int t = 0; t < 2 * RT; ++t) coarse = coarse || is_coarse(a.top[t]);
+    if (__syncthreads_or(coarse && some)) {
+        asm volatile("" ::: "memory");  // (the rows are read again: kept, they would cost the pass above registers)
+        pass(std::true_type());
+    }
+    if (!some) return;
+    typedef typename Element<DT>::type T;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int m = m0 + t * 16 + i;
+        float inv[2], squares = 0.f;
+        const bool there = m < m_all;
+        const int row = s.first_row + min(m, m_all - 1) / q.group, in_group = min(m, m_all - 1) % q.group, out_head = pair * q.group + in_group;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int n = w * RT + t;
+            const float sum = column_sum(a.sum[n]);
+            inv[w] = sum == 0.f ? 0.f : 1.f / sum;
+            if (g == 0 && there) {
+                const int64_t at = (int64_t)row * q.q_heads + (2 * pair + w) * q.group + in_group;
+                if (q.lse) q.lse[at] = sum == 0.f ? kNegInf : log_sum(a.top[n], sum);
+                if (q.stat) *(float2 *)(q.stat + at * 2) = make_float2(a.top[n] == kNegInf ? 0.f : a.top[n], inv[w]);
+            }
+        }
+        const float lam = d.lam[(int64_t)row * d.lam_stride + out_head];
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float o = a.acc[t][j][r] * inv[0] - lam * (a.acc[RT + t][j][r] * inv[1]);
+                a.acc[t][j][r] = o;
+                squares += o * o;
+            }
+        float scale = d.factor;
+        if (d.norm) scale *= 1.f / sqrtf(column_sum(squares) * (1.f / (2 * D)) + d.eps);
+        T *out = (T *)q.out + ((int64_t)row * (q.q_heads / 2) + out_head) * (2 * D);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at = half * D + (4 * g + r) * (D / 16);
+                float o[D / 16];
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[j] = a.acc[t][half * (D / 16) + j][r] * (d.norm ? d.norm[at + j] * scale : scale);
+                if (there) store_row<DT, D / 16>(out + at, o);
+            }
+    }
+}
+
 // Joins the parts of an output head's two maps, a wave to a (row, output head): each lane takes a part's maximum and sum (64 parts at a
 // time), then the lanes take D / 16 coordinates of both halves of every fourth part each.  Sequences without a block have no part:
 // zeros.
@@ -622,6 +880,12 @@ constexpr int64_t kLeastBlocks = 8, kFewBlocks = 32;
 // Rows of a wave, in sixteens, at most.
 constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || dim == 128 ? 1 : 2; }
 
+// Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel).
+#ifndef KRG
+#define KRG 256
+#endif
+constexpr int64_t kRowGroups = KRG;
+
 template <int DT, int D>
 int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, const KvPlan &p, const float *given, float *received, hipStream_t s)
 {
@@ -629,6 +893,12 @@ int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, c
     if (q.nrows > 0) {
         const uint32_t groups = (uint32_t)(c.batch * (c.heads / 2));
         const auto launch = [&](auto rt, auto pos) {
+            if constexpr (DT != PSC_F32) {
+                if (p.own_rows) {
+                    kv_difference_rows_kernel<D, DT, kMost, pos.value><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, d);
+                    return;
+                }
+            }
             if (p.workgroups) kv_difference_kernel<D, DT, rt.value, pos.value, true><<<(uint32_t)p.most_parts, 256, 0, s>>>(c, q, d);
             else kv_difference_kernel<D, DT, rt.value, pos.value, false><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, d);
         };
@@ -659,9 +929,13 @@ KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, 
     // blocks of 32 tokens that a group of rows can see at most
     int64_t blocks = (slots + 31) / 32;
     if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
+    const int most = 64 * most_row_tiles(dtype, c.dim);
+    const int64_t groups = (m + most - 1) / most;
+    p.own_rows = dtype != PSC_F32 && groups * c.batch * pairs >= kRowGroups && m > most / 2;
+    if (p.own_rows) p.row_groups = groups;
     const int64_t units = p.row_groups * c.batch * pairs;
     const int waves = difference_waves(c.dim, dtype, p.row_tiles);  // workgroups to a compute unit
-    if (units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31) p.workgroups = 256 * waves;
+    if (!p.own_rows && units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31) p.workgroups = 256 * waves;
     if (p.workgroups) {
         // at most one part more to a unit than `wanted` of Parts, which is half of the workgroups or more
         p.most_parts = std::min(p.workgroups + units, units * ((blocks + kLeastBlocks - 1) / kLeastBlocks));

@@ -143,6 +143,52 @@ def test_rows_of_nobody_come_out_nan():
     _case(2, "bf16", 128, 1, 2, 16, [5000, 70], [3, 2], nobody=(1, 3))
 
 
+# Calls with so many rows that every wave of the card has some of its own: 64 sequences of 4 pairs, a workgroup or more to each.
+def _many(rng, rows):
+    """Lengths and rows of 64 sequences: few tokens before the rows or many, ends inside blocks and pages; one without rows, one without tokens."""
+    rows = [rows + int(r) for r in rng.integers(0, 30, 64)]
+    lengths = [r + int(t) for r, t in zip(rows, rng.choice([0, 1, 13, 31, 32, 100], 64))]
+    rows[7], lengths[9] = 0, 0
+    return lengths, rows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,rows", [(128, 33), (64, 65)])
+def test_rows_of_their_own(dtype, dim, rows):
+    lengths, rows = _many(np.random.default_rng(dim), rows)
+    _case(dim, dtype, dim, 4, 1, 16, lengths, rows, lam_rows=True, poison=[(3, lengths[3] - 5, 1)], missing=[(4, 0, -1), (5, 1, 1 << 20)], nobody=(2, 5))
+
+
+@pytest.mark.parametrize("dim,rows", [(128, 12), (64, 23)])
+def test_rows_of_their_own_with_windows_and_in_another_order(dim, rows):
+    lengths, rows = _many(np.random.default_rng(dim + 1), rows)
+    _case(1, "bf16", dim, 4, 3, 32, lengths, rows, window=20, sinks=3, weights=False)
+    _case(2, "f16", dim, 4, 3, 16, lengths, rows, evicted=True, window=150, sinks=5, norm=False)
+    _case(3, "bf16", dim, 4, 3, 16, lengths, rows, causal=False, weights=False)
+
+
+def test_rows_of_their_own_with_large_scores():
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(0)
+    buffers, table, lengths = L.random_memory(rng, 64, 8, 64, 16, [100] * 64)
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    q = torch.randn((64 * 70, 8, 64), device="cuda").half()
+    q[5 * 70 + 3] *= 6e4 / q[5 * 70 + 3].abs().max()
+    lam = torch.full((4,), 0.5, device="cuda")
+    # a scale that lifts the scores of one row of sequence 5 over 2^24, and leaves those of the others below it
+    out, lse = cache.attend_difference(q, lam, _cuda(table), _cuda(lengths), scale=64.0)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    few, few_lse = cache.attend_difference(q[5 * 70:6 * 70].contiguous(), lam, _cuda(table[5:6]), _cuda(lengths[5:6]), scale=64.0)
+    # Scores are the same products in both kernels, and so is what a row refers to in the end; probabilities are rounded to float16 against
+    # the largest seen so far, which differs: 2^-11 of each in either kernel.  Held values are 3 at most (6 times 2^-1), the maps weigh 1
+    # and 0.5: 2 * 1.5 * 3 * 2^-11, and two outputs of up to 4.5 rounded to float16: 2 * 4.5 * 2^-11.  The row beyond 2^24 has
+    # scores that 32 bits hardly tell apart: its output is within the held values.
+    mine, others = out[5 * 70:6 * 70], torch.arange(70, device="cuda") != 3
+    assert torch.equal(few_lse, lse[5 * 70:6 * 70])
+    assert float((few[others].float() - mine[others].float()).abs().max()) <= 18 * 2.0 ** -11
+    assert float(mine[3].abs().max()) <= 4.5 and float(few[3].abs().max()) <= 4.5
+
+
 def test_against_two_attentions():
     """The same maps through `attend` of each key head over each value head."""
     import paper_1609_01882_amd as psc
