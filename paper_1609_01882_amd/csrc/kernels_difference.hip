@@ -555,9 +555,10 @@ struct RowsDifference {
     float top[2 * RT], sum[2 * RT];
     Rows<D, DT> rows[2 * RT];
 
-    template <bool kFar>
+    // `keys` and `values` expand what the wave has of the next block, where the matrix units are at work on this one.
+    template <bool kFar, class Keys, class Values>
     __device__ __forceinline__ void block(const KvQueries &q, const Operands<D> &from, const RowMask (&mask)[RT], const int (&pos)[8], int slot, int lim0, int lim1,
-                                          bool whole, float factor, int lane)
+                                          bool whole, float factor, int lane, const Keys &keys, const Values &values)
     {
         const int g = lane >> 4;
         f32x4 s[2 * RT][2];
@@ -571,6 +572,7 @@ struct RowsDifference {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) s[w * RT + t][h] = scores_of<D, DT>(a, rows[w * RT + t]);
             }
+        keys();
         if (!whole) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -618,6 +620,7 @@ struct RowsDifference {
                     p[t][h * 2 + r / 2] = __builtin_bit_cast(uint32_t, (h16x2){(_Float16)e0, (_Float16)e1});
                 }
         }
+        values();
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -680,18 +683,18 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
         load_keys<D>(c, at, i, g, x.k, x.ks);
         load_values<D>(c, at, i, g, x.v, x.vs);
     };
-    const auto expand = [&](const Quarter<D> &x, int slot, int page, Operands<D> &to) {
+    const auto expand_k = [&](const Quarter<D> &x, Operands<D> &to) {
         u32x4 k[D / 32];
         expand_keys<D, DT>(x.k, x.ks, k);
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) to.keys[head][mine][j][lane] = k[j];
+    };
+    const auto expand_v = [&](const Quarter<D> &x, int slot, int page, Operands<D> &to) {
         uint32_t held[4];
+        // what lies past the end may be NaN: with the scale 2^-127 it is zeros in float16
+        const int lim = page < 0 ? 0 : s.n - slot - 16 * mine - 4 * g;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            held[r] = value_scale<D>(x.vs, r, i);
-            // what lies past the end may be NaN: with the scale 2^-127 it is zeros in float16
-            if (page < 0 || slot + 16 * mine + 16 > s.n) held[r] = page >= 0 && slot + 16 * mine + 4 * g + r < s.n ? held[r] : 0u;
-        }
+        for (int r = 0; r < 4; ++r) held[r] = r < lim ? value_scale<D>(x.vs, r, i) : 0u;
 #pragma unroll
         for (int y = 0; y < D / 32; ++y) {
             uint32_t w[4];
@@ -704,16 +707,24 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
             to.values[head][2 * y + 1][mine][lane] = u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
         }
     };
+    // The block that is worked on lies in one buffer; the next one's codes are here and go into the other while the products run, and those of
+    // the one after that are asked for then.  (Past the last block: the last one again.)
     const auto pass = [&](auto far) {
         start();
         if (count == 0) return;
         int ids = pages_from(0), ids_then = pages_from(32);
-        Quarter<D> now, next;
-        load(__builtin_amdgcn_readlane(ids, mine), now);
+        const auto page_of_block = [&](int in, int h) { return __builtin_amdgcn_readlane(in < 32 ? ids : ids_then, 2 * (in & 31) + h); };
+        const auto slot_of = [&](int k) { return blocks.block(min(k, count - 1)) * 32; };
+        Quarter<D> next;
+        load(page_of_block(0, mine), next);
+        expand_k(next, operands[0]);
+        expand_v(next, slot_of(0), page_of_block(0, mine), operands[0]);
+        load(page_of_block(1, mine), next);
+        __syncthreads();
         for (int k = 0; k < count; ++k) {
-            const int in = k & 31, page0 = __builtin_amdgcn_readlane(ids, 2 * in), page1 = __builtin_amdgcn_readlane(ids, 2 * in + 1);
-            load(__builtin_amdgcn_readlane(in < 31 ? ids : ids_then, 2 * ((in + 1) & 31) + mine), next);
-            const int slot = blocks.block(k) * 32;
+            const int in = k & 31, page0 = page_of_block(in, 0), page1 = page_of_block(in, 1), page_next = page_of_block(in + 1, mine);
+            const int page_then = page_of_block(in + 2, mine);
+            const int slot = slot_of(k), slot_next = slot_of(k + 1);
             int pos[8];
             if constexpr (kPos) {
 #pragma unroll
@@ -725,14 +736,17 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
                     pos[4 * h + 3] = x.w;
                 }
             }
-            Operands<D> &buffer = operands[k & 1];
-            expand(now, slot, mine ? page1 : page0, buffer);
-            __syncthreads();
+            const Operands<D> &buffer = operands[k & 1];
+            Operands<D> &other = operands[(k & 1) ^ 1];
             const bool there = slot + 32 <= s.n && page0 >= 0 && page1 >= 0 && !kPos;
             const bool whole = there && (!q.causal || slot + 31 <= lo_pos) && (q.window <= 0 || (int64_t)hi_pos - slot < q.window || slot + 32 <= q.sinks);
-            const bool hidden = !kPos && ((q.causal && slot > hi_pos) || (q.window > 0 && (int64_t)lo_pos - (slot + 31) >= q.window && slot >= q.sinks));
-            if (some && !hidden) a.template block<far.value>(q, buffer, mask, pos, slot, page0 >= 0 ? s.n : 0, page1 >= 0 ? s.n : 0, whole, q.factor, lane);
-            now = next;
+            a.template block<far.value>(q, buffer, mask, pos, slot, page0 >= 0 ? s.n : 0, page1 >= 0 ? s.n : 0, whole, q.factor, lane,
+                                        [&] { expand_k(next, other); },
+                                        [&] {
+                                            expand_v(next, slot_next, page_next, other);
+                                            load(page_then, next);
+                                        });
+            __syncthreads();
             if (in == 31) {
                 ids = ids_then;
                 ids_then = pages_from(k + 33);
