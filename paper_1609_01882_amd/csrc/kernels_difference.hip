@@ -40,6 +40,19 @@ __device__ __forceinline__ void wait_for_loads()  // but for the last N
 }
 __device__ __forceinline__ void wait_for_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// Scores of 32 tokens x 16 rows: as scores_of, with the two sums in turn, since a product waits for the one whose sum it goes on.
+template <int D, int DT>
+__device__ __forceinline__ void scores_of_two(const u32x4 (&a)[2][D / 32], const Rows<D, DT> &rows, f32x4 (&s)[2])
+{
+    s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int term = Rows<D, DT>::kTerms - 1; term >= 0; --term)  // the smallest first
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) s[h] = mfma_scores<DT>(a[h][j], rows.x[term][j], s[h]);
+}
+
 // What a lane reads of a stage.
 template <int D, bool kPos>
 struct StageReader {
@@ -121,15 +134,17 @@ struct Difference {
         f32x4 s[2 * RT][2];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
+        {
+            u32x4 a[2][D / 32];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t k[D / 32], ks;
                 from.read_keys(stage, w, h, k, ks);
-                u32x4 a[D / 32];
-                expand_keys<D, DT>(k, ks, a);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) s[w * RT + t][h] = scores_of<D, DT>(a, rows[w * RT + t]);
+                expand_keys<D, DT>(k, ks, a[h]);
             }
+#pragma unroll
+            for (int t = 0; t < RT; ++t) scores_of_two<D, DT>(a, rows[w * RT + t], s[w * RT + t]);
+        }
         if (!whole) {
             int positions[8];
             from.read_positions(stage, positions);
@@ -564,14 +579,15 @@ struct RowsDifference {
         f32x4 s[2 * RT][2];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
+        {
+            u32x4 a[2][D / 32];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 a[D / 32];
+            for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                for (int j = 0; j < D / 32; ++j) a[j] = from.keys[w][h][j][lane];
+                for (int h = 0; h < 2; ++h) a[h][j] = from.keys[w][h][j][lane];
 #pragma unroll
-                for (int t = 0; t < RT; ++t) s[w * RT + t][h] = scores_of<D, DT>(a, rows[w * RT + t]);
-            }
+            for (int t = 0; t < RT; ++t) scores_of_two<D, DT>(a, rows[w * RT + t], s[w * RT + t]);
+        }
         keys();
         if (!whole) {
 #pragma unroll
@@ -806,86 +822,87 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
     }
 }
 
-// Joins the parts of an output head's two maps, a wave to a (row, output head): each lane takes a part's maximum and sum (64 parts at a
-// time), then the lanes take D / 16 coordinates of both halves of every fourth part each.  Sequences without a block have no part:
-// zeros.
+// Joins the parts of an output head's two maps, a wave to each: its lanes take a part's maximum and sum each (64 parts at a time), then
+// 2 D / 64 coordinates of every part; the second map's wave hands its row to the first's.  Sequences without a block have no part: zeros.  What
+// bounds it is the way from load to load and through its instructions, which no workgroup runs twice: 8 x 16 heads of 128 with
+// 16 parts to each 13.7 us where a wave had both maps one after the other and every fourth part to a quarter of its lanes (10.7 kB
+// of instructions), 17.0 with the maps side by side (12 kB).
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQueries q, KvDifference d)
 {
-    const int lane = lane_id(), run = lane & 15, quarter = lane >> 4, out_heads = q.q_heads / 2;
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    if (item >= (int64_t)q.nrows * out_heads) return;
+    constexpr int N = D / 32;  // coordinates of a lane
+    __shared__ float second[2][2 * D];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), which = wave & 1, lane = lane_id(), out_heads = q.q_heads / 2;
+    const int64_t items = (int64_t)q.nrows * out_heads, item = min((int64_t)blockIdx.x * 2 + (wave >> 1), items - 1);  // (past the last: it again)
     const int r = (int)(item / out_heads), out_head = (int)(item % out_heads), pair = out_head / q.group, in_group = out_head % q.group;
     const int b = __builtin_amdgcn_readfirstlane(sequence_of_row(q.offsets, c.batch, q.each, r));
     const RowSet s = rows_of(c, q, b);
     const int place = r - s.first_row;
-    const int64_t row0 = (int64_t)r * q.q_heads + 2 * pair * q.group + in_group;  // of the first map; the second: q.group further
-    if (place < 0 || place >= s.rows) {  // nobody's
-        float nan[D / 16];
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) nan[j] = __builtin_nanf("");
-        if (quarter < 2) store_row<DT, D / 16>((typename Element<DT>::type *)q.out + item * (2 * D) + quarter * D + run * (D / 16), nan);
-        if (lane < 2 && q.lse) q.lse[row0 + lane * q.group] = nan[0];
-        return;
-    }
-    const int m = place * q.group + in_group, in_unit = m % q.unit_rows;
+    const bool nobodys = place < 0 || place >= s.rows;
+    const int m = nobodys ? 0 : place * q.group + in_group, in_unit = m % q.unit_rows;
     const uint32_t unit = (uint32_t)(m / q.unit_rows * q.unit_heads + pair);
     Parts all(c, q);
-    const int parts = (int)all.parts_of_unit(Parts::blocks_of_unit(q, s));
-    if (parts == 1) return;  // (final already)
-    const int64_t begin = (int64_t)all.first_of(c, q, b) + (int64_t)unit * parts;
-    float x[2][2][D / 16], inv[2];
+    const int parts = nobodys ? 0 : (int)all.parts_of_unit(Parts::blocks_of_unit(q, s));  // 1: final already
+    const int64_t at = (((int64_t)all.first_of(c, q, b) + (int64_t)unit * parts) * 2 + which) * q.unit_rows + in_unit;  // and every 2 unit_rows further
+    const int64_t further = 2 * q.unit_rows, row = (int64_t)r * q.q_heads + (2 * pair + which) * q.group + in_group;
+    float x[N], top = kNegInf, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const int64_t at = (begin * 2 + w) * q.unit_rows + in_unit;  // and every 2 unit_rows further
-        float top = kNegInf, sum = 0.f;
+    for (int j = 0; j < N; ++j) x[j] = 0.f;
+    for (int p0 = 0; p0 < (parts == 1 ? 0 : parts); p0 += 64) {
+        float2 st = make_float2(kNegInf, 0.f);
+        if (p0 + lane < parts) st = *(const float2 *)(q.part_stat + (at + (p0 + lane) * further) * 2);
+        float now = top;
+        if (st.y != 0.f) now = fmaxf(now, st.x);
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int k = 1; k < 64; k *= 2) now = fmaxf(now, __shfl_xor(now, k));
+        const float shrink = now == kNegInf ? 1.f : exp2_fast(top - now);
+        const float theirs = st.y == 0.f ? 0.f : now == kNegInf ? 1.f : exp2_fast(st.x - now);
+        float add = st.y * theirs;  // (a part that saw nothing: 0)
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) x[w][half][j] = 0.f;
-        for (int p0 = 0; p0 < parts; p0 += 64) {
-            float2 st = make_float2(kNegInf, 0.f);
-            if (p0 + lane < parts) st = *(const float2 *)(q.part_stat + (at + (int64_t)(p0 + lane) * 2 * q.unit_rows) * 2);
-            float now = top;
-            if (st.y != 0.f) now = fmaxf(now, st.x);
+        for (int k = 1; k < 64; k *= 2) add += __shfl_xor(add, k);
+        sum = __builtin_fmaf(sum, shrink, add);
+        top = now;
 #pragma unroll
-            for (int k = 1; k < 64; k *= 2) now = fmaxf(now, __shfl_xor(now, k));
-            const float shrink = now == kNegInf ? 1.f : exp2_fast(top - now);
-            const float theirs = st.y == 0.f ? 0.f : now == kNegInf ? 1.f : exp2_fast(st.x - now);
-            float add = st.y * theirs;  // (a part that saw nothing: 0)
+        for (int j = 0; j < N; ++j) x[j] *= shrink;
+        const int last = min(64, parts - p0);
+        for (int p = 0; p < last; p += 16) {  // (past the last: the last again, times 0)
+            float y[16][N];
 #pragma unroll
-            for (int k = 1; k < 64; k *= 2) add += __shfl_xor(add, k);
-            sum = __builtin_fmaf(sum, shrink, add);
-            top = now;
+            for (int u = 0; u < 16; ++u) load_row<PSC_F32, N>(q.part_acc + (at + (p0 + min(p + u, last - 1)) * further) * (2 * D) + lane * N, y[u]);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int u = 0; u < 16; ++u) {
+                const float weight = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(theirs), p + u));
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) x[w][half][j] *= shrink;
-            const int last = min(64, parts - p0);
-            for (int k = 0; k < last; k += 4) {  // (all lanes to the end: a lane's weight is asked of another one)
-                const int p = k + quarter;
-                const float weight = __shfl(theirs, p);  // past the last: 0
-                const float *from = q.part_acc + (at + (int64_t)(p0 + min(p, last - 1)) * 2 * q.unit_rows) * (2 * D) + run * (D / 16);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float y[D / 16];
-                    load_row<PSC_F32, D / 16>(from + half * D, y);
-#pragma unroll
-                    for (int j = 0; j < D / 16; ++j) x[w][half][j] = __builtin_fmaf(y[j], weight, x[w][half][j]);
-                }
+                for (int j = 0; j < N; ++j) x[j] = __builtin_fmaf(y[u][j], weight, x[j]);
             }
         }
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) x[w][half][j] = column_sum(x[w][half][j]);
-        inv[w] = sum == 0.f ? 0.f : 1.f / sum;
-        if (lane == 0) {
-            if (q.lse) q.lse[row0 + w * q.group] = sum == 0.f ? kNegInf : log_sum(top, sum);
-            if (q.stat) *(float2 *)(q.stat + (row0 + w * q.group) * 2) = make_float2(top == kNegInf ? 0.f : top, inv[w]);
-        }
     }
-    if (quarter == 0) finish_row<D, DT>(q, d, r, out_head, run, x, inv);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (lane == 0 && parts != 1) {
+        if (q.lse) q.lse[row] = nobodys ? __builtin_nanf("") : sum == 0.f ? kNegInf : log_sum(top, sum);
+        if (q.stat && !nobodys) *(float2 *)(q.stat + row * 2) = make_float2(top == kNegInf ? 0.f : top, inv);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] *= inv;
+    if (which == 1) store_row<PSC_F32, N>(&second[wave >> 1][lane * N], x);
+    __syncthreads();
+    if (which == 1 || parts == 1) return;
+    const float lam = d.lam[(int64_t)r * d.lam_stride + out_head];
+    float y[N], squares = 0.f, scale = d.factor;
+    load_row<PSC_F32, N>(&second[wave >> 1][lane * N], y);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        x[j] -= lam * y[j];
+        squares += x[j] * x[j];
+    }
+    if (d.norm) {
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) squares += __shfl_xor(squares, k);
+        scale *= 1.f / sqrtf(squares * (1.f / (2 * D)) + d.eps);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = nobodys ? __builtin_nanf("") : x[j] * (d.norm ? d.norm[lane * N + j] * scale : scale);
+    store_row<DT, N>((typename Element<DT>::type *)q.out + item * (2 * D) + lane * N, x);
 }
 
 // Blocks of a part at least, and blocks of a memory up to which a unit stays whole (a block is 32 tokens of both heads).
@@ -896,7 +913,7 @@ constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || di
 
 // Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel).
 #ifndef KRG
-#define KRG 256
+#define KRG 512
 #endif
 constexpr int64_t kRowGroups = KRG;
 
@@ -924,7 +941,7 @@ int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, c
         else launch_rows(std::false_type());
         PSC_HIP_TRY(hipGetLastError());
         if (p.workgroups) {
-            kv_difference_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * (q.q_heads / 2) + 3) / 4), 256, 0, s>>>(c, q, d);
+            kv_difference_join_kernel<D, DT><<<(uint32_t)(((int64_t)q.nrows * (q.q_heads / 2) + 1) / 2), 256, 0, s>>>(c, q, d);
             PSC_HIP_TRY(hipGetLastError());
         }
     }
