@@ -196,7 +196,7 @@ int psc_kv_append_rotary(const psc_kv_cache *cache, const psc_rotary *rotary, in
         PSC_REQUIRE(q_out_dev != q_dev, "queries cannot be turned in place while keys are appended");
     }
     PSC_REQUIRE(aligned(first_dev, 4) && aligned(positions_dev) && aligned(weights_dev), "misaligned first, positions or weights");
-    PSC_REQUIRE((int64_t)nrows * (v.heads + q_heads) * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows,
+    PSC_REQUIRE((int64_t)nrows * 2 * (v.heads + q_heads) * (v.dim / 8) <= kMostWorkgroups * 256, "%d rows of %d heads of %d are too many for a launch", nrows,
                 v.heads + q_heads, v.dim);
     const KvRows r{k_dev, v_dev, k_row_stride, k_head_stride, v_row_stride, v_head_stride, nrows, nrows / v.batch, offsets_dev, first_dev,
                    positions_dev, weights_dev};

@@ -114,7 +114,7 @@ int psc_rotary_rows(const psc_rotary *rotary, int transposed, int dtype, const v
         return aligned(p) && (nrows == 1 || row * (int64_t)size % 16 == 0) && (heads == 1 || head * (int64_t)size % 16 == 0);
     };
     const bool wide = t.dims % 16 == 0 && head_dim % 8 == 0 && sixteens(x_dev, row_stride, head_stride) && sixteens(out_dev, out_row_stride, out_head_stride);
-    PSC_REQUIRE((int64_t)nrows * heads * (wide ? t.dims / 16 + (head_dim - t.dims + 15) / 16 : head_dim - t.dims / 2) <= kMostWorkgroups * 256,
+    PSC_REQUIRE((int64_t)nrows * 2 * heads * (wide ? t.dims / 16 + (head_dim - t.dims + 15) / 16 : head_dim - t.dims / 2) <= kMostWorkgroups * 256,
                 "%d rows of %d heads of %d are too many for a launch", nrows, heads, head_dim);
     RotaryRows r{};
     r.x = x_dev;

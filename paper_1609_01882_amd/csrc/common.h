@@ -377,7 +377,7 @@ struct RotaryRows {
     int nrows, heads, head_dim, batch, each;
     const int32_t *positions, *offsets, *first;
     int transposed;
-    int group;  // heads that a thread takes
+    int slots;  // a thread takes every slots-th head
 
     __device__ int64_t position_of(int row, bool *nobodys) const
     {
@@ -405,7 +405,9 @@ struct RotaryQueries {
     void *out;
     int64_t row_stride, head_stride;
     int heads;
-    int group;  // kv and query heads that a thread takes
+    int slots;       // a thread takes every slots-th head; 0: none
+    int key_group;   // kv heads that a thread takes
+    int64_t key_items;  // rows times groups of kv heads
 };
 int launch_kv_append_rotary(const KvView &c, int dtype, const KvRows &r, const Rotary &t, const RotaryQueries &q, hipStream_t s);
 

@@ -46,7 +46,8 @@ __device__ __forceinline__ void turn_of(const Rotary &t, int pair, int64_t posit
 }
 
 // ------------------------------------------------------------------------------------------- rows on their own
-// A thread takes 8 pairs (or 16 coordinates behind the turned ones, which are copied) of a row, in every head of a group.
+// A thread takes 8 pairs (or 16 coordinates behind the turned ones, which are copied) of a row, in every `slots`-th head: threads beside it take
+// the row's other pairs, then the heads beside it, so that a wave reads and writes in one piece.
 template <int DT, bool kInterleaved>
 __global__ __launch_bounds__(256) void rotary_kernel(Rotary t, RotaryRows r)
 {
@@ -55,14 +56,14 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rotary t, RotaryRows r)
     const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int chunk = (int)(item % chunks);
     const int64_t rest = item / chunks;
-    const int row = (int)(rest % r.nrows), group = (int)(rest / r.nrows), from = group * r.group, to = min(from + r.group, r.heads);
-    if (from >= r.heads) return;
+    const int from = (int)(rest % r.slots), row = (int)(rest / r.slots);
+    if (row >= r.nrows) return;
     const T *x = (const T *)r.x + row * r.row_stride;
     T *y = (T *)r.out + row * r.out_row_stride;
     if (chunk >= turned) {
         const int at = t.dims + (chunk - turned) * 16;
         const bool second = at + 8 < r.head_dim;
-        for (int h = from; h < to; ++h) {
+        for (int h = from; h < r.heads; h += r.slots) {
             float a[8], b[8];
             load_row<DT, 8>(x + h * r.head_stride + at, a);
             if (second) load_row<DT, 8>(x + h * r.head_stride + at + 8, b);
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rotary t, RotaryRows r)
     }
     const int at0 = kInterleaved ? chunk * 16 : chunk * 8, at1 = kInterleaved ? at0 + 8 : at0 + t.dims / 2;
 #pragma unroll 4
-    for (int h = from; h < to; ++h) {
+    for (int h = from; h < r.heads; h += r.slots) {
         float u[8], v[8], p[8], q[8];
         load_row<DT, 8>(x + h * r.head_stride + at0, u);
         load_row<DT, 8>(x + h * r.head_stride + at1, v);
@@ -112,13 +113,13 @@ __global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows
     const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int place = (int)(item % places);
     const int64_t rest = item / places;
-    const int row = (int)(rest % r.nrows), group = (int)(rest / r.nrows), from = group * r.group, to = min(from + r.group, r.heads);
-    if (from >= r.heads) return;
+    const int from = (int)(rest % r.slots), row = (int)(rest / r.slots);
+    if (row >= r.nrows) return;
     const T *x = (const T *)r.x + row * r.row_stride;
     T *y = (T *)r.out + row * r.out_row_stride;
     if (place >= half) {
         const int at = half + place;
-        for (int h = from; h < to; ++h) y[h * r.out_head_stride + at] = x[h * r.head_stride + at];
+        for (int h = from; h < r.heads; h += r.slots) y[h * r.out_head_stride + at] = x[h * r.head_stride + at];
         return;
     }
     bool nobodys;
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows
     const float s = r.transposed ? -(float)sine : (float)sine, c = (float)cosine;
     const int at0 = t.interleaved ? 2 * place : place, at1 = t.interleaved ? at0 + 1 : at0 + half;
 #pragma unroll 4
-    for (int h = from; h < to; ++h) {
+    for (int h = from; h < r.heads; h += r.slots) {
         const float a = Element<DT>::load(x[h * r.head_stride + at0]), b = Element<DT>::load(x[h * r.head_stride + at1]);
         y[h * r.out_head_stride + at0] = Element<DT>::store(a * c - b * s);
         y[h * r.out_head_stride + at1] = Element<DT>::store(b * c + a * s);
@@ -136,8 +137,9 @@ __global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows
 }
 
 // ------------------------------------------------------------------------------------------- into the memory
-// D / 8 lanes to a row, 8 coordinates to a lane, in every head of a group of the kv heads (whose keys are turned, rounded and written
-// with their values) and the query heads behind them.  A key's products are made in 64 bits and rounded to 32, then to 4: a
+// D / 8 lanes to a row, 8 coordinates to a lane.  First the keys, which are turned, rounded and written with their values: lanes beside each
+// other have rows that follow each other, whose codes lie side by side, in a group of the kv heads.  Then the queries, in every `slots`-th
+// head: lanes beside each other have heads beside each other.  A key's products are made in 64 bits and rounded to 32, then to 4: a
 // coordinate next to a border between two codes comes out on the same side as in any other exact computation.
 template <int DT, int D, bool kInterleaved>
 __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows r, Rotary t, RotaryQueries q)
@@ -146,8 +148,10 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
     typedef typename Element<DT>::type T;
     const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
     const int part = (int)(threadIdx.x % L);
-    const int row = (int)(item % r.nrows), group = (int)(item / r.nrows), from = group * q.group, to = min(from + q.group, c.heads + q.heads);
-    if (from >= to) return;
+    const bool keys = item < q.key_items;
+    const int64_t query = item - q.key_items;
+    const int row = (int)(keys ? item % r.nrows : q.slots ? query / q.slots : r.nrows), from = (int)(keys ? item / r.nrows * q.key_group : q.slots ? query % q.slots : 0);
+    if (row >= r.nrows) return;
     const RowPlace p = place_of(c, r, row);
     const bool nobodys = p.place < 0 || (r.offsets && row >= r.offsets[c.batch]);
     const int64_t position = (int64_t)(r.first ? r.first[p.b] : c.lengths[p.b]) + p.place;
@@ -169,67 +173,82 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
             if (!kInterleaved && !second) s[i] = -s[i];  // (then x cos + other sin on both sides)
         }
     }
-    for (int h = from; h < to; ++h) {
-        if (h < c.heads) {
-            const T *k = (const T *)r.k + row * r.k_stride + h * r.k_head_stride;
-            float x[2][8];
-            load_row<DT, 8>(k + at, x[0]);
-            load_row<DT, 8>((const T *)r.v + row * r.v_stride + h * r.v_head_stride + at, x[1]);
-            if (turned) {
-                if constexpr (kInterleaved) {
+    for (int h = from; h < (keys ? min(from + q.key_group, c.heads) : 0); ++h) {
+        const T *k = (const T *)r.k + row * r.k_stride + h * r.k_head_stride;
+        float x[2][8];
+        load_row<DT, 8>(k + at, x[0]);
+        load_row<DT, 8>((const T *)r.v + row * r.v_stride + h * r.v_head_stride + at, x[1]);
+        if constexpr (kInterleaved) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const double a = x[0][2 * i], b = x[0][2 * i + 1];
-                        x[0][2 * i] = (float)__builtin_fma(a, co[i], -(b * s[i]));
-                        x[0][2 * i + 1] = (float)__builtin_fma(b, co[i], a * s[i]);
-                    }
-                } else {
-                    float o[8];
-                    load_row<DT, 8>(k + other, o);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[0][i] = (float)__builtin_fma((double)x[0][i], co[i], (double)o[i] * s[i]);
-                }
+            for (int i = 0; i < 4; ++i) {
+                const double a = x[0][2 * i], b = x[0][2 * i + 1];
+                const float u = (float)__builtin_fma(a, co[i], -(b * s[i])), v = (float)__builtin_fma(b, co[i], a * s[i]);
+                x[0][2 * i] = turned ? u : x[0][2 * i];
+                x[0][2 * i + 1] = turned ? v : x[0][2 * i + 1];
             }
-            write_token<D>(c, r, p, h, part, x);
         } else {
-            const T *from_q = (const T *)q.q + row * q.row_stride + (h - c.heads) * q.head_stride;
-            float x[8];
-            load_row<DT, 8>(from_q + at, x);
-            if (turned) {
-                if constexpr (kInterleaved) {
+            float o[8];
+            load_row<DT, 8>(k + other, o);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = x[2 * i], b = x[2 * i + 1], sf = (float)s[i], cf = (float)co[i];
-                        x[2 * i] = a * cf - b * sf;
-                        x[2 * i + 1] = b * cf + a * sf;
-                    }
-                } else {
-                    float o[8];
-                    load_row<DT, 8>(from_q + other, o);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = x[i] * (float)co[i] + o[i] * (float)s[i];
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float u = (float)__builtin_fma((double)x[0][i], co[i], (double)o[i] * s[i]);
+                x[0][i] = turned ? u : x[0][i];
             }
-            store_row<DT, 8>((T *)q.out + ((int64_t)row * q.heads + h - c.heads) * D + at, x);
         }
+        write_token<D>(c, r, p, h, part, x);
+    }
+    if (keys) return;
+    // (coordinates behind the turned ones keep their bits: a product with 1 would make a signalling NaN a quiet one)
+    float sf[kPairs], cf[kPairs];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        sf[i] = (float)s[i];
+        cf[i] = (float)co[i];
+    }
+#pragma unroll 4
+    for (int h = from; h < q.heads; h += q.slots) {
+        const T *from_q = (const T *)q.q + row * q.row_stride + h * q.head_stride;
+        float x[8];
+        load_row<DT, 8>(from_q + at, x);
+        if constexpr (kInterleaved) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = x[2 * i], b = x[2 * i + 1];
+                x[2 * i] = turned ? a * cf[i] - b * sf[i] : a;
+                x[2 * i + 1] = turned ? b * cf[i] + a * sf[i] : b;
+            }
+        } else {
+            float o[8];
+            load_row<DT, 8>(from_q + other, o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = turned ? x[i] * cf[i] + o[i] * sf[i] : x[i];
+        }
+        store_row<DT, 8>((T *)q.out + ((int64_t)row * q.heads + h) * D + at, x);
     }
 }
 
-// Heads that a thread takes: so many that enough threads are left to fill the card, 8 at most.
+// Threads to a row's place: a thread takes so many heads that enough threads are left to fill the card, 8 at most.
 constexpr int64_t kThreads = (int64_t)256 * 2048;
-int heads_of_a_thread(int64_t threads_of_a_head, int heads)
+int group_of(int64_t threads_of_a_head, int heads)
 {
     int group = 1;
     while (group < 8 && group < heads && threads_of_a_head * heads / (2 * group) >= kThreads) group *= 2;
     return group;
+}
+int slots_of(int64_t threads_of_a_head, int heads)
+{
+    const int group = group_of(threads_of_a_head, heads);
+    int slots = 1;  // (a power of two: so many heads lie beside each other in a wave)
+    while (slots * group < heads) slots *= 2;
+    return slots;
 }
 
 template <int DT>
 int run_rotary(const Rotary &t, RotaryRows r, bool wide, hipStream_t s)
 {
     const int64_t places = wide ? t.dims / 16 + (r.head_dim - t.dims + 15) / 16 : t.dims / 2 + r.head_dim - t.dims;
-    r.group = heads_of_a_thread(places * r.nrows, r.heads);
-    const int64_t blocks = (places * r.nrows * ((r.heads + r.group - 1) / r.group) + 255) / 256;
+    r.slots = slots_of(places * r.nrows, r.heads);
+    const int64_t blocks = (places * r.nrows * r.slots + 255) / 256;
     if (!wide) rotary_single_kernel<DT><<<(uint32_t)blocks, 256, 0, s>>>(t, r);
     else if (t.interleaved) rotary_kernel<DT, true><<<(uint32_t)blocks, 256, 0, s>>>(t, r);
     else rotary_kernel<DT, false><<<(uint32_t)blocks, 256, 0, s>>>(t, r);
@@ -240,9 +259,11 @@ int run_rotary(const Rotary &t, RotaryRows r, bool wide, hipStream_t s)
 template <int DT, int D>
 int run_append_rotary(const KvView &c, const KvRows &r, const Rotary &t, RotaryQueries q, hipStream_t s)
 {
-    const int heads = c.heads + q.heads;
-    q.group = heads_of_a_thread((int64_t)r.nrows * (D / 8), heads);
-    const int64_t blocks = ((int64_t)r.nrows * ((heads + q.group - 1) / q.group) * (D / 8) + 255) / 256;
+    const int64_t threads = (int64_t)r.nrows * (D / 8);
+    q.key_group = group_of(threads, c.heads);
+    q.key_items = (int64_t)r.nrows * ((c.heads + q.key_group - 1) / q.key_group);
+    q.slots = q.heads ? slots_of(threads, q.heads) : 0;
+    const int64_t blocks = ((q.key_items + (int64_t)r.nrows * q.slots) * (D / 8) + 255) / 256;
     if (t.interleaved) kv_append_rotary_kernel<DT, D, true><<<(uint32_t)blocks, 256, 0, s>>>(c, r, t, q);
     else kv_append_rotary_kernel<DT, D, false><<<(uint32_t)blocks, 256, 0, s>>>(c, r, t, q);
     PSC_HIP_TRY(hipGetLastError());
