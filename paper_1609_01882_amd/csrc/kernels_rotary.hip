@@ -141,6 +141,22 @@ __global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows
 // other have rows that follow each other, whose codes lie side by side, in a group of the kv heads.  Then the queries, in every `slots`-th
 // head: lanes beside each other have heads beside each other.  A key's products are made in 64 bits and rounded to 32, then to 4: a
 // coordinate next to a border between two codes comes out on the same side as in any other exact computation.
+//
+// The way from load to load -- offsets, first, lengths, table -- is long beside the work of a lane, so the first head's coordinates are asked
+// for before it, and the next head's before a head is worked on.
+template <int DT>
+struct RawRow {  // 8 coordinates as they lie in memory
+    uint32_t w[DT == PSC_F32 ? 8 : 4];
+    __device__ __forceinline__ void load(const void *p) { __builtin_memcpy(w, __builtin_assume_aligned(p, 16), sizeof w); }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        typename Element<DT>::type t[8];
+        __builtin_memcpy(t, w, sizeof t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = Element<DT>::load(t[i]);
+    }
+};
+
 template <int DT, int D, bool kInterleaved>
 __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows r, Rotary t, RotaryQueries q)
 {
@@ -152,14 +168,26 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
     const int64_t query = item - q.key_items;
     const int row = (int)(keys ? item % r.nrows : q.slots ? query / q.slots : r.nrows), from = (int)(keys ? item / r.nrows * q.key_group : q.slots ? query % q.slots : 0);
     if (row >= r.nrows) return;
-    const RowPlace p = place_of(c, r, row);
-    const bool nobodys = p.place < 0 || (r.offsets && row >= r.offsets[c.batch]);
-    const int64_t position = (int64_t)(r.first ? r.first[p.b] : c.lengths[p.b]) + p.place;
     // the lane's pairs; of pairs half of `dims` apart it has one side, and reads the other side too
     constexpr int kPairs = kInterleaved ? 4 : 8;
     const int at = part * 8, half = t.dims / 2;
     const bool turned = at < t.dims, second = !kInterleaved && at >= half;
     const int other = kInterleaved || !turned ? at : second ? at - half : at + half;
+
+    const T *k = (const T *)r.k + row * r.k_stride, *v = (const T *)r.v + row * r.v_stride, *from_q = (const T *)q.q + row * q.row_stride;
+    const int to = keys ? min(from + q.key_group, c.heads) : q.heads;
+    RawRow<DT> mine, side, value;
+    const auto load = [&](int h) {
+        const T *p = keys ? k + h * r.k_head_stride : from_q + h * q.head_stride;
+        mine.load(p + at);
+        if (!kInterleaved) side.load(p + other);
+        if (keys) value.load(v + h * r.v_head_stride + at);
+    };
+    if (from < to) load(from);
+
+    const RowPlace p = place_of(c, r, row);
+    const bool nobodys = p.place < 0 || (r.offsets && row >= r.offsets[c.batch]);
+    const int64_t position = (int64_t)(r.first ? r.first[p.b] : c.lengths[p.b]) + p.place;
     double s[kPairs], co[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
@@ -173,43 +201,45 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
             if (!kInterleaved && !second) s[i] = -s[i];  // (then x cos + other sin on both sides)
         }
     }
-    for (int h = from; h < (keys ? min(from + q.key_group, c.heads) : 0); ++h) {
-        const T *k = (const T *)r.k + row * r.k_stride + h * r.k_head_stride;
-        float x[2][8];
-        load_row<DT, 8>(k + at, x[0]);
-        load_row<DT, 8>((const T *)r.v + row * r.v_stride + h * r.v_head_stride + at, x[1]);
-        if constexpr (kInterleaved) {
+    if (keys) {
+        for (int h = from; h < to; ++h) {
+            float x[2][8], o[8];
+            mine.get(x[0]);
+            value.get(x[1]);
+            side.get(o);
+            if (h + 1 < to) load(h + 1);
+            // (coordinates behind the turned ones keep their bits: a product with 1 would make a signalling NaN a quiet one)
+            if constexpr (kInterleaved) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const double a = x[0][2 * i], b = x[0][2 * i + 1];
-                const float u = (float)__builtin_fma(a, co[i], -(b * s[i])), v = (float)__builtin_fma(b, co[i], a * s[i]);
-                x[0][2 * i] = turned ? u : x[0][2 * i];
-                x[0][2 * i + 1] = turned ? v : x[0][2 * i + 1];
-            }
-        } else {
-            float o[8];
-            load_row<DT, 8>(k + other, o);
+                for (int i = 0; i < 4; ++i) {
+                    const double a = x[0][2 * i], b = x[0][2 * i + 1];
+                    const float u = (float)__builtin_fma(a, co[i], -(b * s[i])), w = (float)__builtin_fma(b, co[i], a * s[i]);
+                    x[0][2 * i] = turned ? u : x[0][2 * i];
+                    x[0][2 * i + 1] = turned ? w : x[0][2 * i + 1];
+                }
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float u = (float)__builtin_fma((double)x[0][i], co[i], (double)o[i] * s[i]);
-                x[0][i] = turned ? u : x[0][i];
+                for (int i = 0; i < 8; ++i) {
+                    const float u = (float)__builtin_fma((double)x[0][i], co[i], (double)o[i] * s[i]);
+                    x[0][i] = turned ? u : x[0][i];
+                }
             }
+            write_token<D>(c, r, p, h, part, x);
         }
-        write_token<D>(c, r, p, h, part, x);
+        return;
     }
-    if (keys) return;
-    // (coordinates behind the turned ones keep their bits: a product with 1 would make a signalling NaN a quiet one)
     float sf[kPairs], cf[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
         sf[i] = (float)s[i];
         cf[i] = (float)co[i];
     }
-#pragma unroll 4
-    for (int h = from; h < q.heads; h += q.slots) {
-        const T *from_q = (const T *)q.q + row * q.row_stride + h * q.head_stride;
-        float x[8];
-        load_row<DT, 8>(from_q + at, x);
+#pragma unroll 2
+    for (int h = from; h < to; h += q.slots) {
+        float x[8], o[8];
+        mine.get(x);
+        side.get(o);
+        if (h + q.slots < to) load(h + q.slots);
         if constexpr (kInterleaved) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -218,8 +248,6 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
                 x[2 * i + 1] = turned ? b * cf[i] + a * sf[i] : b;
             }
         } else {
-            float o[8];
-            load_row<DT, 8>(from_q + other, o);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = turned ? x[i] * cf[i] + o[i] * sf[i] : x[i];
         }
