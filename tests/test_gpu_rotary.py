@@ -75,7 +75,7 @@ def test_rows_of_sequences():
         at[lo:hi] = int(first[b]) + np.arange(hi - lo)
     got = rope(x, first=first, offsets=offsets)
     want = L.turned(x.double().cpu().numpy(), at, rope.frequencies, 64, False)
-    want[:2], want[19:] = x[:2].cpu(), x[19:].cpu()
+    want[:2], want[19:] = x[:2].cpu().numpy(), x[19:].cpu().numpy()
     assert L.finite_or_same(got.double().cpu().numpy(), want, L.turned_tolerance(x.double().cpu().numpy(), 64, False, 1.0, "f32")) <= 1.0
     assert torch.equal(got[:2], x[:2]) and torch.equal(got[19:], x[19:])
     # without a first: places; without offsets: equal parts
