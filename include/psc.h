@@ -10,7 +10,7 @@
  * per query are returned; plus the inverted-file variant with residual codes
  * (Section 4.3) and the all-against-all k-NN-graph mode (Section 5).  Next to it (psc_kv_*): attention
  * over a language model's keys and values held in 4 bits, the same comparison of full-precision queries
- * with compressed vectors.
+ * with compressed vectors, and what stands around it in a layer (psc_rotary_*, psc_residual_norm_*).
  *
  * General rules
  *   - Pointers named *_dev are device (HBM) pointers, *_host are host pointers.
@@ -39,8 +39,8 @@
  *     psc_last_error() gives a message for the last failure on the calling thread.
  *     Nothing throws or aborts across this boundary.
  *   - n = 0 or nq = 0 succeed; with n = 0 every result row is padding.
- *   - The psc_kv_* calls take no index and keep no state; several may run at once on different streams as
- *     long as none writes what another uses.
+ *   - The psc_kv_*, psc_rotary_* and psc_residual_norm_* calls take no index and keep no state; several may
+ *     run at once on different streams as long as none writes what another uses.
  */
 #ifndef PSC_H
 #define PSC_H
@@ -525,7 +525,7 @@ int psc_kv_evict(const psc_kv_cache *cache, const float *weights_dev, const int3
  * weights after_dev, before_dev [width] of weight_dtype (float32 or the block's).  Rows x_stride, y_stride, gate_stride
  * elements apart, coordinates contiguous, no alignment beyond the type's.  gate_dev has gate_rows rows, of
  * which each serves rows / gate_rows consecutive rows: one to a row, to a sequence of equal lengths, or one to all.
- * width 1 .. 16384.  Everything between loads and stores is float32. */
+ * width 1 .. 16384, rows under 2^30.  Everything between loads and stores is float32. */
 #define PSC_GATE_PLAIN 0
 #define PSC_GATE_SIGMOID 1
 #define PSC_GATE_SILU 2

@@ -36,7 +36,7 @@ uint64_t turns_of(double radians)
 int check_norm(const psc_residual_norm *n, ResidualNorm *p)
 {
     PSC_REQUIRE(n != nullptr, "null residual_norm");
-    PSC_REQUIRE(n->rows >= 0, "%d rows", n->rows);
+    PSC_REQUIRE(n->rows >= 0 && n->rows < 1 << 30, "%d rows: under 2^30", n->rows);
     PSC_REQUIRE(n->width >= 1 && n->width <= PSC_MAX_NORM_WIDTH, "width must be 1 to %d, got %d", PSC_MAX_NORM_WIDTH, n->width);
     PSC_TRY(check_dtype(n->stream_dtype));
     PSC_TRY(check_dtype(n->block_dtype));

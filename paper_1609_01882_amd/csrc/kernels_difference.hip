@@ -3,6 +3,11 @@
 // kv heads 2j and 2j + 1 are a pair: each has keys of its own, their values lie side by side (2 D wide), and an output head is
 //   o = softmax(s q1 K1) V - lam softmax(s q2 K2) V,   then o * rsqrt(mean o^2 + eps) * norm * factor.
 // A wave has both maps of its rows, so that the memory is read once, and values are expanded once for both.
+//
+// What it is bound by.  A few rows: reading the memory, 4.8 TB/s (8 sequences of 40 to 100 thousand tokens x 8 heads x 128, 618 MB in 128 us;
+// 146 with the codes through registers and one wave to a SIMD).  Many rows: vector instructions and the way from one product's
+// operands to the next product: 2048 rows of 32 query heads over 16384 tokens 940 to 1010 us by card, 770 to 830 TFLOP/s (through registers
+// 1768; every wave with expansions of its own 1178).
 #include <algorithm>
 #include <type_traits>
 
@@ -13,7 +18,7 @@ namespace {
 
 // Codes, scales and positions of a block of 32 tokens on their way through LDS: a wave has kStages places of its own, into which loads write
 // past the registers, so that the blocks after the one that is worked on are under way whatever the registers hold.  No other wave
-// reads them: no barrier, the wave counts its loads.  Each load moves 16 bytes (scales, positions: 4) of every lane to consecutive places; which
+// reads them: no barrier, the wave counts its loads (the first to return are the first asked for).  Each load moves 16 bytes (scales, positions: 4) of every lane to consecutive places; which
 // bytes a lane asks for is chosen so that what it reads back lies without conflicts over the banks:
 //   keys      in the order in which the lanes read them (coordinates g D/4 ... of token i, as for kv_device.h's load_keys)
 //   values    a row of D / 2 bytes to a token, the four tokens of g turned by g (D = 64: g / 2) places
@@ -252,7 +257,7 @@ struct Difference {
     }
 };
 
-// Waves of a SIMD that the registers are to leave room for.
+// Waves of a SIMD that the registers are to leave room for (D = 64 with 16 rows: three waves spill, 1 x 700 tokens 15.5 us instead of 12.7).
 constexpr int difference_waves(int dim, int dtype, int row_tiles)
 {
     if (dtype == PSC_F32) return dim == 64 ? 2 : 1;
@@ -525,7 +530,8 @@ __global__ __launch_bounds__(256, difference_waves(D, DT, RT)) void kv_differenc
     __shared__ __attribute__((aligned(16))) PairLds<D, RT, kPos> lds;
     const int pairs = c.heads / 2;
     if constexpr (!kParts) {
-        const int b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, m0 = (int)blockIdx.x * 16 * RT;
+        // (the last rows first: they see the most)
+        const int b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, m0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 16 * RT;
         const RowSet s = rows_of(c, q, b);
         if (q.offsets && m0 == 0) {
             if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
@@ -552,8 +558,10 @@ __global__ __launch_bounds__(256, difference_waves(D, DT, RT)) void kv_differenc
 // ------------------------------------------------------------------------------------------- many rows
 // Where there are rows for it, a wave has 16 RT rows of its own and a workgroup's four waves take every block together: each expands a
 // quarter of the block's keys and values -- sixteen tokens of a head -- into LDS as the operands of the products, and all four read them.  Two
-// buffers in turn: one barrier to a block.  A wave's expansions (192 vector instructions to a block of 128 coordinates, of 390 altogether) become 48.
-// 16 RT rows past the last one take part in the expansions alone.
+// buffers in turn: one barrier to a block.  A wave's expansions (192 vector instructions to a block of 128 coordinates, of 390
+// altogether) become 48.  Vector instructions are then issued in 48 % of the cycles, the matrix cores busy in 34 %, LDS in 45 %: none of them, but
+// the way through them bounds it, with the two waves to a SIMD that the registers leave room for.  32 rows of 128 coordinates
+// to a wave do not fit (6296 us).
 template <int D>
 struct Operands {
     u32x4 keys[2][2][D / 32][64];      // [map][sixteen][32 coordinates]: a lane's operand of a product
@@ -659,7 +667,8 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
     const int pairs = c.heads / 2, b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const RowSet s = rows_of(c, q, b);
-    const int group0 = (int)blockIdx.x * 64 * RT, m_all = s.rows * q.group, group_end = min(group0 + 64 * RT, m_all);
+    // (the last rows first: they see the most)
+    const int group0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 64 * RT, m_all = s.rows * q.group, group_end = min(group0 + 64 * RT, m_all);
     if (q.offsets && group0 == 0) {
         if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
         difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
@@ -823,10 +832,10 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
 }
 
 // Joins the parts of an output head's two maps, a wave to each: its lanes take a part's maximum and sum each (64 parts at a time), then
-// 2 D / 64 coordinates of every part; the second map's wave hands its row to the first's.  Sequences without a block have no part: zeros.  What
-// bounds it is the way from load to load and through its instructions, which no workgroup runs twice: 8 x 16 heads of 128 with
-// 16 parts to each 13.7 us where a wave had both maps one after the other and every fourth part to a quarter of its lanes (10.7 kB
-// of instructions), 17.0 with the maps side by side (12 kB).
+// 2 D / 64 coordinates of every part, sixteen parts on their way; the second map's wave hands its row to the first's.  Sequences
+// without a block have no part: zeros.  What bounds it is the way from load to load and through its instructions, which no workgroup runs
+// twice.  8 x 16 heads of 128 with 16 parts to each: 8.7 us; a wave with both maps, and every fourth part to a quarter of its lanes, 13.7 one
+// map after the other, 17.0 side by side; four parts on their way 13.0.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQueries q, KvDifference d)
 {
@@ -905,17 +914,17 @@ __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQue
     store_row<DT, N>((typename Element<DT>::type *)q.out + item * (2 * D) + lane * N, x);
 }
 
-// Blocks of a part at least, and blocks of a memory up to which a unit stays whole (a block is 32 tokens of both heads).
+// Blocks of a part at least, and blocks of a memory up to which a unit stays whole (a block is 32 tokens of both heads: half of what they are
+// for kv_attention_kernel).
 constexpr int64_t kLeastBlocks = 8, kFewBlocks = 32;
 
 // Rows of a wave, in sixteens, at most.
 constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || dim == 128 ? 1 : 2; }
 
-// Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel).
-#ifndef KRG
-#define KRG 512
-#endif
-constexpr int64_t kRowGroups = KRG;
+// Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel): two to a compute unit.  8 heads x 128, us with rows of their
+// own and without: 512 rows x 4 over 8000 tokens (512 workgroups) 444 and 485, 2048 over 8000 (512) 509 and 578, 8192 of 8192 (2048) 1102 and 1320;
+// 2048 of 2048 (512) 140 and 138, 3000 over 8000 (752) 830 and 790; 1024 over 8000 (256) 385 and 315, 256 x 4 over 8000 (256) 382 and 287.
+constexpr int64_t kRowGroups = 512;
 
 template <int DT, int D>
 int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, const KvPlan &p, const float *given, float *received, hipStream_t s)

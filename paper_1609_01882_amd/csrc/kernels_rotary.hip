@@ -7,6 +7,9 @@
 // quarter turn after the nearest quarters are taken off goes into Taylor's series in 64 bits (|t| <= pi/4: sine to t^15, off by
 // 5e-17, cosine to t^16, off by 2e-18).  64-bit operations issue at the rate of single 32-bit ones here, and a thread uses its sines and
 // cosines for several heads.
+//
+// Bound by HBM: 16384 rows of 32 heads x 128 bfloat16 in 54 us, 5.0 TB/s (67 with rows, not heads, beside each other in a wave); 27 thousand rows
+// of 32 query heads and 8 kv heads x 128 float16 into the memory in 133 us, 4.5 TB/s (159 without the loads ahead).
 #include "kv_device.h"
 
 namespace psc {

@@ -172,7 +172,7 @@ def _norm(**other):
     return _Norm(*f.values())
 
 
-BAD_NORMS = [dict(rows=-1), dict(width=0), dict(width=16385), dict(stream_dtype=3), dict(block_dtype=-1), dict(weight_dtype=1), dict(weight_dtype=5), dict(stream_dtype=1),
+BAD_NORMS = [dict(rows=-1), dict(rows=1 << 30, gate=None), dict(width=0), dict(width=16385), dict(stream_dtype=3), dict(block_dtype=-1), dict(weight_dtype=1), dict(weight_dtype=5), dict(stream_dtype=1),
              dict(stream_dtype=0, block_dtype=2), dict(x=None, y=None), dict(y=None), dict(y=None, gate=None), dict(y=None, after=None), dict(activation=3), dict(activation=-1),
              dict(gate_rows=4), dict(gate_rows=0), dict(gate_rows=-3), dict(x=A + 1), dict(y=A + 1), dict(gate=A + 1), dict(after=A + 2), dict(before=A + 2),
              dict(x_stride=1 << 40), dict(gate_stride=-(1 << 40)), dict(residual_scale=float("nan")), dict(block_scale=float("inf")), dict(eps=-1e-6), dict(eps=float("nan"))]
