@@ -237,21 +237,39 @@ constexpr size_t weights_lds(int lanes) { return (size_t)lanes * NV * 64; }
 #define PSC_EACH                        \
     _Pragma("unroll") for (int v = 0; v < NV; ++v) _Pragma("unroll") for (int i = 0; i < 8; ++i)
 
-// The gate g's factor and its derivative, from s = sigmoid(g) (which a plain gate does not ask for).
+// Multiplies by the gate g's factor and by its derivative, from s = sigmoid(g) (which a plain gate does not ask for): one of three loops, not a
+// choice for every coordinate.
 struct Gate {
     bool plain, silu;
     __device__ explicit Gate(int activation) : plain(activation == PSC_GATE_PLAIN), silu(activation == PSC_GATE_SILU) {}
-    __device__ float factor(float g, float s) const { return plain ? g : silu ? g * s : s; }
-    __device__ float slope(float g, float s) const
-    {
-        const float of_sigmoid = s * (1.f - s);
-        return plain ? 1.f : silu ? __builtin_fmaf(g, of_sigmoid, s) : of_sigmoid;
-    }
     template <int TB, int NV>
     __device__ __forceinline__ void sigmoids(const Eight<TB> (&g)[NV], float (&s)[NV][8]) const
     {
-        if (plain) PSC_EACH s[v][i] = 0.f;
-        else PSC_EACH s[v][i] = sigmoid(g[v][i]);
+        if (!plain) PSC_EACH s[v][i] = sigmoid(g[v][i]);
+    }
+    template <int TB, int NV>
+    __device__ __forceinline__ void factors(const Eight<TB> (&g)[NV], float (&f)[NV][8]) const
+    {
+        if (plain) {
+            PSC_EACH f[v][i] = g[v][i];
+            return;
+        }
+        PSC_EACH f[v][i] = sigmoid(g[v][i]);
+        if (silu) PSC_EACH f[v][i] *= g[v][i];
+    }
+    template <int TB, int NV>
+    __device__ __forceinline__ void open(float (&x)[NV][8], const Eight<TB> (&g)[NV], const float (&s)[NV][8]) const
+    {
+        if (plain) PSC_EACH x[v][i] *= g[v][i];
+        else if (silu) PSC_EACH x[v][i] *= g[v][i] * s[v][i];
+        else PSC_EACH x[v][i] *= s[v][i];
+    }
+    template <int TB, int NV>
+    __device__ __forceinline__ void slope(float (&x)[NV][8], const Eight<TB> (&g)[NV], const float (&s)[NV][8]) const
+    {
+        if (plain) return;
+        if (silu) PSC_EACH x[v][i] *= __builtin_fmaf(g[v][i], s[v][i] * (1.f - s[v][i]), s[v][i]);
+        else PSC_EACH x[v][i] *= s[v][i] * (1.f - s[v][i]);
     }
 };
 
@@ -326,9 +344,9 @@ __global__ __launch_bounds__(kThreads) void residual_norm_kernel(ResidualNorm p,
                 PSC_EACH h[v][i] = h[v][i] * root_y * w[v][i];
             }
             if (p.gate) {
-                float s[NV][8];
-                gate.sigmoids(now.g, s);
-                PSC_EACH h[v][i] *= gate.factor(now.g[v][i], s[v][i]);
+                float f[NV][8];
+                gate.factors(now.g, f);
+                PSC_EACH h[v][i] *= f[v][i];
             }
             PSC_EACH h[v][i] *= p.block_scale;
             if (p.x) PSC_EACH h[v][i] = __builtin_fmaf(p.residual_scale, now.x[v][i], h[v][i]);
@@ -437,12 +455,15 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
             to.load(p, &d, col, row, kShared ? gate : row);
         };
         if (kAhead && begin < end) load(begin, now);
-        Eight<TB> g[NV];
-        float s_of_gate[NV][8];
-        if constexpr (kShared) {  // one for all of these rows
+        float of_gate[NV][8];  // its factors, where all of these rows share it; else the sigmoids of a row's
+        const auto load_gate = [&](Eight<TB> (&g)[NV]) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) load_eight<TB>(p.gate, (int64_t)gate * p.gate_stride + col.at(v), col.template count<NV>(v), col.tail, g[v]);
-            act.sigmoids(g, s_of_gate);
+        };
+        if constexpr (kShared) {
+            Eight<TB> g[NV];
+            load_gate(g);
+            act.factors(g, of_gate);
         }
         for (int row0 = begin; row0 < end; row0 += rows_at_once) {
             const int64_t row = min(row0 + mine, end - 1);
@@ -451,13 +472,18 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
             else load(row0, now);
             const float root_y = now.stat.x, root_h = now.stat.y;
             float grad[NV][8];  // of h, then of u and what lies before it
+            Eight<TB> g[kShared ? 1 : NV];
             if constexpr (!kShared) {
                 if (p.gate) {
 #pragma unroll
                     for (int v = 0; v < NV; ++v) g[v] = now.g[v];
-                    act.sigmoids(g, s_of_gate);
+                    act.sigmoids(g, of_gate);
                 }
             }
+            const auto open = [&](float (&x)[NV][8]) __attribute__((always_inline)) {
+                if constexpr (kShared) PSC_EACH x[v][i] *= of_gate[v][i];
+                else act.open(x, g, of_gate);
+            };
             if (d.dz) {
                 float normed[NV][8], w[NV][8], s = 0.f;
                 if (p.y) {
@@ -466,7 +492,7 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
                         weights.get(p, col, 0, w);
                         PSC_EACH normed[v][i] = normed[v][i] * root_y * w[v][i];
                     }
-                    if (p.gate) PSC_EACH normed[v][i] *= act.factor(g[v][i], s_of_gate[v][i]);
+                    if (p.gate) open(normed);
                     PSC_EACH normed[v][i] *= p.block_scale;
                     if (p.x) PSC_EACH normed[v][i] = __builtin_fmaf(p.residual_scale, now.x[v][i], normed[v][i]);
                 } else {
@@ -506,10 +532,10 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
                         const float counts = there ? 1.f : 0.f;
                         PSC_EACH dg[v][i] = __builtin_fmaf(t[v][i], counts, dg[v][i]);
                     } else if (d.dgate && there) {
-                        PSC_EACH t[v][i] *= act.slope(g[v][i], s_of_gate[v][i]);
+                        act.slope(t, g, of_gate);
                         store_vectors<TB>(d.dgate, row, col, t);
                     }
-                    PSC_EACH grad[v][i] *= act.factor(g[v][i], s_of_gate[v][i]);
+                    open(grad);
                 }
                 if (p.after) {
                     float s = 0.f, t[NV][8];
@@ -536,7 +562,10 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
                     if (d.split > 1) {
                         store_vectors<PSC_F32>(d.gate_parts, (int64_t)blockIdx.x, col, dg);
                     } else {
-                        PSC_EACH dg[v][i] *= act.slope(g[v][i], s_of_gate[v][i]);
+                        Eight<TB> g[NV];
+                        load_gate(g);
+                        act.sigmoids(g, of_gate);
+                        act.slope(dg, g, of_gate);
                         store_vectors<TB>(d.dgate, gate, col, dg);
                     }
                 }
@@ -584,9 +613,12 @@ __global__ __launch_bounds__(256) void residual_norm_sums_kernel(ResidualNorm p,
         if (p.weight_f32) ((float *)to)[column] = x;
         else ((typename Stored<TB>::type *)to)[column] = Stored<TB>::store(x);
     } else {
-        const Gate act(p.activation);
         const float g = Stored<TB>::load(((const typename Stored<TB>::type *)p.gate)[(int64_t)(which - 2) * p.gate_stride + column]);
-        ((typename Stored<TB>::type *)d.dgate)[(int64_t)(which - 2) * p.width + column] = Stored<TB>::store(x * act.slope(g, act.plain ? 0.f : sigmoid(g)));
+        if (p.activation != PSC_GATE_PLAIN) {
+            const float s = sigmoid(g), of_sigmoid = s * (1.f - s);
+            x *= p.activation == PSC_GATE_SILU ? __builtin_fmaf(g, of_sigmoid, s) : of_sigmoid;
+        }
+        ((typename Stored<TB>::type *)d.dgate)[(int64_t)(which - 2) * p.width + column] = Stored<TB>::store(x);
     }
 }
 
