@@ -6,7 +6,7 @@
 //
 // What it is bound by.  A few rows: reading the memory, 4.8 TB/s (8 sequences of 40 to 100 thousand tokens x 8 heads x 128, 618 MB in 128 us;
 // 146 with the codes through registers and one wave to a SIMD).  Many rows: vector instructions and the way from one product's
-// operands to the next product: 2048 rows of 32 query heads over 16384 tokens 940 to 1010 us by card, 770 to 830 TFLOP/s (through registers
+// operands to the next product: 2048 rows of 32 query heads over 16384 tokens 925 to 1050 us by card, 740 to 840 TFLOP/s (through registers
 // 1768; every wave with expansions of its own 1178).
 #include <algorithm>
 #include <type_traits>
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(256, difference_waves(D, DT, RT)) void kv_differenc
 // Where there are rows for it, a wave has 16 RT rows of its own and a workgroup's four waves take every block together: each expands a
 // quarter of the block's keys and values -- sixteen tokens of a head -- into LDS as the operands of the products, and all four read them.  Two
 // buffers in turn: one barrier to a block.  A wave's expansions (192 vector instructions to a block of 128 coordinates, of 390
-// altogether) become 48.  Vector instructions are then issued in 48 % of the cycles, the matrix cores busy in 34 %, LDS in 45 %: none of them, but
+// altogether) become 48.  Vector instructions are then issued in 48 % of the cycles, the matrix cores busy in 36 %, LDS in 48 %: none of them, but
 // the way through them bounds it, with the two waves to a SIMD that the registers leave room for.  32 rows of 128 coordinates
 // to a wave do not fit (6296 us).
 template <int D>
