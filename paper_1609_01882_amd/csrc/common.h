@@ -452,6 +452,7 @@ struct KvDifference {
     int64_t lam_stride;
     const float *norm;   // [2 dim], or null
     float eps, factor;
+    int few = 0, most = 0x7fffffff;  // rows (times query heads) of a sequence: those with more than `few`, or up to `most`
 };
 KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered,
                           bool weights);

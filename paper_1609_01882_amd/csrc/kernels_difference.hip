@@ -537,7 +537,7 @@ __global__ __launch_bounds__(256, difference_waves(D, DT, RT)) void kv_differenc
             if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
             difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
         }
-        if (m0 >= s.rows * q.group) return;
+        if (m0 >= s.rows * q.group || s.rows * q.group > d.most) return;
         const Blocks blocks = blocks_of(q, s.n, s.first_pos + m0 / q.group, s.first_pos + (min(m0 + 16 * RT, s.rows * q.group) - 1) / q.group);
         attend_pair<D, DT, RT, kPos>(c, q, d, s, b, pair, m0, blocks, 0, blocks.count(), -1, lds);
     } else {
@@ -673,7 +673,7 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
         if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
         difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
     }
-    if (group0 >= m_all) return;
+    if (group0 >= m_all || m_all <= d.few) return;  // (few: left to kv_difference_kernel)
     const int m0 = group0 + wave * 16 * RT, m_end = min(m0 + 16 * RT, m_all);
     const bool some = m0 < m_all;
     const int lo_pos = s.first_pos + min(m0, m_all - 1) / q.group, hi_pos = s.first_pos + (m_end - 1) / q.group;
@@ -935,7 +935,12 @@ int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, c
         const auto launch = [&](auto rt, auto pos) {
             if constexpr (DT != PSC_F32) {
                 if (p.own_rows) {
-                    kv_difference_rows_kernel<D, DT, kMost, pos.value><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, d);
+                    // of a batch with rows of any number, sequences of one tile go to a workgroup whose waves share out the tokens
+                    KvDifference mine = d;
+                    mine.few = q.offsets && c.batch > 1 ? 16 : 0;
+                    kv_difference_rows_kernel<D, DT, kMost, pos.value><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, mine);
+                    mine.most = mine.few;
+                    if (mine.few) kv_difference_kernel<D, DT, 1, pos.value, false><<<dim3(1, 1, groups), 256, 0, s>>>(c, q, mine);
                     return;
                 }
             }
@@ -971,7 +976,8 @@ KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, 
     if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
     const int most = 64 * most_row_tiles(dtype, c.dim);
     const int64_t groups = (m + most - 1) / most;
-    p.own_rows = dtype != PSC_F32 && groups * c.batch * pairs >= kRowGroups && m > most / 2;
+    // (by the rows that there are, not by the most that a sequence may have: single tokens beside a prompt do not fill workgroups)
+    p.own_rows = dtype != PSC_F32 && nrows * group * pairs >= kRowGroups * most && m > most / 2;
     if (p.own_rows) p.row_groups = groups;
     const int64_t units = p.row_groups * c.batch * pairs;
     const int waves = difference_waves(c.dim, dtype, p.row_tiles);  // workgroups to a compute unit

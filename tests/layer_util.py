@@ -36,22 +36,52 @@ def turned_tolerance(x, dims, interleaved, factor, dtype):
 
 
 def difference(q, lam, buffers, table, lengths, offsets, first, positions, scale, causal, window, sinks, norm, eps, factor, dtype):
-    """(out, lse, received) in float64 and the tolerances of each.  q [rows, q_heads, dim] float64, lam [rows, q_heads / 2]."""
-    heads, dim = buffers[0].shape[1], q.shape[2]
-    group = q.shape[1] // heads
-    pos = None if positions is None else np.repeat(positions[:, 0::2], 2, axis=1)
-    # the maps: the attention of each key head over either head's values
-    maps, tols = [], []
-    for value in (0, 1):
-        swapped = [buffers[0], buffers[1]] + [np.repeat(v[:, value::2], 2, axis=1) for v in buffers[2:]]
-        (out, lse, got), (tol_out, tol_lse, tol_got) = U.attend(q, swapped, table, lengths, offsets, first, pos, scale, causal, window, sinks,
-                                                                 "f32" if dtype == "f32" else dtype)
-        maps.append(out)
-        # without the output's own rounding, which comes once, at the end
-        tols.append(np.maximum(tol_out - 1.01 * UNIT[dtype] * np.abs(out), 0.0) + 4 * EPS32 * np.abs(out))
-    rows = q.shape[0]
-    o = np.concatenate(maps, -1).reshape(rows, heads // 2, 2, group, 2 * dim)
-    t = np.concatenate(tols, -1).reshape(rows, heads // 2, 2, group, 2 * dim)
+    """(out, lse, received) in float64 and the tolerances of each.  q [rows, q_heads, dim] float64, lam [rows, q_heads / 2].  The maps' own
+    tolerances are those of `kv_util.attend`."""
+    heads, page, dim = buffers[0].shape[1], buffers[0].shape[2], q.shape[2]
+    group, slots, rows = q.shape[1] // heads, table.shape[1] * page, q.shape[0]
+    unit_p = torch.finfo(torch.float16).eps / 2
+    unit_p = unit_p ** 2 if dtype == "f32" else unit_p
+    o, t = (np.zeros((rows, heads // 2, 2, group, 2 * dim)) for _ in range(2))
+    lse, tol_lse = np.full((rows, heads, group), -np.inf), np.zeros((rows, heads, group))
+    got, tol_got = (np.zeros((len(lengths), heads // 2, slots)) for _ in range(2))
+    for b in range(len(lengths)):
+        n, mine = min(int(lengths[b]), slots), slice(int(offsets[b]), int(offsets[b + 1]))
+        count = mine.stop - mine.start
+        if n <= 0 or count == 0:
+            continue
+        pos_q = (n - count if first is None else int(first[b])) + np.arange(count)
+        for j in range(heads // 2):
+            held = [U.held(buffers, table, b, 2 * j + w, n) for w in (0, 1)]
+            v, there = np.concatenate([x[1] for x in held], -1), held[0][2]
+            pos_k = np.arange(n) if positions is None else positions[b, 2 * j, :n].astype(np.int64)
+            sees = np.broadcast_to(there, (count, n)).copy()
+            if causal:
+                sees &= pos_k <= pos_q[:, None]
+            if window:
+                sees &= (pos_q[:, None] - pos_k < window) | (pos_k < sinks)
+            sees, some = sees[:, None], sees.any(-1)[:, None]                       # of every query head alike
+            v = np.where(there[:, None], v, 0.0)
+            for w in (0, 1):
+                k, qs = held[w][0], q[mine, (2 * j + w) * group:(2 * j + w + 1) * group]
+                with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+                    s = np.where(sees, scale * (qs.reshape(-1, dim) @ k.T).reshape(count, group, n), -np.inf)
+                    top = s.max(-1, keepdims=True)
+                    e = np.exp(s - np.where(top == -np.inf, 0.0, top))
+                    total = e.sum(-1, keepdims=True)
+                    p = np.where(some[..., None], e / total, 0.0)
+                    span = np.where(sees, scale * (np.abs(qs).reshape(-1, dim) @ np.abs(k).T).reshape(count, group, n), 0.0).max(-1, keepdims=True)
+                    # a score: dim products and sums, then the scaling; a probability: two scores, two roundings of the scaled ones, exp2, the sum
+                    off = 2 * (dim + 4) * EPS32 * span + 4 * EPS32 * np.abs(np.where(sees, s, 0.0)).max(-1, keepdims=True) + (8 + np.sqrt(n) + n / 64) * EPS32
+                    flat = lambda x, m: (x.reshape(-1, n) @ m).reshape(count, group, -1)  # noqa: E731
+                    size, seen_v = flat(p, np.abs(v)), flat(np.broadcast_to(sees, s.shape).astype(float), np.abs(v))
+                    o[mine, j, w] = flat(p, v)
+                    t[mine, j, w] = np.where(some[..., None], (unit_p + off) * size + 2.0 ** -25 * seen_v / total, 0.0) + 4 * EPS32 * np.abs(o[mine, j, w])
+                    lse[mine, 2 * j + w] = np.where(some, (top + np.log(total))[..., 0], -np.inf)
+                    tol_lse[mine, 2 * j + w] = off[..., 0] + 4 * EPS32 * np.abs(lse[mine, 2 * j + w])
+                    lost = np.isnan(np.where(sees, s, 0.0)).any(-1, keepdims=True)             # (adds nothing)
+                    got[b, j, :n] += np.where(lost, 0.0, p).sum((0, 1))
+                    tol_got[b, j, :n] += np.where(lost, 0.0, p * off + 2.0 ** -125 * sees).sum((0, 1))
     l = np.asarray(lam, np.float64).reshape(rows, heads // 2, group)[..., None]
     out = (o[:, :, 0] - l * o[:, :, 1]).reshape(rows, -1, 2 * dim)
     tol = (t[:, :, 0] + np.abs(l) * t[:, :, 1] + 3 * EPS32 * (np.abs(o[:, :, 0]) + np.abs(l * o[:, :, 1]))).reshape(rows, -1, 2 * dim)
@@ -61,10 +91,9 @@ def difference(q, lam, buffers, table, lengths, offsets, first, positions, scale
         tol = (tol + np.abs(out) / root * np.sqrt((tol ** 2).mean(-1, keepdims=True))) / root * np.abs(norm) + 16 * EPS32 * np.abs(out / root * norm)
         out = out / root * norm
     out, tol = out * factor, tol * abs(factor)
-    tol = 1.01 * tol + (UNIT[dtype] + 2 * EPS32) * np.abs(out) + (2.0 ** -25 if dtype == "f16" else 1e-30)
-    pair = got.reshape(got.shape[0], heads // 2, 2, -1).sum(2).repeat(2, 1)
-    tol_pair = tol_got.reshape(got.shape[0], heads // 2, 2, -1).sum(2).repeat(2, 1) + 4 * EPS32 * pair
-    return (out, lse, pair), (tol, tol_lse, tol_pair)
+    tol = 1.02 * tol + (UNIT[dtype] + 2 * EPS32) * np.abs(out) + (2.0 ** -25 if dtype == "f16" else 1e-30)
+    pair, tol_pair = got.repeat(2, 1), tol_got.repeat(2, 1)
+    return (out, lse.reshape(rows, -1), pair), (tol, tol_lse.reshape(rows, -1), tol_pair + 8 * EPS32 * pair)
 
 
 def act(name, g):

@@ -143,50 +143,71 @@ def test_rows_of_nobody_come_out_nan():
     _case(2, "bf16", 128, 1, 2, 16, [5000, 70], [3, 2], nobody=(1, 3))
 
 
-# Calls with so many rows that every wave of the card has some of its own: 64 sequences of 4 pairs, a workgroup or more to each.
-def _many(rng, rows):
-    """Lengths and rows of 64 sequences: few tokens before the rows or many, ends inside blocks and pages; one without rows, one without tokens."""
-    rows = [rows + int(r) for r in rng.integers(0, 30, 64)]
-    lengths = [r + int(t) for r, t in zip(rows, rng.choice([0, 1, 13, 31, 32, 100], 64))]
-    rows[7], lengths[9] = 0, 0
+# Calls with so many rows that every wave of the card has some of its own: 512 workgroups' worth of 64 rows (128 with 64 coordinates).
+def _many(rng, batch, rows):
+    """Lengths and rows of sequences: few tokens before the rows or many, ends inside blocks and pages; one without rows, one without tokens, some
+    of a single row."""
+    rows = [rows + int(r) for r in rng.integers(0, 30, batch)]
+    rows[3], rows[7], rows[11] = 1, 0, 2
+    lengths = [r + int(t) for r, t in zip(rows, rng.choice([0, 1, 13, 31, 32, 100], batch))]
+    lengths[9] = 0
     return lengths, rows
 
 
+def _fills_the_card(dim, pairs, group, rows):
+    assert sum(rows) * group * pairs >= 512 * (64 if dim == 128 else 128)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("dim,rows", [(128, 33), (64, 65)])
-def test_rows_of_their_own(dtype, dim, rows):
-    lengths, rows = _many(np.random.default_rng(dim), rows)
-    _case(dim, dtype, dim, 4, 1, 16, lengths, rows, lam_rows=True, poison=[(3, lengths[3] - 5, 1)], missing=[(4, 0, -1), (5, 1, 1 << 20)], nobody=(2, 5))
+@pytest.mark.parametrize("dim,rows,group", [(128, 40, 3), (64, 60, 4)])
+def test_rows_of_their_own(dtype, dim, rows, group):
+    lengths, rows = _many(np.random.default_rng(dim), 32, rows)
+    _fills_the_card(dim, 8, group, rows)
+    _case(dim, dtype, dim, 8, group, 16, lengths, rows, lam_rows=True, poison=[(2, lengths[2] - 5, 1)], missing=[(4, 0, -1), (5, 1, 1 << 20)], nobody=(2, 5))
 
 
-@pytest.mark.parametrize("dim,rows", [(128, 12), (64, 23)])
-def test_rows_of_their_own_with_windows_and_in_another_order(dim, rows):
-    lengths, rows = _many(np.random.default_rng(dim + 1), rows)
-    _case(1, "bf16", dim, 4, 3, 32, lengths, rows, window=20, sinks=3, weights=False)
-    _case(2, "f16", dim, 4, 3, 16, lengths, rows, evicted=True, window=150, sinks=5, norm=False)
-    _case(3, "bf16", dim, 4, 3, 16, lengths, rows, causal=False, weights=False)
+@pytest.mark.parametrize("dim,rows,group", [(128, 40, 3), (64, 60, 4)])
+def test_rows_of_their_own_with_windows_and_in_another_order(dim, rows, group):
+    lengths, rows = _many(np.random.default_rng(dim + 1), 32, rows)
+    _fills_the_card(dim, 8, group, rows)
+    _case(1, "bf16", dim, 8, group, 32, lengths, rows, window=20, sinks=3, weights=False)
+    _case(2, "f16", dim, 8, group, 16, lengths, rows, evicted=True, window=150, sinks=5, norm=False)
+    _case(3, "bf16", dim, 8, group, 16, lengths, rows, causal=False, weights=False)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_as_many_rows_to_every_sequence(dim):
+    # (without offsets; memories of several places of 32 blocks, first positions behind the tokens: a window leaves some rows nothing)
+    rows = [256 if dim == 64 else 128] * 4
+    _fills_the_card(dim, 8, 8, rows)
+    _case(5, "bf16", dim, 8, 8, 64, [2200, 1300, 600, 256], rows, first=[2100, 1172, 900, 0], window=500)
 
 
 def test_rows_of_their_own_with_large_scores():
     import paper_1609_01882_amd as psc
     rng = np.random.default_rng(0)
-    buffers, table, lengths = L.random_memory(rng, 64, 8, 64, 16, [100] * 64)
+    buffers, table, lengths = L.random_memory(rng, 64, 16, 64, 16, [200] * 64)
     cache = psc.KvCache(*(_cuda(x) for x in buffers))
-    q = torch.randn((64 * 70, 8, 64), device="cuda").half()
-    q[5 * 70 + 3] *= 6e4 / q[5 * 70 + 3].abs().max()
-    lam = torch.full((4,), 0.5, device="cuda")
+    q = torch.randn((64 * 140, 16, 64), device="cuda").half()
+    q[5 * 140 + 3] *= 6e4 / q[5 * 140 + 3].abs().max()
+    lam = torch.full((8,), 0.5, device="cuda")
     # a scale that lifts the scores of one row of sequence 5 over 2^24, and leaves those of the others below it
     out, lse = cache.attend_difference(q, lam, _cuda(table), _cuda(lengths), scale=64.0)
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
-    few, few_lse = cache.attend_difference(q[5 * 70:6 * 70].contiguous(), lam, _cuda(table[5:6]), _cuda(lengths[5:6]), scale=64.0)
+    few, few_lse = cache.attend_difference(q[5 * 140:6 * 140].contiguous(), lam, _cuda(table[5:6]), _cuda(lengths[5:6]), scale=64.0)
     # Scores are the same products in both kernels, and so is what a row refers to in the end; probabilities are rounded to float16 against
     # the largest seen so far, which differs: 2^-11 of each in either kernel.  Held values are 3 at most (6 times 2^-1), the maps weigh 1
     # and 0.5: 2 * 1.5 * 3 * 2^-11, and two outputs of up to 4.5 rounded to float16: 2 * 4.5 * 2^-11.  The row beyond 2^24 has
     # scores that 32 bits hardly tell apart: its output is within the held values.
-    mine, others = out[5 * 70:6 * 70], torch.arange(70, device="cuda") != 3
-    assert torch.equal(few_lse, lse[5 * 70:6 * 70])
+    mine, others = out[5 * 140:6 * 140], torch.arange(140, device="cuda") != 3
+    assert float((few_lse - lse[5 * 140:6 * 140]).abs()[others].max()) <= 2.0 ** -9      # (scores of up to 2^14: a step of 2^-10 in either)
     assert float((few[others].float() - mine[others].float()).abs().max()) <= 18 * 2.0 ** -11
     assert float(mine[3].abs().max()) <= 4.5 and float(few[3].abs().max()) <= 4.5
+
+
+def test_a_prompt_beside_single_tokens():
+    # 8 pairs: the prompt fills the card, the others have a row or two over long memories
+    _case(4, "bf16", 64, 8, 8, 64, [1030, 3000, 1, 2500, 40], [1030, 1, 1, 2, 3], weights=False)
 
 
 def test_against_two_attentions():
@@ -222,6 +243,39 @@ def test_both_heads_receive_the_same_and_are_cut_alike():
     out, _ = cache.attend_difference(q, lam, _cuda(table)[:, :7].contiguous(), after, first=_cuda(lengths) - 1,
                                      positions=torch.nn.functional.pad(pos, (0, 12), value=1 << 30))
     assert bool(torch.isfinite(out).all())
+
+
+def test_calls_without_rows_pass_the_weights_on():
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(8)
+    buffers, table, lengths = L.random_memory(rng, 2, 4, 64, 16, [200, 150])
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    w = torch.rand((2, 4, table.shape[1] * 16), device="cuda")
+    out = torch.full_like(w, -1.0)
+    q, lam = torch.zeros((0, 4, 64), device="cuda"), torch.zeros(2, device="cuda")
+    cache.attend_difference(q, lam, _cuda(table), _cuda(lengths), weights=w, weights_out=out)
+    assert torch.equal(out, w)
+    cache.attend_difference(q, lam, _cuda(table), _cuda(lengths), weights_out=out)
+    assert bool((out == 0).all())
+
+
+def test_two_calls_at_once():
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(9)
+    buffers, table, lengths = L.random_memory(rng, 2, 2, 64, 16, [6000, 3000])
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    table, lengths = _cuda(table), _cuda(lengths)
+    qs, lam = [torch.randn((2, 4, 64), device="cuda").half() for _ in range(2)], torch.rand(2, device="cuda")
+    want = [cache.attend_difference(q, lam, table, lengths) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = []
+    for q, stream in zip(qs, streams):
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            got.append([cache.attend_difference(q, lam, table, lengths) for _ in range(5)])
+    torch.cuda.synchronize()
+    for w, many in zip(want, got):
+        assert all(torch.equal(w[0], o) and torch.equal(w[1], l) for o, l in many)
 
 
 def test_captured_graphs_repeat():

@@ -193,6 +193,38 @@ def test_strides_and_shapes():
     assert torch.equal(torch.autograd.grad(z.sum(), empty[2])[0], torch.zeros_like(w))
 
 
+def test_gradients_as_autograd_hands_them_over():
+    import paper_1609_01882_amd as psc
+    x, y, w = (torch.randn(s, device="cuda", requires_grad=True) for s in ((5, 4, 40), (5, 4, 40), (40,)))
+    h, z = psc.residual_norm(x, y, after=w, before=w)
+    # sums hand over one value, expanded; transposed products a transposed one
+    got = torch.autograd.grad(h.sum() + (z.transpose(0, 2) * 2.0).sum(), (x, y, w), retain_graph=True)
+    ones = torch.ones_like(h)
+    want = torch.autograd.grad((h, z), (x, y, w), (ones, 2.0 * ones), retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # the sum of a weight that stands in two places is that of both
+    a, b = w.detach().clone().requires_grad_(), w.detach().clone().requires_grad_()
+    h, z = psc.residual_norm(x, y, after=a, before=b)
+    ga, gb = torch.autograd.grad((h, z), (a, b), (ones, 2.0 * ones))
+    assert torch.equal(ga + gb, want[2])
+    # one stream tensor as both
+    h, z = psc.residual_norm(x, x, before=w, block_scale=0.5)
+    gx, = torch.autograd.grad((h, z), x, (ones, ones))
+    x1, x2 = x.detach().clone().requires_grad_(), x.detach().clone().requires_grad_()
+    g1, g2 = torch.autograd.grad(psc.residual_norm(x1, x2, before=w, block_scale=0.5), (x1, x2), (ones, ones))
+    assert torch.equal(gx, g1 + g2)
+    # no second derivative, and no gradient of what has been overwritten
+    h, z = psc.residual_norm(x, y, after=w, before=w)
+    first, = torch.autograd.grad(z.sum(), y, create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(first.sum(), y)
+    v = y * 1.0
+    h, z = psc.residual_norm(x, v, after=w, before=w)
+    v.mul_(2.0)
+    with pytest.raises(RuntimeError):
+        z.sum().backward()
+
+
 def test_results_repeat_and_graphs_replay():
     import paper_1609_01882_amd as psc
     given = _given(5, 900, 1000, "f32", "bf16", "f32", 3, NAMES)

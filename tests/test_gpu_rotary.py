@@ -108,6 +108,33 @@ def test_the_gradient_is_the_transposed(dtype):
         assert abs(float(left - (dx.double() * v.double()).sum())) < 5376 * 16 * L.EPS32
 
 
+def test_gradients_as_autograd_hands_them_over():
+    import paper_1609_01882_amd as psc
+    rope = psc.Rotary(32)
+    x = torch.randn((6, 2, 64), device="cuda", requires_grad=True)
+    at = torch.arange(6, dtype=torch.int32, device="cuda")
+    y = rope(x, at)
+    dx, = torch.autograd.grad(y.sum(), x)
+    assert torch.equal(dx, rope.inverse(torch.ones((6, 2, 64), device="cuda"), at))
+    first, = torch.autograd.grad((rope(x, at) ** 2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(first.sum(), x)
+    y = rope(x, at)
+    at += 1
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
+    # on another stream than the tensors' own
+    want = rope(x.detach(), at)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        leaf = x.detach().clone().requires_grad_()
+        y = rope(leaf, at)
+        dx, = torch.autograd.grad(y, leaf, torch.ones_like(y))
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and torch.equal(dx, rope.inverse(torch.ones_like(want), at))
+
+
 def test_frequencies_for_long_contexts():
     import paper_1609_01882_amd as psc
     x = torch.randn((40, 2, 128), device="cuda")
