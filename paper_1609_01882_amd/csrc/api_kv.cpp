@@ -145,6 +145,7 @@ int use_plan(const KvView &v, const KvPlan &p, void *workspace, size_t bytes, Kv
     q->stat = p.stat_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes) : nullptr;
     q->scores = p.scores_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes + p.stat_bytes) : nullptr;
     q->scores_rows = p.scores_rows;
+    q->weight_parts = p.weight_parts_bytes ? (float *)(ws + p.part_stat_bytes + p.part_acc_bytes + p.stat_bytes + p.scores_bytes) : nullptr;
     return PSC_OK;
 }
 

@@ -427,6 +427,7 @@ struct KvQueries {
     float *stat;                  // [nrows][q_heads][2]: reference (units of log 2), 1 / sum over it
     float *scores;                // [batch][kv_heads][scores_rows][slots], or null
     int scores_rows;
+    float *weight_parts;          // differential attention: [parts][batch][kv_heads][slots], or null
 };
 struct KvPlan {
     int row_tiles = 0;       // of 16, to a unit
@@ -438,8 +439,9 @@ struct KvPlan {
     int scores_rows = 0;     // the scores of so many rows are kept for the weights (0: they are computed again)
     bool split_rows = false;     // and then a workgroup's waves take rows each, not tokens
     int64_t weights_groups = 0;  // workgroups of the weights to a (sequence, kv head)
-    size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0, scores_bytes = 0;
-    size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes + scores_bytes; }
+    int weight_parts = 0;        // of the rows, for the weights of pairs; 0: no such parts
+    size_t part_stat_bytes = 0, part_acc_bytes = 0, stat_bytes = 0, scores_bytes = 0, weight_parts_bytes = 0;
+    size_t bytes() const { return part_stat_bytes + part_acc_bytes + stat_bytes + scores_bytes + weight_parts_bytes; }
 };
 KvPlan plan_kv_attention(const KvView &c, int dtype, int group, int64_t nrows, int max_rows, int window, int sinks, bool ordered,
                          bool weights);

@@ -122,6 +122,23 @@ struct StageReader {
     }
 };
 
+// Whether all rows of a wave see all 32 tokens of a block that stands in no order: mostly so, for what an eviction kept lies mostly
+// behind all rows; the comparisons and selections for every score and row are then passed over.
+template <int RT>
+__device__ __forceinline__ bool all_seen(const KvQueries &q, const RowMask (&mask)[RT], const int (&pos)[8], int slot, int lim0, int lim1)
+{
+    int lo = pos[0], hi = pos[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+        lo = min(lo, pos[e]);
+        hi = max(hi, pos[e]);
+    }
+    bool all = slot + 16 <= lim0 && slot + 32 <= lim1;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) all = all && hi <= mask[t].pos && (q.window <= 0 || lo > mask[t].after || hi < q.sinks);
+    return __all(all);
+}
+
 // One wave attends with 16 RT rows, in both maps, over every fourth of the workgroup's blocks.  As in kv_attention_kernel: scores K Q^T leave
 // 8 scores of one row in a lane, which are the operand of V^T P^T as they are; maximum, sum and rescaling are the lane's own.
 // Tile t of map w is number w RT + t.  Accumulator (h D / 16 + j) of a tile has coordinate (4 g + r) D / 16 + j of value half h.
@@ -150,9 +167,9 @@ struct Difference {
 #pragma unroll
             for (int t = 0; t < RT; ++t) scores_of_two<D, DT>(a, rows[w * RT + t], s[w * RT + t]);
         }
-        if (!whole) {
-            int positions[8];
-            from.read_positions(stage, positions);
+        int positions[8];
+        if (kPos) from.read_positions(stage, positions);
+        if (!(whole || (kPos && all_seen<RT>(q, mask, positions, slot, lim0, lim1)))) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -597,7 +614,7 @@ struct RowsDifference {
             for (int t = 0; t < RT; ++t) scores_of_two<D, DT>(a, rows[w * RT + t], s[w * RT + t]);
         }
         keys();
-        if (!whole) {
+        if (!(whole || (kPos && all_seen<RT>(q, mask, pos, slot, lim0, lim1)))) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -989,7 +1006,7 @@ KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, 
         p.part_acc_bytes = (size_t)(p.most_parts * 32 * p.row_tiles * 2 * c.dim * 4 + 255) / 256 * 256;
     }
     p.least_blocks = kLeastBlocks;
-    if (weights) plan_weights(c, m, nrows * group * c.heads, &p);
+    if (weights) plan_pair_weights(c, m, nrows * group * c.heads, &p);
     return p;
 }
 

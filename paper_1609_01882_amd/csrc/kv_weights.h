@@ -1,6 +1,8 @@
 // The weight that every token of an attention memory received.
 #pragma once
 
+#include <algorithm>
+
 #include "kv_device.h"
 
 namespace psc {
@@ -68,7 +70,13 @@ constexpr int split_tiles(int dim) { return dim == 256 ? 2 : 4; }
 // their places found by adding, not dividing.  The shares are added in one order.  Rows that came out NaN add nothing.  16 exp2
 // and some 90 other vector instructions for 16 rows x 64 tokens: up to 701 rows of 3 x 4 heads x 64 over 5003, 40 us (with 32
 // tokens 52), in which a compute unit works 58 % of the time and issues vector instructions in 81 % of the cycles that it works.
-template <int D, int DT, bool kSplitRows, int kTiles, int kHeads>
+//
+// Whether rows have a window is asked once for all scores that are compared with positions: two comparisons less for each (624 rows x 8 x 64
+// over 6209 that stand in no order, pairs: 114 -> 72 us).
+//
+// kParts: a pair's two maps, and parts of their rows, go to workgroups of their own (blockIdx.y: the part), each of which leaves its sums for
+// kv_pair_weights_kernel (see plan_pair_weights).
+template <int D, int DT, bool kSplitRows, int kTiles, int kHeads, bool kParts>
 __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_weights_kernel(KvView c, KvQueries q, const float *given, float *received)
 {
     const int lane = lane_id(), i = lane & 15, g = lane >> 4;
@@ -76,6 +84,7 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
     const int b = (int)blockIdx.z / (c.heads / kHeads), head0 = (int)blockIdx.z % (c.heads / kHeads) * kHeads;
     const RowSet s = rows_of(c, q, b);
     const int64_t stride = (int64_t)c.width << c.page_shift, dense = (int64_t)blockIdx.z * kHeads * stride;
+    const int64_t of_pair = kParts ? ((int64_t)b * c.heads + (head0 & ~1)) * stride : dense;  // whose positions count
     const int64_t block = kSplitRows ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
     if (block * 16 * kTiles >= stride) return;  // (with kSplitRows the whole workgroup)
     const int slot = (int)(block * 16 * kTiles), m_all = s.rows * q.group;
@@ -85,7 +94,8 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
     for (int head = head0; head < head0 + kHeads; ++head) {
         if (!(slot < s.n && m_all > 0)) break;
         int places[kTiles], pos[kTiles][4];
-        bool there = !q.positions;
+        bool there = true;
+        int lowest = 0x7fffffff, highest = -0x7fffffff - 1;  // of the lane's tokens' positions
         u32x4 a[kTiles][D / 32];
 #pragma unroll
         for (int h = 0; h < kTiles; ++h) {
@@ -97,7 +107,9 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int at = slot + 16 * h + 4 * g + r;
-                pos[h][r] = q.positions && at < s.n ? q.positions[dense + at] : at;
+                pos[h][r] = q.positions && at < s.n ? q.positions[of_pair + at] : at;
+                lowest = min(lowest, pos[h][r]);
+                highest = max(highest, pos[h][r]);
             }
         }
         int64_t m_begin = 0, m_end = m_all;
@@ -105,6 +117,11 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
             if (q.causal) m_begin = max((int64_t)0, (int64_t)slot - s.first_pos) * q.group / 16 * 16;
             if (q.window > 0 && slot >= q.sinks)
                 m_end = min(m_end, max((int64_t)0, (int64_t)slot + 16 * kTiles - 1 + q.window - s.first_pos) * q.group);
+        }
+        if constexpr (kParts) {
+            const int64_t steps = max((int64_t)0, (m_end - m_begin + 63) / 64), from = m_begin + steps * blockIdx.y / gridDim.y * 64;
+            m_end = min(m_end, m_begin + steps * (blockIdx.y + 1) / gridDim.y * 64);
+            m_begin = from;
         }
         const int step = kSplitRows ? 64 : 16, more_rows = step / q.group, more_heads = step % q.group;
         int64_t m0 = m_begin + (kSplitRows ? wave * 16 : 0);
@@ -138,14 +155,22 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
 #pragma unroll
                 for (int h = 0; h < kTiles; ++h) x[h] = scores_of<D, DT>(a[h], rows);
                 const int pos_q = s.first_pos + at;
-                const bool coarse = is_coarse(st.x), mine = there && !coarse && (!q.causal || pos_q >= slot + 16 * kTiles - 1) && (q.window <= 0 || (int64_t)pos_q - slot < q.window || slot + 16 * kTiles <= q.sinks);
+                const bool coarse = is_coarse(st.x), mine = there && !coarse && (!q.causal || pos_q >= highest) && (q.window <= 0 || (int64_t)pos_q - lowest < q.window || highest < q.sinks);
                 if (!__all(mine)) {
                     const RowMask mask = row_mask(q, pos_q);
+                    if (q.window <= 0) {
 #pragma unroll
-                    for (int h = 0; h < kTiles; ++h)
+                        for (int h = 0; h < kTiles; ++h)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (!(places[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]))) x[h][r] = kNegInf;
+                            for (int r = 0; r < 4; ++r)
+                                if (!(places[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && pos[h][r] <= mask.pos)) x[h][r] = kNegInf;
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < kTiles; ++h)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (!(places[h] >= 0 && slot + 16 * h + 4 * g + r < s.n && sees(q, mask, pos[h][r]))) x[h][r] = kNegInf;
+                    }
                     if (__any(coarse)) {  // such rows' scores become their exponents over the factor
                         const float inverse = 1.f / q.factor;
 #pragma unroll
@@ -183,12 +208,30 @@ __global__ __launch_bounds__(256, D == 256 && DT == PSC_F32 ? 1 : 2) void kv_wei
         if (wave > 0) return;
         if (one) mine = parts[0][in_block] + parts[1][in_block] + parts[2][in_block] + parts[3][in_block];
     }
-    if (one && slot + in_block < stride) {
+    if (kParts) {
+        if (one && slot + in_block < stride) received[(int64_t)blockIdx.y * gridDim.z * stride + dense + slot + in_block] = mine;
+    } else if (one && slot + in_block < stride) {
 #pragma unroll
         for (int which = 0; which < kHeads; ++which) {
             const int64_t at = dense + which * stride + slot + in_block;
             received[at] = (given ? given[at] : 0.f) + mine;
         }
+    }
+}
+
+// Adds up the parts of a pair's two maps, in order: a thread to four slots.
+__global__ __launch_bounds__(256) void kv_pair_weights_kernel(KvView c, const float *parts, int splits, const float *given, float *received)
+{
+    const int64_t stride = (int64_t)c.width << c.page_shift, slot = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (slot >= stride) return;
+    const int64_t dense = (int64_t)blockIdx.z * 2 * stride + slot, further = (int64_t)c.batch * c.heads * stride;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < splits; ++p) sum += *(const f32x4 *)(parts + p * further + dense) + *(const f32x4 *)(parts + p * further + dense + stride);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        f32x4 x = sum;
+        if (given) x += *(const f32x4 *)(given + dense + which * stride);
+        *(f32x4 *)(received + dense + which * stride) = x;
     }
 }
 
@@ -200,10 +243,19 @@ int run_weights(const KvView &c, const KvQueries &q, const KvPlan &p, const floa
         if (p.scores_rows == 1) kv_weights_of_scores_kernel<1, kHeads><<<grid, 256, 0, s>>>(c, q, given, received);
         else if (p.scores_rows <= 4) kv_weights_of_scores_kernel<4, kHeads><<<grid, 256, 0, s>>>(c, q, given, received);
         else kv_weights_of_scores_kernel<kScoreRows, kHeads><<<grid, 256, 0, s>>>(c, q, given, received);
+    } else if (kHeads == 2 && p.weight_parts > 0) {
+        if constexpr (kHeads == 2) {
+            const int64_t slots = (int64_t)c.width << c.page_shift;
+            kv_weights_kernel<D, DT, true, split_tiles(D), 1, true>
+                <<<dim3((uint32_t)p.weights_groups, (uint32_t)p.weight_parts, (uint32_t)(c.batch * c.heads)), 256, 0, s>>>(c, q, nullptr, q.weight_parts);
+            PSC_HIP_TRY(hipGetLastError());
+            kv_pair_weights_kernel<<<dim3((uint32_t)((slots + 1023) / 1024), 1, (uint32_t)(c.batch * c.heads / 2)), 256, 0, s>>>(c, q.weight_parts, p.weight_parts, given,
+                                                                                                                           received);
+        }
     } else if (p.split_rows) {
-        kv_weights_kernel<D, DT, true, split_tiles(D), kHeads><<<grid, 256, 0, s>>>(c, q, given, received);
+        kv_weights_kernel<D, DT, true, split_tiles(D), kHeads, false><<<grid, 256, 0, s>>>(c, q, given, received);
     } else {
-        kv_weights_kernel<D, DT, false, 2, kHeads><<<grid, 256, 0, s>>>(c, q, given, received);
+        kv_weights_kernel<D, DT, false, 2, kHeads, false><<<grid, 256, 0, s>>>(c, q, given, received);
     }
     PSC_HIP_TRY(hipGetLastError());
     return PSC_OK;
@@ -222,6 +274,21 @@ inline void plan_weights(const KvView &c, int64_t m, int64_t rows, KvPlan *p)
         p->scores_rows = (int)m;
         p->scores_bytes = (size_t)(scores_bytes + 255) / 256 * 256;
     }
+}
+
+// The same where two kv heads are a pair.  Where workgroups with all rows of both maps would be few, the maps go to workgroups of their
+// own and the rows are cut into parts of at least 256, whose sums kv_pair_weights_kernel adds in order (4 bytes to a slot, head and part, at most
+// some 1 MB; it takes 4 to 5 us, where the cut saved 6 and more in all that was measured).  Not cut and cut, both kernels: 3 x 359 rows of 6 x 8 x 128 over
+// 395 with a window of 43, 154 and 26 us; 2048 of 8 x 4 x 128 over 2048, 173 and 86; 624 of 4 x 8 x 64 over 6209, 93 and 55; 20 of 4 x 4 x 128
+// over 9000, 14.7 and 13.  Up to 1024, 2048 and 4096 workgroups: the second, 92, 86, 90.
+constexpr int64_t kWeightGroups = 2048;
+inline void plan_pair_weights(const KvView &c, int64_t m, int64_t rows, KvPlan *p)
+{
+    plan_weights(c, m, rows, p);
+    const int64_t groups = p->weights_groups * c.batch * c.heads;
+    if (p->scores_rows > 0 || !p->split_rows || rows == 0 || groups >= kWeightGroups) return;
+    p->weight_parts = (int)std::min((kWeightGroups + groups - 1) / groups, (m + 255) / 256);
+    p->weight_parts_bytes = (size_t)(p->weight_parts * (int64_t)c.batch * c.heads * ((int64_t)c.width << c.page_shift) * 4 + 255) / 256 * 256;
 }
 
 }  // namespace

@@ -371,3 +371,12 @@ def test_a_layer_step():
         assert torch.allclose(o.double(), d.reshape(batch, -1, 2 * dim), rtol=1e-4, atol=1e-4)
         want = x.double() + (lambda t: t / torch.sqrt(t.square().mean(-1, keepdim=True) + 1e-6))(y.double())
         assert torch.allclose(h.double(), want, rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("dtype,dim,group", [("bf16", 64, 8), ("f16", 128, 4), ("f32", 64, 5), ("f32", 128, 3)])
+@pytest.mark.parametrize("evicted", [False, True])
+def test_weights_of_many_rows(dtype, dim, group, evicted):
+    # few tokens and many rows: the rows are cut into parts that are added up in order
+    _case(dim, dtype, dim, 1, group, 16, [900, 130, 350], [130, 1, 90], evicted=evicted)
+    _case(dim + 1, dtype, dim, 2, group, 32, [400, 0, 33], [77, 2, 33], window=50, sinks=5, evicted=evicted, nobody=(1, 3))
+    _case(dim + 2, dtype, dim, 1, group, 64, [300, 500], [100, 100], causal=False, evicted=evicted, first=[200, 399])
