@@ -137,7 +137,7 @@ int use_plan(const KvView &v, const KvPlan &p, void *workspace, size_t bytes, Kv
     PSC_REQUIRE(bytes >= p.bytes() && (p.bytes() == 0 || workspace), "workspace too small: %zu bytes, %zu needed", bytes, p.bytes());
     PSC_REQUIRE(aligned(workspace), "workspace must be 16-byte aligned");
     char *ws = (char *)workspace;
-    q->unit_rows = 16 * p.row_tiles;
+    q->unit_rows = p.unit_rows ? p.unit_rows : 16 * p.row_tiles;
     q->workgroups = (uint32_t)p.workgroups;
     q->least_blocks = (uint32_t)p.least_blocks;
     q->part_stat = (float *)ws;

@@ -431,6 +431,7 @@ struct KvQueries {
 };
 struct KvPlan {
     int row_tiles = 0;       // of 16, to a unit
+    int unit_rows = 0;       // 0: 16 row_tiles
     int64_t row_groups = 0;  // units of a sequence's kv head
     int64_t workgroups = 0;  // units are cut into parts, about so many together; 0: a workgroup has a unit
     int64_t most_parts = 0;

@@ -677,25 +677,47 @@ struct RowsDifference {
     }
 };
 
-template <int D, int DT, int RT, bool kPos>
+// kParts: what a workgroup's rows see is cut into parts as in kv_difference_kernel, for kv_difference_join_kernel.
+template <int D, int DT, int RT, bool kPos, bool kParts>
 __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, KvQueries q, KvDifference d)
 {
     __shared__ Operands<D> operands[2];
-    const int pairs = c.heads / 2, b = (int)blockIdx.z / pairs, pair = (int)blockIdx.z % pairs, lane = lane_id(), i = lane & 15, g = lane >> 4;
+    const int pairs = c.heads / 2, lane = lane_id(), i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const RowSet s = rows_of(c, q, b);
-    // (the last rows first: they see the most)
-    const int group0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 64 * RT, m_all = s.rows * q.group, group_end = min(group0 + 64 * RT, m_all);
-    if (q.offsets && group0 == 0) {
-        if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
-        difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
+    int b, pair, group0;
+    uint32_t part = 0, parts = 1, each = 0;
+    if constexpr (kParts) {
+        Parts all(c, q);
+        if (blockIdx.x >= all.total) return;
+        uint32_t first;
+        b = all.find(c, q, blockIdx.x, &first);
+        each = Parts::blocks_of_unit(q, rows_of(c, q, b));
+        parts = all.parts_of_unit(each);
+        const uint32_t unit = (blockIdx.x - first) / parts;
+        part = blockIdx.x - first - unit * parts;
+        pair = (int)unit % pairs;
+        group0 = (int)unit / pairs * 64 * RT;
+    } else {
+        // (the last rows first: they see the most)
+        b = (int)blockIdx.z / pairs;
+        pair = (int)blockIdx.z % pairs;
+        group0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 64 * RT;
     }
-    if (group0 >= m_all || m_all <= d.few) return;  // (few: left to kv_difference_kernel)
+    const RowSet s = rows_of(c, q, b);
+    const int m_all = s.rows * q.group, group_end = min(group0 + 64 * RT, m_all);
+    if constexpr (!kParts) {
+        if (q.offsets && group0 == 0) {
+            if (b == 0) difference_of_nobody<D, DT>(q, pair, 0, s.first_row);
+            difference_of_nobody<D, DT>(q, pair, s.first_row + s.rows, b + 1 < c.batch ? q.offsets[b + 1] : q.nrows);
+        }
+        if (group0 >= m_all || m_all <= d.few) return;  // (few: left to kv_difference_kernel)
+    }
     const int m0 = group0 + wave * 16 * RT, m_end = min(m0 + 16 * RT, m_all);
     const bool some = m0 < m_all;
     const int lo_pos = s.first_pos + min(m0, m_all - 1) / q.group, hi_pos = s.first_pos + (m_end - 1) / q.group;
     const Blocks blocks = blocks_of(q, s.n, s.first_pos + group0 / q.group, s.first_pos + (group_end - 1) / q.group);
-    const int count = blocks.count();
+    const int begin = kParts ? min(blocks.count(), (int)((uint64_t)part * each / parts)) : 0;
+    const int count = (kParts ? min(blocks.count(), (int)((uint64_t)(part + 1) * each / parts)) : blocks.count()) - begin;
     const int64_t slots = (int64_t)c.width << c.page_shift, dense = ((int64_t)b * c.heads + 2 * pair) * slots;
     const int next_head = 1 << (c.page_shift - 4);  // sixteens from a head's slots to the next head's
 
@@ -719,7 +741,7 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
     };
     // The places of 32 blocks are held across the lanes, a sixteen to each; a wave's quarter is sixteen `mine` of head `head`.
     const int head = wave >> 1, mine = wave & 1;
-    const auto pages_from = [&](int k) { return sixteen_of(c, b, 2 * pair, s.n, blocks.block(min(k + (lane >> 1), count - 1)) * 32 + (lane & 1) * 16); };
+    const auto pages_from = [&](int k) { return sixteen_of(c, b, 2 * pair, s.n, blocks.block(begin + min(k + (lane >> 1), count - 1)) * 32 + (lane & 1) * 16); };
     const auto load = [&](int page, Quarter<D> &x) {
         const int at = max(page, 0) + head * next_head;
         load_keys<D>(c, at, i, g, x.k, x.ks);
@@ -756,7 +778,7 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
         if (count == 0) return;
         int ids = pages_from(0), ids_then = pages_from(32);
         const auto page_of_block = [&](int in, int h) { return __builtin_amdgcn_readlane(in < 32 ? ids : ids_then, 2 * (in & 31) + h); };
-        const auto slot_of = [&](int k) { return blocks.block(min(k, count - 1)) * 32; };
+        const auto slot_of = [&](int k) { return blocks.block(begin + min(k, count - 1)) * 32; };
         Quarter<D> next;
         load(page_of_block(0, mine), next);
         expand_k(next, operands[0]);
@@ -805,6 +827,28 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
         pass(std::true_type());
     }
     if (!some) return;
+    if (kParts && parts > 1) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int n = w * RT + t;
+                const float sum = column_sum(a.sum[n]);
+                if (m0 + t * 16 + i >= m_all) continue;
+                const int64_t at = ((int64_t)blockIdx.x * 2 + w) * (64 * RT) + (wave * RT + t) * 16 + i;
+                if (g == 0) *(float2 *)(q.part_stat + at * 2) = make_float2(a.top[n], sum);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float o[D / 16];
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j) o[j] = a.acc[n][half * (D / 16) + j][r];
+                        store_row<PSC_F32, D / 16>(q.part_acc + at * (2 * D) + half * D + (4 * g + r) * (D / 16), o);
+                    }
+            }
+        return;
+    }
     typedef typename Element<DT>::type T;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -851,7 +895,8 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
 // Joins the parts of an output head's two maps, a wave to each: its lanes take a part's maximum and sum each (64 parts at a time), then
 // 2 D / 64 coordinates of every part, sixteen parts on their way; the second map's wave hands its row to the first's.  Sequences
 // without a block have no part: zeros.  What bounds it is the way from load to load and through its instructions, which no workgroup runs
-// twice.  8 x 16 heads of 128 with 16 parts to each: 8.7 us; a wave with both maps, and every fourth part to a quarter of its lanes, 13.7 one
+// twice.  8 x 16 heads of 128 with 16 parts to each: 8.7 us (with few
+// parts as many as there are: 2 and 5 parts of 624 x 32 heads of 64 in 28 us, 32 with sixteen); a wave with both maps, and every fourth part to a quarter of its lanes, 13.7 one
 // map after the other, 17.0 side by side; four parts on their way 13.0.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQueries q, KvDifference d)
@@ -891,17 +936,22 @@ __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQue
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] *= shrink;
         const int last = min(64, parts - p0);
-        for (int p = 0; p < last; p += 16) {  // (past the last: the last again, times 0)
-            float y[16][N];
+        const auto add_parts = [&](auto ahead) {
+            for (int p = 0; p < last; p += ahead.value) {  // (past the last: the last again, times 0)
+                float y[ahead.value][N];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) load_row<PSC_F32, N>(q.part_acc + (at + (p0 + min(p + u, last - 1)) * further) * (2 * D) + lane * N, y[u]);
+                for (int u = 0; u < ahead.value; ++u) load_row<PSC_F32, N>(q.part_acc + (at + (p0 + min(p + u, last - 1)) * further) * (2 * D) + lane * N, y[u]);
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
-                const float weight = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(theirs), p + u));
+                for (int u = 0; u < ahead.value; ++u) {
+                    const float weight = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(theirs), p + u));
 #pragma unroll
-                for (int j = 0; j < N; ++j) x[j] = __builtin_fmaf(y[u][j], weight, x[j]);
+                    for (int j = 0; j < N; ++j) x[j] = __builtin_fmaf(y[u][j], weight, x[j]);
+                }
             }
-        }
+        };
+        if (last <= 2) add_parts(std::integral_constant<int, 2>());
+        else if (last <= 6) add_parts(std::integral_constant<int, 6>());
+        else add_parts(std::integral_constant<int, 16>());
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     if (lane == 0 && parts != 1) {
@@ -943,6 +993,13 @@ constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || di
 // 2048 of 2048 (512) 140 and 138, 3000 over 8000 (752) 830 and 790; 1024 over 8000 (256) 385 and 315, 256 x 4 over 8000 (256) 382 and 287.
 constexpr int64_t kRowGroups = 512;
 
+// 64 coordinates: where workgroups with rows of their own would be fewer, what they see is cut into parts, as many workgroups as those, if there are
+// kRowUnits units and kRowBlocks blocks to a part at least.  4 heads x 64, float16, 8 query heads to each, us so cut and with waves that share out the
+// tokens, joins with both: 624 rows over 6209 tokens 138 and 193, in any order 170 and 246; 3 x 300 over 3000 (21 blocks to a part) 99 and 127, 400 over
+// 6000 (18) 103 and 137, 900 over 3000 (21) 128 and 122, 1200 over 1900 (14) 105 and 90; 100 over 40000 (14 units) 136 and 140, 40 over 60000 (6 units) 103 and 97.
+// (128 coordinates, a part's sums twice as long: 256 rows over 8000 120 and 112, over 30000 292 and 310; 1024 over 4000 203 and 167: never taken.)
+constexpr int64_t kRowUnits = 16, kRowBlocks = 16;
+
 template <int DT, int D>
 int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, const KvPlan &p, const float *given, float *received, hipStream_t s)
 {
@@ -951,11 +1008,17 @@ int run_difference(const KvView &c, const KvQueries &q, const KvDifference &d, c
         const uint32_t groups = (uint32_t)(c.batch * (c.heads / 2));
         const auto launch = [&](auto rt, auto pos) {
             if constexpr (DT != PSC_F32) {
+                if constexpr (D == 64) {
+                    if (p.own_rows && p.workgroups) {
+                        kv_difference_rows_kernel<D, DT, kMost, pos.value, true><<<(uint32_t)p.most_parts, 256, 0, s>>>(c, q, d);
+                        return;
+                    }
+                }
                 if (p.own_rows) {
                     // of a batch with rows of any number, sequences of one tile go to a workgroup whose waves share out the tokens
                     KvDifference mine = d;
                     mine.few = q.offsets && c.batch > 1 ? 16 : 0;
-                    kv_difference_rows_kernel<D, DT, kMost, pos.value><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, mine);
+                    kv_difference_rows_kernel<D, DT, kMost, pos.value, false><<<dim3((uint32_t)p.row_groups, 1, groups), 256, 0, s>>>(c, q, mine);
                     mine.most = mine.few;
                     if (mine.few) kv_difference_kernel<D, DT, 1, pos.value, false><<<dim3(1, 1, groups), 256, 0, s>>>(c, q, mine);
                     return;
@@ -988,22 +1051,37 @@ KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, 
     const int64_t m = (int64_t)max_rows * group, slots = (int64_t)c.width << c.page_shift, pairs = c.heads / 2;
     p.row_tiles = m <= 16 ? 1 : most_row_tiles(dtype, c.dim);
     p.row_groups = (m + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
-    // blocks of 32 tokens that a group of rows can see at most
-    int64_t blocks = (slots + 31) / 32;
-    if (ordered && window > 0) blocks = std::min(blocks, ((int64_t)window + 16 * p.row_tiles / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32);
+    // blocks of 32 tokens that a unit's rows can see at most
+    const auto blocks_of_rows = [&](int64_t unit_rows) {
+        const int64_t all = (slots + 31) / 32;
+        return ordered && window > 0 ? std::min(all, ((int64_t)window + unit_rows / group + 1) / 32 + 2 + ((int64_t)sinks + 31) / 32) : all;
+    };
+    int64_t blocks = blocks_of_rows(16 * p.row_tiles);
     const int most = 64 * most_row_tiles(dtype, c.dim);
     const int64_t groups = (m + most - 1) / most;
     // (by the rows that there are, not by the most that a sequence may have: single tokens beside a prompt do not fill workgroups)
     p.own_rows = dtype != PSC_F32 && nrows * group * pairs >= kRowGroups * most && m > most / 2;
     if (p.own_rows) p.row_groups = groups;
-    const int64_t units = p.row_groups * c.batch * pairs;
+    int64_t units = p.row_groups * c.batch * pairs;
     const int waves = difference_waves(c.dim, dtype, p.row_tiles);  // workgroups to a compute unit
-    if (!p.own_rows && units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31) p.workgroups = 256 * waves;
+    p.unit_rows = 16 * p.row_tiles;
+    // units of workgroups with rows of their own: as many as there can be, and about as many as there are
+    const int64_t most_units = groups * c.batch * pairs, some_units = std::min(most_units, (nrows * group / most + c.batch) * pairs), row_blocks = blocks_of_rows(most);
+    if (!p.own_rows && dtype != PSC_F32 && c.dim == 64 && m > most / 2 && nrows * group >= (int64_t)c.batch * most / 2 && some_units >= kRowUnits &&
+        most_units <= kRowGroups && some_units * row_blocks >= kRowGroups * kRowBlocks && most_units * row_blocks < (int64_t)1 << 31) {
+        p.own_rows = true;
+        p.unit_rows = most;
+        p.workgroups = (int)kRowGroups;
+        units = most_units;
+        blocks = row_blocks;
+    } else if (!p.own_rows && units > 0 && units < 256 * waves && blocks > kFewBlocks && units * blocks < (int64_t)1 << 31) {
+        p.workgroups = 256 * waves;
+    }
     if (p.workgroups) {
         // at most one part more to a unit than `wanted` of Parts, which is half of the workgroups or more
         p.most_parts = std::min(p.workgroups + units, units * ((blocks + kLeastBlocks - 1) / kLeastBlocks));
-        p.part_stat_bytes = (size_t)(p.most_parts * 32 * p.row_tiles * 8 + 255) / 256 * 256;
-        p.part_acc_bytes = (size_t)(p.most_parts * 32 * p.row_tiles * 2 * c.dim * 4 + 255) / 256 * 256;
+        p.part_stat_bytes = (size_t)(p.most_parts * 2 * p.unit_rows * 8 + 255) / 256 * 256;
+        p.part_acc_bytes = (size_t)(p.most_parts * 2 * p.unit_rows * 2 * c.dim * 4 + 255) / 256 * 256;
     }
     p.least_blocks = kLeastBlocks;
     if (weights) plan_pair_weights(c, m, nrows * group * c.heads, &p);

@@ -380,3 +380,41 @@ def test_weights_of_many_rows(dtype, dim, group, evicted):
     _case(dim, dtype, dim, 1, group, 16, [900, 130, 350], [130, 1, 90], evicted=evicted)
     _case(dim + 1, dtype, dim, 2, group, 32, [400, 0, 33], [77, 2, 33], window=50, sinks=5, evicted=evicted, nobody=(1, 3))
     _case(dim + 2, dtype, dim, 1, group, 64, [300, 500], [100, 100], causal=False, evicted=evicted, first=[200, 399])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_rows_of_workgroups_over_parts_of_the_tokens(dtype):
+    # 64 coordinates, workgroups of 128 rows times query heads, cut into parts of the tokens: batches whose longest memory has many blocks
+    short = [130, 9, 700, 33, 64, 1000, 31, 250]
+    few = dict(weights=False, norm=False, factor=1.0)
+    _case(1, dtype, 64, 8, 8, 32, [4200] + short, [9] * 9, weights=False)
+    _case(2, dtype, 64, 8, 8, 32, [4200] + short, [9, 40, 1, 2, 33, 17, 16, 0, 31], nobody=(2, 3))
+    _case(3, dtype, 64, 16, 8, 64, [300, 4100, 200, 10], [10, 9, 16, 9], evicted=True, lam_rows=True)
+    _case(4, dtype, 64, 16, 5, 16, [5200, 1900, 20], [50, 70, 14], window=4000, sinks=40)
+    _case(5, dtype, 64, 16, 5, 16, [5200, 1900, 20], [50, 70, 14], window=4000, sinks=40, evicted=True)
+    _case(6, dtype, 64, 16, 8, 16, [4100, 64, 128, 99], [9, 20, 16, 11], missing=[(0, 7, -1), (0, 20, 1 << 30), (3, 0, -5)], first=[900, 44, 112, -3], **few)
+    _case(7, dtype, 64, 16, 8, 16, [0, 4100, 200, 77], [9, 9, 20, 12], causal=False, weights=False)
+    _case(8, dtype, 64, 16, 8, 16, [4100, 64, 128, 99], [9, 20, 16, 11], q_scale=200.0, **few)
+    got, _, _ = _case(10, dtype, 64, 16, 8, 16, [4100, 64, 128, 99], [9, 20, 16, 11], poison=[(0, 4095, 4), (2, 0, 1)], weights=False)
+    assert torch.isnan(got).any(-1).any(-1).tolist() == [4 <= p < 9 or 29 <= p < 45 for p in range(56)]
+
+
+def test_rows_of_workgroups_over_parts_with_large_scores():
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(0)
+    buffers, table, lengths = L.random_memory(rng, 1, 32, 64, 16, [4100])
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    q = torch.randn((80, 256, 64), device="cuda").half()
+    q[3] *= 6e4 / q[3].abs().max()
+    lam = torch.full((128,), 0.5, device="cuda")
+    call = lambda q: cache.attend_difference(q, lam, _cuda(table), _cuda(lengths), first=_cuda(np.array([4020], np.int32)), scale=64.0)  # noqa: E731
+    out, lse = call(q)
+    few, few_lse = call(q[:8].contiguous())      # (64 rows times query heads: waves share out the tokens)
+    # tolerances: as in test_rows_of_their_own_with_large_scores, and 2^-24 for each of up to 64 scaled sums of parts, which 2^-11 dwarfs
+    others = torch.arange(8, device="cuda") != 3
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert float((few_lse - lse[:8]).abs()[others].max()) <= 2.0 ** -9
+    assert float((few.float() - out[:8].float())[others].abs().max()) <= 18 * 2.0 ** -11
+    assert float(out[3].abs().max()) <= 4.5 and float(few[3].abs().max()) <= 4.5
+    again, again_lse = call(q)
+    assert torch.equal(again, out) and torch.equal(again_lse, lse)
