@@ -896,7 +896,7 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
 // 2 D / 64 coordinates of every part, sixteen parts on their way; the second map's wave hands its row to the first's.  Sequences
 // without a block have no part: zeros.  What bounds it is the way from load to load and through its instructions, which no workgroup runs
 // twice.  8 x 16 heads of 128 with 16 parts to each: 8.7 us (with few
-// parts as many as there are: 2 and 5 parts of 624 x 32 heads of 64 in 28 us, 32 with sixteen); a wave with both maps, and every fourth part to a quarter of its lanes, 13.7 one
+// parts as many as there are: 5 parts of 624 x 32 heads of 64, 28 us; sixteen all the same, 32); a wave with both maps, and every fourth part to a quarter of its lanes, 13.7 one
 // map after the other, 17.0 side by side; four parts on their way 13.0.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQueries q, KvDifference d)
