@@ -418,3 +418,32 @@ def test_rows_of_workgroups_over_parts_with_large_scores():
     assert float(out[3].abs().max()) <= 4.5 and float(few[3].abs().max()) <= 4.5
     again, again_lse = call(q)
     assert torch.equal(again, out) and torch.equal(again_lse, lse)
+
+
+def test_captured_chunks_repeat():
+    # rows' workgroups over parts of the tokens, the weights' parts: a graph replayed between eager calls that have other rows
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(12)
+    buffers, table, lengths = L.random_memory(rng, 1, 32, 64, 16, [4100])
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    table, lengths = _cuda(table), _cuda(lengths)
+    q, lam = torch.randn((80, 256, 64), device="cuda").bfloat16(), torch.rand(128, device="cuda")
+    w = torch.rand((1, 32, table.shape[1] * 16), device="cuda")
+    call = lambda **more: cache.attend_difference(q, lam, table, lengths, weights=w, **more)  # noqa: E731
+    ws = torch.empty(cache.attend_difference_workspace_bytes(1, table.shape[1], 80, 80, 256, q.dtype, weights=True), dtype=torch.uint8, device="cuda")
+    got, out = torch.empty_like(w), (torch.empty((80, 128, 128), dtype=q.dtype, device="cuda"), torch.empty((80, 256), device="cuda"))
+    call(weights_out=got, out=out, workspace=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(weights_out=got, out=out, workspace=ws)
+    for turn in range(4):
+        q.mul_(1.25)
+        lengths.sub_(100 * turn)
+        seen = torch.empty_like(w)
+        want = call(weights_out=seen)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]) and torch.equal(got, seen), turn
+    with pytest.raises(psc.PscError, match="workspace too small"):
+        call(weights_out=got, out=out, workspace=ws[:-16])
