@@ -281,11 +281,13 @@ constexpr int difference_waves(int dim, int dtype, int row_tiles)
     return 2;
 }
 
-// From a row's sums over both maps, D / 16 coordinates of both value halves to each of 16 lanes that stand in a row: the output.
+// From a row's sums over both maps, D / 16 coordinates of both value halves to each of 16 lanes that stand in a row: the output.  A row that sees
+// nothing (both `inv` are 0) is 0 whatever lam, norm and eps are, here and at both other ends: 0 / 0 and 0 times infinity would be NaN.
 template <int D, int DT>
 __device__ __forceinline__ void finish_row(const KvQueries &q, const KvDifference &d, int row, int out_head, int run, const float (&x)[2][2][D / 16], const float (&inv)[2])
 {
     const float lam = d.lam[(int64_t)row * d.lam_stride + out_head];
+    const bool nothing = inv[0] == 0.f && inv[1] == 0.f;
     float o[2][D / 16], squares = 0.f;
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -305,7 +307,7 @@ __device__ __forceinline__ void finish_row(const KvQueries &q, const KvDifferenc
     for (int half = 0; half < 2; ++half) {
         const int at = half * D + run * (D / 16);
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) o[half][j] *= d.norm ? d.norm[at + j] * scale : scale;
+        for (int j = 0; j < D / 16; ++j) o[half][j] = nothing ? 0.f : o[half][j] * (d.norm ? d.norm[at + j] * scale : scale);
         store_row<DT, D / 16>(out + at, o[half]);
     }
 }
@@ -868,6 +870,7 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
             }
         }
         const float lam = d.lam[(int64_t)row * d.lam_stride + out_head];
+        const bool nothing = inv[0] == 0.f && inv[1] == 0.f;
 #pragma unroll
         for (int j = 0; j < D / 8; ++j)
 #pragma unroll
@@ -886,7 +889,7 @@ __global__ __launch_bounds__(256, 2) void kv_difference_rows_kernel(KvView c, Kv
                 const int at = half * D + (4 * g + r) * (D / 16);
                 float o[D / 16];
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) o[j] = a.acc[t][half * (D / 16) + j][r] * (d.norm ? d.norm[at + j] * scale : scale);
+                for (int j = 0; j < D / 16; ++j) o[j] = nothing ? 0.f : a.acc[t][half * (D / 16) + j][r] * (d.norm ? d.norm[at + j] * scale : scale);
                 if (there) store_row<DT, D / 16>(out + at, o);
             }
     }
@@ -902,7 +905,7 @@ template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQueries q, KvDifference d)
 {
     constexpr int N = D / 32;  // coordinates of a lane
-    __shared__ float second[2][2 * D];
+    __shared__ float second[2][2 * D], second_inv[2];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), which = wave & 1, lane = lane_id(), out_heads = q.q_heads / 2;
     const int64_t items = (int64_t)q.nrows * out_heads, item = min((int64_t)blockIdx.x * 2 + (wave >> 1), items - 1);  // (past the last: it again)
     const int r = (int)(item / out_heads), out_head = (int)(item % out_heads), pair = out_head / q.group, in_group = out_head % q.group;
@@ -960,10 +963,14 @@ __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQue
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] *= inv;
-    if (which == 1) store_row<PSC_F32, N>(&second[wave >> 1][lane * N], x);
+    if (which == 1) {
+        store_row<PSC_F32, N>(&second[wave >> 1][lane * N], x);
+        if (lane == 0) second_inv[wave >> 1] = inv;
+    }
     __syncthreads();
     if (which == 1 || parts == 1) return;
     const float lam = d.lam[(int64_t)r * d.lam_stride + out_head];
+    const bool nothing = inv == 0.f && second_inv[wave >> 1] == 0.f;
     float y[N], squares = 0.f, scale = d.factor;
     load_row<PSC_F32, N>(&second[wave >> 1][lane * N], y);
 #pragma unroll
@@ -977,7 +984,7 @@ __global__ __launch_bounds__(256) void kv_difference_join_kernel(KvView c, KvQue
         scale *= 1.f / sqrtf(squares * (1.f / (2 * D)) + d.eps);
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = nobodys ? __builtin_nanf("") : x[j] * (d.norm ? d.norm[lane * N + j] * scale : scale);
+    for (int j = 0; j < N; ++j) x[j] = nobodys ? __builtin_nanf("") : nothing ? 0.f : x[j] * (d.norm ? d.norm[lane * N + j] * scale : scale);
     store_row<DT, N>((typename Element<DT>::type *)q.out + item * (2 * D) + lane * N, x);
 }
 

@@ -1,0 +1,57 @@
+"""Calls around the attention memory that their documentation allows and where they can go wrong (needs an MI355X)."""
+import numpy as np
+import pytest
+import torch
+
+import kv_util as U
+import layer_util as L
+
+pytestmark = pytest.mark.gpu
+
+
+def _cuda(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+# ------------------------------------------------------------------------------------------- differential attention
+# (pairs, group, lengths, rows, first): one workgroup to a unit; units cut into parts and joined; waves with rows of their own; those cut into parts.
+# Sequences that have no tokens, or whose tokens' pages are all missing (lengths below 0 stand for so many).
+WAYS = {
+    "whole": (2, 3, [0, 40, -64], [2, 3, 2], None),
+    "parts": (1, 2, [5000, -5000, 0, 33], [1, 2, 3, 1], None),
+    "rows": (8, 8, [600, 0, -300, 256], [128, 128, 128, 128], [500, 0, 10, 128]),
+    "rows_64": (8, 8, [600, 0, -300, 256], [256, 256, 256, 256], [500, 0, 10, 0]),
+    "rows_in_parts": (16, 8, [4100, -4100, 128, 0], [9, 20, 16, 11], None),
+}
+
+
+@pytest.mark.parametrize("dtype,dim,way", [("bf16", 64, "whole"), ("f32", 128, "whole"), ("f16", 64, "parts"), ("bf16", 128, "parts"), ("f32", 64, "parts"), ("f16", 128, "rows"),
+                                           ("bf16", 64, "rows_64"), ("f16", 64, "rows_in_parts")])
+def test_rows_that_see_nothing_are_0_whatever_norms_them(dtype, dim, way):
+    import paper_1609_01882_amd as psc
+    pairs, group, lengths, rows, first = WAYS[way]
+    rng = np.random.default_rng(dim)
+    tokens = [abs(n) for n in lengths]
+    buffers, table, held = L.random_memory(rng, len(lengths), 2 * pairs, dim, 16, [max(n, 1) for n in tokens])
+    held[:] = tokens
+    for b, n in enumerate(lengths):
+        if n < 0:
+            table[b] = -1
+    offsets = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    blind = np.concatenate([np.full(r, n <= 0) for n, r in zip(lengths, rows)])
+    n, heads = len(blind), 2 * pairs * group
+    lam = rng.uniform(0.1, 0.9, (n, heads // 2)).astype(np.float32)
+    wild = lam.copy()
+    wild[blind, 0], wild[blind, -1] = np.inf, np.nan
+    cache = psc.KvCache(*(_cuda(x) for x in buffers))
+    q = torch.from_numpy(rng.normal(size=(n, heads, dim))).to(U.TYPES[dtype]).cuda()
+    norm = torch.ones(2 * dim, device="cuda")
+    print(f"nothing seen: {way} {dtype} {dim}", flush=True)
+    call = lambda lam, eps: cache.attend_difference(q, _cuda(lam), _cuda(table), _cuda(held), offsets=_cuda(offsets), max_rows=max(rows),  # noqa: E731
+                                                    first=_cuda(None if first is None else np.array(first, np.int32)), norm=norm, eps=eps)
+    got, lse = call(wild, 0.0)
+    at = _cuda(blind)
+    assert bool((got[at] == 0).all()) and bool((lse[at] == -np.inf).all())
+    # (2^-126 is lost beside any mean square of the others')
+    want, _ = call(lam, 2.0 ** -126)
+    assert bool(torch.isfinite(got).all()) and torch.equal(got, want)
