@@ -429,10 +429,10 @@ int psc_rotary_turns(const double *radians, int n, uint64_t *turns);
 
 /* Rows x_dev [nrows][heads][head_dim] turned (transposed != 0: by the opposite angles, which is the gradient) into
  * out_dev, which may be x_dev with the same strides.  A row stands at positions_dev[row], or, positions_dev NULL, at
- * first_dev[b] + its place in its sequence b (offsets_dev as above; first_dev NULL: 0).  Rows that no sequence has are
- * copied.  Sines and cosines are computed in 64 bits and rounded to 32, products and sums are float32.  head_dim 2 .. 65536,
- * any even dims; strides in elements, any alignment of the type (16-byte aligned rows and heads with dims a multiple of
- * 16 and head_dim one of 8 go faster). */
+ * first_dev[b] + its place in its sequence b (offsets_dev as above; first_dev NULL: 0).  Rows that no sequence has, and
+ * what lies behind the pairs, are copied bit for bit.  Sines and cosines are computed in 64 bits and rounded to 32,
+ * products and sums are float32.  head_dim 2 .. 65536, any even dims; strides in elements, any alignment of the type
+ * (16-byte aligned rows and heads with dims a multiple of 16 and head_dim one of 8 go faster). */
 int psc_rotary_rows(const psc_rotary *rotary, int transposed, int dtype, const void *x_dev, int64_t row_stride,
                     int64_t head_stride, int nrows, int heads, int head_dim, const int32_t *positions_dev, int batch,
                     const int32_t *offsets_dev, const int32_t *first_dev, void *out_dev, int64_t out_row_stride,
@@ -441,7 +441,7 @@ int psc_rotary_rows(const psc_rotary *rotary, int transposed, int dtype, const v
 /* psc_kv_append with the keys turned first: row r of sequence b by the angles of first_dev[b] + r (first_dev NULL: its
  * slot).  Keys are turned in 64 bits and rounded to float32, then to 4 bits.  The queries of the same rows (q_heads may be
  * 0) are turned into q_out_dev [nrows][q_heads][head_dim], which is another array than q_dev; those of rows that no sequence
- * has are copied.  dims is a multiple of 16 here. */
+ * has are copied bit for bit.  dims is a multiple of 16 here. */
 int psc_kv_append_rotary(const psc_kv_cache *cache, const psc_rotary *rotary, int dtype, const void *k_dev,
                          int64_t k_row_stride, int64_t k_head_stride, const void *v_dev, int64_t v_row_stride,
                          int64_t v_head_stride, const void *q_dev, int64_t q_row_stride, int64_t q_head_stride,
@@ -488,7 +488,8 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
  * Both heads of a pair hold the same tokens in the same slots: positions_dev is read for the even one.  weights_out_dev:
  * both heads of a pair receive the sum of both maps' probabilities, so that psc_kv_evict cuts them alike where
  * they began alike.  A map that comes out NaN adds nothing to the weights; its output head is NaN.  Rows that see
- * nothing come out 0, whatever lam, norm and eps are.  Everything else as for psc_kv_attention, the precision of a map's products too. */
+ * nothing come out 0, whatever lam, norm and eps are.  Everything else as for psc_kv_attention, the precision of a map's
+ * products too. */
 size_t psc_kv_difference_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
                                          int window, int sinks, int has_positions, int has_weights);
 int psc_kv_difference(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,

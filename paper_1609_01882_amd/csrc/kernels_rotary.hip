@@ -40,16 +40,53 @@ __device__ __forceinline__ void sincos_of_turns(uint64_t turns, double *sine, do
     *cosine = (quarters + 1) & 2 ? -c0 : c0;
 }
 
-// Sine and cosine of a pair times the factor (the rows that nobody has: as they are).
-__device__ __forceinline__ void turn_of(const Rotary &t, int pair, int64_t position, bool nobodys, double *sine, double *cosine)
+// Sine and cosine of a pair times the factor.
+__device__ __forceinline__ void turn_of(const Rotary &t, int pair, int64_t position, double *sine, double *cosine)
 {
     sincos_of_turns((uint64_t)position * t.turns[pair], sine, cosine);
-    *sine = nobodys ? 0.0 : *sine * t.factor;
-    *cosine = nobodys ? 1.0 : *cosine * t.factor;
+    *sine *= t.factor;
+    *cosine *= t.factor;
 }
 
+// What is copied -- coordinates behind the turned ones, rows that nobody has -- keeps its bits: turned by nothing, an infinity or a NaN would
+// make its partner NaN, and -0 could become 0.
+template <int DT>
+struct RawRow {  // 8 coordinates as they lie in memory
+    static constexpr int kWords = DT == PSC_F32 ? 8 : 4;
+    u32x4 w[kWords / 4];  // (arrays of words that are copied as bytes go to LDS)
+    __device__ __forceinline__ void load(const void *p)
+    {
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i) w[i] = ((const u32x4 *)p)[i];
+    }
+    __device__ __forceinline__ void store(void *p) const
+    {
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i) ((u32x4 *)p)[i] = w[i];
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (DT == PSC_F32) x[i] = __uint_as_float(w[i / 4][i % 4]);
+            else x[i] = Element<DT>::load((uint16_t)(i & 1 ? w[0][i / 2] >> 16 : w[0][i / 2]));
+        }
+    }
+    // x, or what was given: of all coordinates.
+    __device__ __forceinline__ void choose(bool given, const float (&x)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            uint32_t made;
+            if constexpr (DT == PSC_F32) made = __float_as_uint(x[i]);
+            else made = (uint32_t)Element<DT>::store(x[2 * i]) | (uint32_t)Element<DT>::store(x[2 * i + 1]) << 16;
+            w[i / 4][i % 4] = given ? w[i / 4][i % 4] : made;
+        }
+    }
+};
+
 // ------------------------------------------------------------------------------------------- rows on their own
-// A thread takes 8 pairs (or 16 coordinates behind the turned ones, which are copied) of a row, in every `slots`-th head: threads beside it take
+// A thread takes 8 pairs (or 16 coordinates that are copied) of a row, in every `slots`-th head: threads beside it take
 // the row's other pairs, then the heads beside it, so that a wave reads and writes in one piece.
 template <int DT, bool kInterleaved>
 __global__ __launch_bounds__(256) void rotary_kernel(Rotary t, RotaryRows r)
@@ -63,29 +100,29 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rotary t, RotaryRows r)
     if (row >= r.nrows) return;
     const T *x = (const T *)r.x + row * r.row_stride;
     T *y = (T *)r.out + row * r.out_row_stride;
-    if (chunk >= turned) {
-        const int at = t.dims + (chunk - turned) * 16;
-        const bool second = at + 8 < r.head_dim;
+    int64_t position = 0;
+    bool copied = chunk >= turned;
+    const int at0 = copied ? t.dims + (chunk - turned) * 16 : kInterleaved ? chunk * 16 : chunk * 8, at1 = copied || kInterleaved ? at0 + 8 : at0 + t.dims / 2;
+    if (!copied) position = r.position_of(row, &copied);
+    if (copied) {
+        const bool second = at1 < r.head_dim;
         for (int h = from; h < r.heads; h += r.slots) {
-            float a[8], b[8];
-            load_row<DT, 8>(x + h * r.head_stride + at, a);
-            if (second) load_row<DT, 8>(x + h * r.head_stride + at + 8, b);
-            store_row<DT, 8>(y + h * r.out_head_stride + at, a);
-            if (second) store_row<DT, 8>(y + h * r.out_head_stride + at + 8, b);
+            RawRow<DT> a, b;
+            a.load(x + h * r.head_stride + at0);
+            b.load(x + h * r.head_stride + (second ? at1 : at0));
+            a.store(y + h * r.out_head_stride + at0);
+            if (second) b.store(y + h * r.out_head_stride + at1);
         }
         return;
     }
-    bool nobodys;
-    const int64_t position = r.position_of(row, &nobodys);
     float s[8], c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         double sine, cosine;
-        turn_of(t, chunk * 8 + i, position, nobodys, &sine, &cosine);
+        turn_of(t, chunk * 8 + i, position, &sine, &cosine);
         s[i] = r.transposed ? -(float)sine : (float)sine;
         c[i] = (float)cosine;
     }
-    const int at0 = kInterleaved ? chunk * 16 : chunk * 8, at1 = kInterleaved ? at0 + 8 : at0 + t.dims / 2;
 #pragma unroll 4
     for (int h = from; h < r.heads; h += r.slots) {
         float u[8], v[8], p[8], q[8];
@@ -125,12 +162,20 @@ __global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows
         for (int h = from; h < r.heads; h += r.slots) y[h * r.out_head_stride + at] = x[h * r.head_stride + at];
         return;
     }
+    const int at0 = t.interleaved ? 2 * place : place, at1 = t.interleaved ? at0 + 1 : at0 + half;
     bool nobodys;
     const int64_t position = r.position_of(row, &nobodys);
+    if (nobodys) {
+        for (int h = from; h < r.heads; h += r.slots) {
+            const T a = x[h * r.head_stride + at0], b = x[h * r.head_stride + at1];
+            y[h * r.out_head_stride + at0] = a;
+            y[h * r.out_head_stride + at1] = b;
+        }
+        return;
+    }
     double sine, cosine;
-    turn_of(t, place, position, nobodys, &sine, &cosine);
+    turn_of(t, place, position, &sine, &cosine);
     const float s = r.transposed ? -(float)sine : (float)sine, c = (float)cosine;
-    const int at0 = t.interleaved ? 2 * place : place, at1 = t.interleaved ? at0 + 1 : at0 + half;
 #pragma unroll 4
     for (int h = from; h < r.heads; h += r.slots) {
         const float a = Element<DT>::load(x[h * r.head_stride + at0]), b = Element<DT>::load(x[h * r.head_stride + at1]);
@@ -147,19 +192,6 @@ __global__ __launch_bounds__(256) void rotary_single_kernel(Rotary t, RotaryRows
 //
 // The way from load to load -- offsets, first, lengths, table -- is long beside the work of a lane, so the first head's coordinates are asked
 // for before it, and the next head's before a head is worked on.
-template <int DT>
-struct RawRow {  // 8 coordinates as they lie in memory
-    uint32_t w[DT == PSC_F32 ? 8 : 4];
-    __device__ __forceinline__ void load(const void *p) { __builtin_memcpy(w, __builtin_assume_aligned(p, 16), sizeof w); }
-    __device__ __forceinline__ void get(float (&x)[8]) const
-    {
-        typename Element<DT>::type t[8];
-        __builtin_memcpy(t, w, sizeof t);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = Element<DT>::load(t[i]);
-    }
-};
-
 template <int DT, int D, bool kInterleaved>
 __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows r, Rotary t, RotaryQueries q)
 {
@@ -200,7 +232,7 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
     if (turned) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            turn_of(t, kInterleaved ? part * 4 + i : second ? other + i : at + i, position, nobodys, &s[i], &co[i]);
+            turn_of(t, kInterleaved ? part * 4 + i : second ? other + i : at + i, position, &s[i], &co[i]);
             if (!kInterleaved && !second) s[i] = -s[i];  // (then x cos + other sin on both sides)
         }
     }
@@ -231,6 +263,7 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
         }
         return;
     }
+    const bool copied = !turned || nobodys;
     float sf[kPairs], cf[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
@@ -240,6 +273,7 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
 #pragma unroll 2
     for (int h = from; h < to; h += q.slots) {
         float x[8], o[8];
+        RawRow<DT> out = mine;
         mine.get(x);
         side.get(o);
         if (h + q.slots < to) load(h + q.slots);
@@ -247,14 +281,15 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView c, KvRows 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float a = x[2 * i], b = x[2 * i + 1];
-                x[2 * i] = turned ? a * cf[i] - b * sf[i] : a;
-                x[2 * i + 1] = turned ? b * cf[i] + a * sf[i] : b;
+                x[2 * i] = a * cf[i] - b * sf[i];
+                x[2 * i + 1] = b * cf[i] + a * sf[i];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = turned ? x[i] * cf[i] + o[i] * sf[i] : x[i];
+            for (int i = 0; i < 8; ++i) x[i] = x[i] * cf[i] + o[i] * sf[i];
         }
-        store_row<DT, 8>((T *)q.out + ((int64_t)row * q.heads + h) * D + at, x);
+        out.choose(copied, x);
+        out.store((T *)q.out + ((int64_t)row * q.heads + h) * D + at);
     }
 }
 

@@ -55,3 +55,48 @@ def test_rows_that_see_nothing_are_0_whatever_norms_them(dtype, dim, way):
     # (2^-126 is lost beside any mean square of the others')
     want, _ = call(lam, 2.0 ** -126)
     assert bool(torch.isfinite(got).all()) and torch.equal(got, want)
+
+
+# ------------------------------------------------------------------------------------------- rotary positions
+def _odd_bits(seed, shape, dtype):
+    """Numbers among which a third are infinities, NaN (quiet and signalling), zeros of both signs and denormal numbers; as bits, and the type to view them as."""
+    kind, odd = {"bf16": (torch.int16, [0x7f80, -0x80, 0x7fc0, 0x7f81, -1, -0x8000, 0, 1, -0x7fff]), "f16": (torch.int16, [0x7c00, -0x400, 0x7e00, 0x7c01, -1, -0x8000, 0, 1, -0x7fff]),
+                 "f32": (torch.int32, [0x7f800000, -0x800000, 0x7fc00000, 0x7f800001, -1, -0x80000000, 0, 1, -0x7fffffff])}[dtype]
+    g = torch.Generator().manual_seed(seed)
+    bits = torch.randn(shape, generator=g).to(U.TYPES[dtype]).view(kind)
+    which = torch.tensor(odd, dtype=kind)[torch.randint(len(odd), shape, generator=g)]
+    return torch.where(torch.rand(shape, generator=g) < 0.33, which, bits).cuda(), kind
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,dims", [(64, 64), (128, 96), (88, 32), (50, 26)])
+def test_what_is_copied_keeps_its_bits(dtype, interleaved, dim, dims):
+    import paper_1609_01882_amd as psc
+    bits, kind = _odd_bits(dim, (40, 5, dim), dtype)
+    x = bits.view(U.TYPES[dtype])
+    rope = psc.Rotary(dims, interleaved=interleaved, factor=0.5)
+    offsets = torch.tensor([7, 7, 20, 33], dtype=torch.int32, device="cuda")          # rows 0 .. 6 and 33 .. 39 are nobody's
+    nobodys = torch.tensor([r < 7 or r >= 33 for r in range(40)], device="cuda")
+    into = torch.zeros_like(x)
+    for got in (rope(x, offsets=offsets), rope.inverse(x, offsets=offsets), rope(x[:, ::2], offsets=offsets), rope(x, offsets=offsets, out=into), rope(x[..., :dim], offsets=offsets)):
+        want = bits[:, ::2] if got.shape[1] == 3 else bits
+        assert torch.equal(got.view(kind)[nobodys], want[nobodys])
+        assert torch.equal(got.view(kind)[..., dims:], want[..., dims:])
+    rope(x, offsets=offsets, out=x)
+    assert torch.equal(x.view(kind)[nobodys], into.view(kind)[nobodys]) and torch.equal(x.nan_to_num(7.0), into.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,dims", [(64, 64), (128, 96), (256, 16)])
+def test_queries_that_an_append_copies_keep_their_bits(dtype, interleaved, dim, dims):
+    import paper_1609_01882_amd as psc
+    bits, kind = _odd_bits(dims, (40, 6, dim), dtype)
+    k = torch.randn((40, 2, dim), device="cuda").to(U.TYPES[dtype])
+    cache = psc.KvCache.empty(6, 2, dim, 16)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(2, 3)
+    lengths, offsets = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([1, 0], [7, 20, 33]))
+    q = bits.view(U.TYPES[dtype])
+    got = cache.append(k, k, table, lengths, offsets=offsets, rotary=psc.Rotary(dims, interleaved=interleaved), q=q).view(kind)
+    assert torch.equal(got[:7], bits[:7]) and torch.equal(got[33:], bits[33:]) and torch.equal(got[..., dims:], bits[..., dims:])
