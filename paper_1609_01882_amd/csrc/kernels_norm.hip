@@ -175,6 +175,11 @@ __device__ __forceinline__ float sigmoid(float g)
     return __builtin_amdgcn_rcpf(1.f + p);
 }
 
+// From m = sigmoid(-|g|).
+__device__ __forceinline__ float sigmoid_of(float g, float m) { return g >= 0.f ? 1.f - m : m; }
+__device__ __forceinline__ float sigmoid_slope(float m) { return m * (1.f - m); }
+__device__ __forceinline__ float silu_slope(float g, float m) { return __builtin_fmaf(g, sigmoid_slope(m), sigmoid_of(g, m)); }
+
 // Places of a lane's coordinates in its row.
 struct Columns {
     int lane, lanes, width;
@@ -237,15 +242,16 @@ constexpr size_t weights_lds(int lanes) { return (size_t)lanes * NV * 64; }
 #define PSC_EACH                        \
     _Pragma("unroll") for (int v = 0; v < NV; ++v) _Pragma("unroll") for (int i = 0; i < 8; ++i)
 
-// Multiplies by the gate g's factor and by its derivative, from s = sigmoid(g) (which a plain gate does not ask for): one of three loops, not a
-// choice for every coordinate (which took 271 us backward instead of 226).
+// Multiplies by the gate g's factor and by its derivative, from m = sigmoid(-|g|), the smaller of sigmoid(g) and 1 - sigmoid(g) (which a plain
+// gate does not ask for): the larger, 1 - m, and the slope m (1 - m) keep their bits, where 1 - sigmoid(g) of an open gate would
+// lose them (all of them from g = 17 on).  One of three loops, not a choice for every coordinate (which took 271 us backward instead of 226).
 struct Gate {
     bool plain, silu;
     __device__ explicit Gate(int activation) : plain(activation == PSC_GATE_PLAIN), silu(activation == PSC_GATE_SILU) {}
     template <int TB, int NV>
-    __device__ __forceinline__ void sigmoids(const Eight<TB> (&g)[NV], float (&s)[NV][8]) const
+    __device__ __forceinline__ void smaller(const Eight<TB> (&g)[NV], float (&m)[NV][8]) const
     {
-        if (!plain) PSC_EACH s[v][i] = sigmoid(g[v][i]);
+        if (!plain) PSC_EACH m[v][i] = sigmoid(-fabsf(g[v][i]));
     }
     template <int TB, int NV>
     __device__ __forceinline__ void factors(const Eight<TB> (&g)[NV], float (&f)[NV][8]) const
@@ -258,18 +264,18 @@ struct Gate {
         if (silu) PSC_EACH f[v][i] *= g[v][i];
     }
     template <int TB, int NV>
-    __device__ __forceinline__ void open(float (&x)[NV][8], const Eight<TB> (&g)[NV], const float (&s)[NV][8]) const
+    __device__ __forceinline__ void open(float (&x)[NV][8], const Eight<TB> (&g)[NV], const float (&m)[NV][8]) const
     {
         if (plain) PSC_EACH x[v][i] *= g[v][i];
-        else if (silu) PSC_EACH x[v][i] *= g[v][i] * s[v][i];
-        else PSC_EACH x[v][i] *= s[v][i];
+        else if (silu) PSC_EACH x[v][i] *= g[v][i] * sigmoid_of(g[v][i], m[v][i]);
+        else PSC_EACH x[v][i] *= sigmoid_of(g[v][i], m[v][i]);
     }
     template <int TB, int NV>
-    __device__ __forceinline__ void slope(float (&x)[NV][8], const Eight<TB> (&g)[NV], const float (&s)[NV][8]) const
+    __device__ __forceinline__ void slope(float (&x)[NV][8], const Eight<TB> (&g)[NV], const float (&m)[NV][8]) const
     {
         if (plain) return;
-        if (silu) PSC_EACH x[v][i] *= __builtin_fmaf(g[v][i], s[v][i] * (1.f - s[v][i]), s[v][i]);
-        else PSC_EACH x[v][i] *= s[v][i] * (1.f - s[v][i]);
+        if (silu) PSC_EACH x[v][i] *= silu_slope(g[v][i], m[v][i]);
+        else PSC_EACH x[v][i] *= sigmoid_slope(m[v][i]);
     }
 };
 
@@ -455,7 +461,7 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
             to.load(p, &d, col, row, kShared ? gate : row);
         };
         if (kAhead && begin < end) load(begin, now);
-        float of_gate[NV][8];  // its factors, where all of these rows share it; else the sigmoids of a row's
+        float of_gate[NV][8];  // its factors, where all of these rows share it; else what `smaller` gives of a row's
         const auto load_gate = [&](Eight<TB> (&g)[NV]) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) load_eight<TB>(p.gate, (int64_t)gate * p.gate_stride + col.at(v), col.template count<NV>(v), col.tail, g[v]);
@@ -477,7 +483,7 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
                 if (p.gate) {
 #pragma unroll
                     for (int v = 0; v < NV; ++v) g[v] = now.g[v];
-                    act.sigmoids(g, of_gate);
+                    act.smaller(g, of_gate);
                 }
             }
             const auto open = [&](float (&x)[NV][8]) __attribute__((always_inline)) {
@@ -564,7 +570,7 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
                     } else {
                         Eight<TB> g[NV];
                         load_gate(g);
-                        act.sigmoids(g, of_gate);
+                        act.smaller(g, of_gate);
                         act.slope(dg, g, of_gate);
                         store_vectors<TB>(d.dgate, gate, col, dg);
                     }
@@ -615,8 +621,8 @@ __global__ __launch_bounds__(256) void residual_norm_sums_kernel(ResidualNorm p,
     } else {
         const float g = Stored<TB>::load(((const typename Stored<TB>::type *)p.gate)[(int64_t)(which - 2) * p.gate_stride + column]);
         if (p.activation != PSC_GATE_PLAIN) {
-            const float s = sigmoid(g), of_sigmoid = s * (1.f - s);
-            x *= p.activation == PSC_GATE_SILU ? __builtin_fmaf(g, of_sigmoid, s) : of_sigmoid;
+            const float m = sigmoid(-fabsf(g));
+            x *= p.activation == PSC_GATE_SILU ? silu_slope(g, m) : sigmoid_slope(m);
         }
         ((typename Stored<TB>::type *)d.dgate)[(int64_t)(which - 2) * p.width + column] = Stored<TB>::store(x);
     }

@@ -100,3 +100,27 @@ def test_queries_that_an_append_copies_keep_their_bits(dtype, interleaved, dim, 
     q = bits.view(U.TYPES[dtype])
     got = cache.append(k, k, table, lengths, offsets=offsets, rotary=psc.Rotary(dims, interleaved=interleaved), q=q).view(kind)
     assert torch.equal(got[:7], bits[:7]) and torch.equal(got[33:], bits[33:]) and torch.equal(got[..., dims:], bits[..., dims:])
+
+
+# ------------------------------------------------------------------------------------------- norms around a block
+@pytest.mark.parametrize("block", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("activation", ["sigmoid", "silu"])
+@pytest.mark.parametrize("rows,gates", [(6, 6), (1100, 1100), (700, 1), (3000, 1500), (2, 1)])
+def test_slopes_of_open_and_shut_gates(rows, gates, activation, block):
+    """The gate's gradient where y and the gradient of h are 1: the slope itself, times the rows that share it."""
+    import paper_1609_01882_amd as psc
+    g = torch.cat([torch.linspace(-80.0, 80.0, 101), torch.tensor([0.0, 1e-3, -1e-3, 8.0, 10.0, 14.0, 17.0, 20.0, 30.0, -8.0, -17.0, -30.0, 1.278, -1.278])]).to(U.TYPES[block])
+    gate = g.repeat(gates, 1).cuda().requires_grad_()
+    ones = torch.ones((rows, len(g)), dtype=g.dtype, device="cuda")
+    h, _ = psc.residual_norm(None, ones, gate=gate, activation=activation)
+    dgate, = torch.autograd.grad(h, gate, ones)
+    g = g.double()
+    s, rest = 1 / (1 + torch.exp(-g)), 1 / (1 + torch.exp(g))
+    slope = s * rest
+    want, size = (slope, slope) if activation == "sigmoid" else (s + g * slope, s + g.abs() * slope)
+    # In units of 2^-24: the power (a step of exp2's result, 2, and what is put back, 1), 1 + it 1, the quotient 2 -- 6, of m and no more of
+    # m (1 - m), where 1 - m and the product take 1 each; with a sum and the product with what flows in 10, and 16 are allowed.  Then the output's rounding.
+    want, size = want * (rows // gates), size * (rows // gates)
+    tol = 16 * L.EPS32 * size + U.UNIT[block] * want.abs() + (2.0 ** -25 if block == "f16" else 2.0 ** -126)
+    off = (dgate.double().cpu() - want).abs()
+    assert bool((off <= tol).all()), (g[(off > tol).any(0)], (off / tol).max())
