@@ -534,9 +534,8 @@ __global__ __launch_bounds__(kThreads, 2) void residual_norm_backward_kernel(Res
                     PSC_EACH t[v][i] = now.y[v][i];
                     if (p.after) PSC_EACH t[v][i] = t[v][i] * root_y * w[v][i];
                     PSC_EACH t[v][i] *= grad[v][i];
-                    if constexpr (kShared) {
-                        const float counts = there ? 1.f : 0.f;
-                        PSC_EACH dg[v][i] = __builtin_fmaf(t[v][i], counts, dg[v][i]);
+                    if constexpr (kShared) {  // (a selection: 0 times an infinity would be NaN)
+                        PSC_EACH dg[v][i] += there ? t[v][i] : 0.f;
                     } else if (d.dgate && there) {
                         act.slope(t, g, of_gate);
                         store_vectors<TB>(d.dgate, row, col, t);

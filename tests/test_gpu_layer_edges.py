@@ -124,3 +124,18 @@ def test_slopes_of_open_and_shut_gates(rows, gates, activation, block):
     tol = 16 * L.EPS32 * size + U.UNIT[block] * want.abs() + (2.0 ** -25 if block == "f16" else 2.0 ** -126)
     off = (dgate.double().cpu() - want).abs()
     assert bool((off <= tol).all()), (g[(off > tol).any(0)], (off / tol).max())
+
+
+@pytest.mark.parametrize("rows,gates,width", [(3, 1, 40), (9, 3, 40), (5, 1, 700), (3000, 3, 64), (2, 1, 2000)])
+def test_an_infinity_in_the_last_row_that_shares_a_gate(rows, gates, width):
+    # rows that a workgroup has past a gate's last one are that row again, and do not count
+    import paper_1609_01882_amd as psc
+    y, dh = torch.ones((rows, width), device="cuda"), torch.ones((rows, width), device="cuda")
+    each = rows // gates
+    y[each - 1::each, 5] = float("inf")
+    y[each - 1::each, 7] = -float("inf")
+    gate = torch.ones((gates, width), device="cuda", requires_grad=True)
+    h, _ = psc.residual_norm(None, y, gate=gate)
+    dgate, = torch.autograd.grad(h, gate, dh)
+    want = y.view(gates, each, width).sum(1)
+    assert torch.equal(dgate, want)
