@@ -16,8 +16,10 @@ import ctypes as C
 import functools
 import math
 import struct
+import types
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import PscError, _check, _load, _workspace
 
@@ -27,6 +29,16 @@ _DTYPES = {torch.bfloat16: PSC_BF16, torch.float16: PSC_F16, torch.float32: PSC_
 
 # The address of a device's current stream: 0.1 us where torch has a function that gives it alone, 1.1 through a stream object.
 _stream_address = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+# Where torch says whether tensors may carry tangents (a level below 0: none does), so that calls without any ask nothing else.
+_duals = forward_ad if hasattr(forward_ad, "_current_level") else types.SimpleNamespace(_current_level=0)
+
+
+def _no_tangents(*tensors):
+    """Refuses tensors that carry a tangent: these calls have no forward-mode derivatives, and would drop it without a word."""
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise PscError("a tensor carries a tangent, and there are no forward-mode derivatives here: take its primal, or differentiate backwards where that is offered")
 
 
 class _Cache(C.Structure):
@@ -125,7 +137,7 @@ class KvCache:
         slots); `weights`, per slot (float32), receives 0.
         `rotary` (a `Rotary`, of a multiple of 16 dimensions): keys are turned first, row r of a sequence by the angles of first[b] + r, and so
         are the queries q [n, q_heads, head_dim] of the same rows, which are returned (in `q_out`, another tensor than q).
-        Nothing flows back: tensors that want a gradient are refused then."""
+        Nothing flows back or forward: tensors that want a gradient or carry a tangent are refused then."""
         c, batch, slots = self._args(table, lengths)
         n = k.shape[0]
         if v.dtype != k.dtype or v.shape != k.shape:
@@ -146,6 +158,8 @@ class KvCache:
             raise PscError(f"rotary: expected on {self.device}, got {rotary.device}")
         if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (k, v, q, q_out)):
             raise PscError("k, v, q: what goes into a memory in 4 bits has no gradient; detach, or call under torch.no_grad()")
+        if _duals._current_level >= 0:
+            _no_tangents(k, v, q, q_out)
         rows, to = (None, 0, 0), None
         if q is not None:
             heads = q.shape[1] if q.dim() == 3 else 0
@@ -182,7 +196,7 @@ class KvCache:
         more rows (with `offsets`; None: n).  `window` > 0: rows see that many positions back from their own, and the
         positions below `sinks`.  `scale` None: 1 / sqrt(head_dim).  `weights_out`, per slot (float32), receives
         `weights` (None: 0) plus the weight that each token was given; they may be the same tensor.  Nothing flows back:
-        a `q` that wants a gradient is refused."""
+        a `q` that wants a gradient, or carries a tangent, is refused."""
         return self._attend("psc_kv_attention", (self.head_dim, 1), None, q, table, lengths, offsets, max_rows, first, positions, scale, causal,
                             window, sinks, weights, weights_out, out, workspace)
 
@@ -211,6 +225,8 @@ class KvCache:
             at = lam.data_ptr()
         if torch.is_grad_enabled() and (lam.requires_grad or (norm is not None and norm.requires_grad)):
             raise PscError("lam, norm: attention over a memory in 4 bits has no gradient; detach them, or call under torch.no_grad()")
+        if _duals._current_level >= 0:
+            _no_tangents(lam, norm)
         more = at, row, _array(norm, torch.float32, (2 * self.head_dim,), "norm", self._index), eps, factor
         return self._attend("psc_kv_difference", (2 * self.head_dim, 2), more, q, table, lengths, offsets, max_rows, first, positions, scale, causal,
                             window, sinks, weights, weights_out, out, workspace)
@@ -229,6 +245,8 @@ class KvCache:
         _ints(max_rows=max_rows, window=window, sinks=sinks)
         if q.requires_grad and torch.is_grad_enabled():
             raise PscError("q: attention over a memory in 4 bits has no gradient; detach q, or call under torch.no_grad()")
+        if _duals._current_level >= 0:
+            _no_tangents(q)
         outs = (n, heads // shape[1], shape[0])
         if out is None:
             out = (torch.empty(outs, dtype=q.dtype, device=self.device),

@@ -15,7 +15,7 @@ import struct
 import torch
 
 from .binding import PscError, _check, _load, _workspace
-from .kv import _DTYPES, _array, _dtype, _stream_address
+from .kv import _DTYPES, _array, _dtype, _duals, _no_tangents, _stream_address
 
 
 class _Rotary(C.Structure):
@@ -96,7 +96,10 @@ class Rotary:
     def __call__(self, x, positions=None, first=None, offsets=None, out=None):
         """x [rows, heads, head_dim] (or [rows, head_dim]) turned: row r at positions[r] (int32), or at first[b] + its place in
         its sequence b, [batch] (int32; `offsets` [batch + 1]: where sequences begin, None: equal parts), or at r.
-        Rows that no sequence has are copied.  Differentiable in x; `out` (which may be x): written, and no gradient."""
+        Rows that no sequence has are copied.  Differentiable in x, backwards (an x that carries a tangent is refused); `out` (which may be x):
+        written, and no gradient."""
+        if _duals._current_level >= 0:
+            _no_tangents(x, out)
         if out is None and x.requires_grad and torch.is_grad_enabled():
             return _Turned.apply(x, self, positions, first, offsets)
         if out is not None and torch.is_grad_enabled() and (x.requires_grad or out.requires_grad):
@@ -105,6 +108,8 @@ class Rotary:
 
     def inverse(self, x, positions=None, first=None, offsets=None, out=None):
         """The transposed: turned back, times the factor (with factor 1 the inverse).  Nothing flows back."""
+        if _duals._current_level >= 0:
+            _no_tangents(x, out)
         if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
             raise PscError("x: the transposed has no gradient; detach x, or call under torch.no_grad()")
         return self._turn(x, positions, first, offsets, out, True)
@@ -242,7 +247,9 @@ def residual_norm(x, y=None, *, gate=None, activation="none", after=None, before
     `after`, `before` [width] (None: no such norm; without `before` z is None), `gate` (None: none) of y's rows, or with
     fewer rows [rows', width] of which each serves rows / rows' consecutive ones, through `activation` ("none", "sigmoid",
     "silu").  x or y may be None.  h has x's type (float32, or y's), z and the gate y's.  Without y and with residual_scale 1 h is x.
-    Differentiable in all tensors."""
+    Differentiable in all tensors, backwards and once (tensors that carry a tangent are refused)."""
+    if _duals._current_level >= 0:
+        _no_tangents(x, y, gate, after, before)
     some = y if x is None else x
     if some is None:
         raise PscError("x and y are None")

@@ -139,3 +139,27 @@ def test_an_infinity_in_the_last_row_that_shares_a_gate(rows, gates, width):
     dgate, = torch.autograd.grad(h, gate, dh)
     want = y.view(gates, each, width).sum(1)
     assert torch.equal(dgate, want)
+
+
+# ------------------------------------------------------------------------------------------- forward-mode derivatives
+def test_tangents_are_refused():
+    import paper_1609_01882_amd as psc
+    from torch.autograd import forward_ad
+    rope, w = psc.Rotary(64), torch.ones(64, device="cuda")
+    x = torch.randn((4, 2, 64), device="cuda")
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.arange(4, dtype=torch.int32, device="cuda").view(4, 1), torch.ones(4, dtype=torch.int32, device="cuda")
+    lam, norm = torch.ones(1, device="cuda"), torch.ones(128, device="cuda")
+    want = rope(x), psc.residual_norm(x, x, before=w)[1], cache.attend_difference(x, lam, table, lengths)[0]
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: rope(dual(x)), lambda: rope.inverse(dual(x)), lambda: psc.residual_norm(dual(x), x, before=w), lambda: psc.residual_norm(x, x, before=dual(w)),
+                     lambda: cache.append(dual(x), x, table, lengths, rotary=rope), lambda: cache.append(x, x, table, lengths, rotary=rope, q=dual(x)),
+                     lambda: cache.attend(dual(x), table, lengths), lambda: cache.attend_difference(dual(x), lam, table, lengths),
+                     lambda: cache.attend_difference(x, dual(lam), table, lengths), lambda: cache.attend_difference(x, lam, table, lengths, norm=dual(norm))):
+            with pytest.raises(psc.PscError, match="tangent"):
+                call()
+        # the others go on as ever
+        got = rope(x), psc.residual_norm(x, x, before=w)[1], cache.attend_difference(x, lam, table, lengths)[0]
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(rope(x), want[0])

@@ -1,0 +1,24 @@
+"""Refusals of the package's calls around the attention memory (no GPU: nothing is launched)."""
+import pytest
+import torch
+from torch.autograd import forward_ad
+
+
+def test_tangents_are_refused():
+    import paper_1609_01882_amd as psc
+    x, w = torch.zeros((2, 1, 8)), torch.ones(8)
+    rope = psc.Rotary(8, device="cpu")
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: rope(dual(x)), lambda: rope(x, out=dual(x)), lambda: rope.inverse(dual(x)), lambda: psc.residual_norm(dual(x), before=w),
+                     lambda: psc.residual_norm(x, dual(x), before=w), lambda: psc.residual_norm(x, before=dual(w)), lambda: psc.residual_norm(x, x, after=dual(w)),
+                     lambda: psc.residual_norm(x, x, gate=dual(x))):
+            with pytest.raises(psc.PscError, match="tangent"):
+                call()
+            with torch.no_grad(), pytest.raises(psc.PscError, match="tangent"):     # (which leaves tangents as they are)
+                call()
+        with pytest.raises(psc.PscError, match="tangent"):
+            rope(dual(x).requires_grad_())
+        # others are not meant: host tensors are refused for what they are
+        with pytest.raises(psc.PscError, match="CUDA"):
+            psc.residual_norm(x, before=w)
