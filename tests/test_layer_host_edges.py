@@ -22,3 +22,19 @@ def test_tangents_are_refused():
         # others are not meant: host tensors are refused for what they are
         with pytest.raises(psc.PscError, match="CUDA"):
             psc.residual_norm(x, before=w)
+
+
+def test_assembly_that_writes_m0_says_so():
+    import glob
+    import os
+    import re
+    import paper_1609_01882_amd as psc
+    source, found = os.path.join(os.path.dirname(psc.__file__), "csrc"), 0
+    for name in glob.glob(os.path.join(source, "*")):
+        with open(name) as f:
+            text = f.read()
+        for statement in re.findall(r"\basm\b[^;]*;", text):
+            if re.search(r"s_mov_b32 m0", statement):
+                found += 1
+                assert statement.count('"m0"') == 1, (os.path.basename(name), statement)
+    assert found >= 2
