@@ -139,9 +139,9 @@ class KvCache:
         are the queries q [n, q_heads, head_dim] of the same rows, which are returned (in `q_out`, another tensor than q).
         Nothing flows back or forward: tensors that want a gradient or carry a tangent are refused then."""
         c, batch, slots = self._args(table, lengths)
+        if k.dim() != 3 or v.dtype != k.dtype or v.shape != k.shape:
+            raise PscError(f"k, v: expected [rows, {self.kv_heads}, {self.head_dim}] of one type, got {k.dtype} {list(k.shape)} and {v.dtype} {list(v.shape)}")
         n = k.shape[0]
-        if v.dtype != k.dtype or v.shape != k.shape:
-            raise PscError("k and v differ in type or shape")
         if rotary is not None:
             return self._append_rotary(c, batch, slots, k, v, offsets, first, positions, weights, rotary, q, q_out)
         if q is not None or q_out is not None:
@@ -163,7 +163,7 @@ class KvCache:
         rows, to = (None, 0, 0), None
         if q is not None:
             heads = q.shape[1] if q.dim() == 3 else 0
-            if q.dtype != k.dtype or q.shape[0] != n or heads < 1:
+            if heads < 1 or q.dtype != k.dtype or q.shape[0] != n:
                 raise PscError(f"q: expected {k.dtype} [{n}, q_heads, {self.head_dim}], got {q.dtype} {list(q.shape)}")
             rows = self._rows(q, heads, "q")
             if q_out is None:
@@ -218,7 +218,7 @@ class KvCache:
             row = 0
             at = _array(lam, torch.float32, (heads // 2,), "lam", self._index)
         else:
-            row = lam.stride(0)
+            row = lam.stride(0) if lam.dim() else 0
             if lam.shape != (n, heads // 2) or lam.dtype != torch.float32 or lam.get_device() != self._index or (heads > 2 and lam.stride(1) != 1):
                 raise PscError(f"lam: expected float32 [{heads // 2}] or [{n}, {heads // 2}] on {self.device} with contiguous heads, got {lam.dtype} "
                                f"{list(lam.shape)} with strides {list(lam.stride())} on {lam.device}")
@@ -235,7 +235,7 @@ class KvCache:
                 out, workspace):
         """`shape`: width of an output head, and how many query heads it takes; `more`: what the call takes behind the sinks."""
         c, batch, slots = self._args(table, lengths)
-        n, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+        n, heads = (q.shape[0], q.shape[1]) if q.dim() == 3 else (0, 0)
         code, device = _dtype(q, "q"), self._index
         rows = self._rows(q, heads, "q")
         if offsets is None:

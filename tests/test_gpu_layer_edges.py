@@ -163,3 +163,19 @@ def test_tangents_are_refused():
         got = rope(x), psc.residual_norm(x, x, before=w)[1], cache.attend_difference(x, lam, table, lengths)[0]
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.equal(rope(x), want[0])
+
+
+# ------------------------------------------------------------------------------------------- what is refused
+def test_tensors_without_dimensions_are_refused():
+    import paper_1609_01882_amd as psc
+    rope, w, none = psc.Rotary(64), torch.ones(64, device="cuda"), torch.zeros((), device="cuda")
+    x = torch.zeros((4, 2, 64), device="cuda")
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.arange(4, dtype=torch.int32, device="cuda").view(4, 1), torch.ones(4, dtype=torch.int32, device="cuda")
+    lam = torch.ones(1, device="cuda")
+    for call in (lambda: rope(none), lambda: rope(x, first=none.int()), lambda: rope(x, offsets=none.int()), lambda: psc.residual_norm(none, before=w), lambda: psc.residual_norm(x, before=none),
+                 lambda: cache.append(none, none, table, lengths), lambda: cache.append(none, none, table, lengths, rotary=rope), lambda: cache.append(x, x, table, lengths, rotary=rope, q=none),
+                 lambda: cache.attend(none, table, lengths), lambda: cache.attend(x, none.int(), lengths), lambda: cache.attend_difference(none, lam, table, lengths),
+                 lambda: cache.attend_difference(x, none, table, lengths), lambda: cache.attend_difference(x, lam, table, lengths, norm=none)):
+        with pytest.raises(psc.PscError):
+            call()
