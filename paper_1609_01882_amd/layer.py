@@ -33,6 +33,9 @@ _pack = struct.Struct("@5iPqPqPq2i2P3f0P").pack     # the same fields, packed at
 assert struct.calcsize("@5iPqPqPq2i2P3f0P") == C.sizeof(_Norm)
 
 
+_MOST_FLOAT32 = float.fromhex("0x1.fffffep127")
+
+
 def _current(index, what):
     if torch.cuda.current_device() != index:
         raise PscError(f"{what} is on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
@@ -83,8 +86,8 @@ class Rotary:
         frequencies = rotary_frequencies(dims, base) if frequencies is None else [float(f) for f in frequencies]
         if dims < 2 or dims % 2 or len(frequencies) != dims // 2:
             raise PscError(f"dims ({dims}) must be even, with a frequency for each pair, got {len(frequencies)}")
-        if not math.isfinite(factor):
-            raise PscError("factor must be finite")
+        if not abs(factor) <= _MOST_FLOAT32:
+            raise PscError("factor must be finite in 32 bits")
         turns = (C.c_uint64 * (dims // 2))()
         _check(_load().psc_rotary_turns((C.c_double * (dims // 2))(*frequencies), dims // 2, turns))
         self.dims, self.interleaved, self.factor, self.frequencies = dims, bool(interleaved), float(factor), frequencies
@@ -136,6 +139,8 @@ class Rotary:
             batch = offsets.shape[0] - 1 if offsets.dim() == 1 else 0
         if batch < 1:
             raise PscError("first, offsets: expected [batch] and [batch + 1]")
+        if (rows | heads | dim | batch) >> 31:
+            raise PscError(f"x, first, offsets: {rows} rows of {heads} heads of {dim} and {batch} sequences do not fit 32 bits")
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
             to = heads * dim, dim
@@ -178,22 +183,25 @@ def _struct_of(x, y, gate, after, before, numbers):
     y_at, y_stride = (0, 0) if y is None else (y.data_ptr(), y.stride(0))
     gate_at, gate_stride, gate_rows = (0, 0, 0) if gate is None else (gate.data_ptr(), gate.stride(0), gate.shape[0])
     activation, *scales = numbers
-    return _pack(rows, width, _DTYPES[some.dtype], _DTYPES[block.dtype], _DTYPES[torch.float32 if weights is None else weights.dtype],
-                 x_at, x_stride, y_at, y_stride, gate_at, gate_stride, gate_rows, activation, 0 if after is None else after.data_ptr(),
-                 0 if before is None else before.data_ptr(), *scales)
+    try:
+        return _pack(rows, width, _DTYPES[some.dtype], _DTYPES[block.dtype], _DTYPES[torch.float32 if weights is None else weights.dtype],
+                     x_at, x_stride, y_at, y_stride, gate_at, gate_stride, gate_rows, activation, 0 if after is None else after.data_ptr(),
+                     0 if before is None else before.data_ptr(), *scales)
+    except (struct.error, OverflowError) as e:
+        raise PscError(f"x [{rows}, {width}], scales {scales}: {e}") from None
 
 
 def _forward(x, y, gate, after, before, numbers, want_h, want_stat):
     some = y if x is None else x
+    norm = _struct_of(x, y, gate, after, before, numbers)
     h = torch.empty_like(some, memory_format=torch.contiguous_format) if want_h else None
     z = stat = None
     if before is not None:
         z = torch.empty_like(some if y is None else y, memory_format=torch.contiguous_format)
     if want_stat:
         stat = torch.empty((some.shape[0], 2), dtype=torch.float32, device=some.device)
-    _check(_load().psc_residual_norm_forward(_struct_of(x, y, gate, after, before, numbers), h.data_ptr() if want_h else None,
-                                             None if z is None else z.data_ptr(), stat.data_ptr() if want_stat else None,
-                                             _current(some.get_device(), "x")))
+    _check(_load().psc_residual_norm_forward(norm, h.data_ptr() if want_h else None, None if z is None else z.data_ptr(),
+                                             stat.data_ptr() if want_stat else None, _current(some.get_device(), "x")))
     return h, z, stat
 
 

@@ -179,3 +179,22 @@ def test_tensors_without_dimensions_are_refused():
                  lambda: cache.attend_difference(x, none, table, lengths), lambda: cache.attend_difference(x, lam, table, lengths, norm=none)):
         with pytest.raises(psc.PscError):
             call()
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    import paper_1609_01882_amd as psc
+    rope, w = psc.Rotary(64), torch.ones(64, device="cuda")
+    x, many = torch.zeros((4, 2, 64), device="cuda"), (1 << 32) + 4
+    long = torch.zeros((1, 2, 64), device="cuda").expand(many, 2, 64)                    # (as 32 bits: 4)
+    cache = psc.KvCache.empty(4, 2, 64, 16)
+    table, lengths = torch.arange(4, dtype=torch.int32, device="cuda").view(4, 1), torch.ones(4, dtype=torch.int32, device="cuda")
+    lam, offsets = torch.ones(1, device="cuda"), torch.arange(5, dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros((1, 2, 64), device="cuda").expand(many, 2, 64), torch.zeros((1, 2), device="cuda").expand(many, 2)
+    space = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    for call in (lambda: rope(long, out=out), lambda: rope(long, offsets=offsets, out=out), lambda: rope.inverse(long, out=out),
+                 lambda: rope(x[:, :1].expand(4, many, 64), out=x[:, :1].expand(4, many, 64)),
+                 lambda: cache.append(long, long, table, lengths, offsets=offsets), lambda: cache.append(long, long, table, lengths, offsets=offsets, rotary=rope),
+                 lambda: cache.attend(long, table, lengths, offsets=offsets, max_rows=1, out=(out, lse), workspace=space),
+                 lambda: psc.residual_norm(long[:, 0], long[:, 1], before=w), lambda: psc.residual_norm(x, x, before=w, residual_scale=1e39), lambda: psc.residual_norm(x, x, before=w, eps=1e39)):
+        with pytest.raises(psc.PscError):
+            call()

@@ -38,3 +38,11 @@ def test_assembly_that_writes_m0_says_so():
                 found += 1
                 assert statement.count('"m0"') == 1, (os.path.basename(name), statement)
     assert found >= 2
+
+
+def test_factors_that_32_bits_do_not_hold():
+    import paper_1609_01882_amd as psc
+    assert psc.Rotary(8, factor=-3.4e38, device="cpu").factor == -3.4e38
+    for factor in (3.5e38, -1e39, float("inf"), float("nan")):
+        with pytest.raises(psc.PscError):
+            psc.Rotary(8, factor=factor, device="cpu")
