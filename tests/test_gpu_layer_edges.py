@@ -5,6 +5,7 @@ import torch
 
 import kv_util as U
 import layer_util as L
+import test_gpu_difference as D
 
 pytestmark = pytest.mark.gpu
 
@@ -55,6 +56,70 @@ def test_rows_that_see_nothing_are_0_whatever_norms_them(dtype, dim, way):
     # (2^-126 is lost beside any mean square of the others')
     want, _ = call(lam, 2.0 ** -126)
     assert bool(torch.isfinite(got).all()) and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 128), ("f32", 128)])
+@pytest.mark.parametrize("batch,rows", [(70, 1), (130, 2)])
+def test_parts_of_more_sequences_than_a_wave_has_lanes(dtype, dim, batch, rows):
+    # 64 sequences at a time are looked through for a part's own: the long ones stand at both sides of every 64th, some have no tokens or no rows
+    rng = np.random.default_rng(batch)
+    tokens, counts = rng.integers(1, 60, batch), np.full(batch, rows)
+    for b, n in ((3, 1500), (63, 2000), (64, 1200), (69, 3000), (batch - 1, 1700)):
+        tokens[b] = n
+    tokens[5], tokens[66], counts[7], counts[65], counts[batch - 2] = 0, 0, 0, 0, 0
+    D._case(batch, dtype, dim, 1, 2, 16, tokens, counts, nobody=(1, 3))
+    D._case(batch + 1, dtype, dim, 2, 3, 32, tokens, counts, evicted=True, lam_rows=True)
+    D._case(batch + 2, dtype, dim, 1, 2, 16, tokens, np.full(batch, rows), window=300, sinks=5, weights=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("batch,pairs", [(70, 2), (130, 1)])
+def test_rows_in_parts_of_more_sequences_than_a_wave_has_lanes(dtype, batch, pairs):
+    # the same where waves have rows of their own: 64 rows times query heads to a sequence and more, 16 blocks to a workgroup and more
+    rng = np.random.default_rng(batch)
+    tokens, counts = rng.integers(20, 60, batch), rng.integers(8, 17, batch)
+    for b, n in ((0, 900), (63, 2000), (64, 1200), (69, 4100), (batch - 1, 1700)):
+        tokens[b], counts[b] = n, 16
+    tokens[5], tokens[66], counts[7], counts[65], counts[batch - 2] = 0, 0, 0, 1, 0
+    slots, most = 4112, int(counts.max())
+    assert 64 < most * 8 <= 128 and counts.sum() * 8 >= 64 * batch and batch * pairs <= 512 and batch * pairs * (slots // 32) >= 512 * 16
+    D._case(batch, dtype, 64, pairs, 8, 16, tokens, counts, nobody=(1, 3))
+    D._case(batch + 1, dtype, 64, pairs, 8, 16, tokens, counts, evicted=True, weights=False, lam_rows=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim,tokens,rows", [(64, 500, 3), (128, 4000, 1), (64, 300, 60)])
+def test_maps_that_nearly_cancel(dtype, dim, tokens, rows):
+    """Equal keys, queries and lam that differ by little: what is left of the maps is small beside what the rounding of their probabilities
+    leaves, and the norm makes it large; the definition's tolerance follows it."""
+    import paper_1609_01882_amd as psc
+    rng = np.random.default_rng(tokens)
+    buffers, table, lengths = L.random_memory(rng, 1, 2, dim, 16, [tokens])
+    for buf in buffers[:2]:
+        buf[:, 1] = buf[:, 0]
+    q = rng.normal(size=(rows, 1, dim)).repeat(2, 1)
+    q[:, 1] += rng.normal(size=(rows, dim)) * 0.02
+    q = torch.from_numpy(q).to(U.TYPES[dtype]).cuda()
+    lam, norm, offsets = np.full((rows, 1), 1.0 - 2.0 ** -6, np.float32), np.ones(2 * dim, np.float32), np.array([0, rows])
+    cache, args = psc.KvCache(*(_cuda(x) for x in buffers)), dict(scale=dim ** -0.5, eps=1e-12)
+    for weight in (None, norm):
+        out, lse = cache.attend_difference(q, _cuda(lam), _cuda(table), _cuda(lengths), norm=_cuda(weight), **args)
+        ref, tol = L.difference(q.double().cpu().numpy(), lam, buffers, table, lengths, offsets, None, None, float(np.float32(dim ** -0.5)), True, 0, 0, weight,
+                                float(np.float32(1e-12)), 1.0, dtype)
+        got = out.double().cpu().numpy()
+        worst = L.finite_or_same(got, ref[0], tol[0])
+        assert worst <= 1.0, (weight is None, worst)
+        if weight is None and dtype != "f32":
+            # That is the worst case, and here more than a value.  A probability p is off by at most 2^-11 p and, taken as spread evenly, by 2^-11 p / sqrt(3)
+            # in the root mean square; tokens are off independently.  Twice that, and the output's rounding.
+            k, v = (np.stack([U.held(buffers, table, 0, w, tokens)[i] for w in (0, 1)]) for i in (0, 1))
+            at = np.arange(tokens) <= tokens - rows + np.arange(rows)[:, None]
+            p = np.exp(np.einsum("rwd,wtd->wrt", q.double().cpu().numpy(), k) * dim ** -0.5 - ref[1].T[..., None]) * at
+            size = (p[0] ** 2 + (lam.astype(np.float64) * p[1]) ** 2) @ np.concatenate((v[0], v[1]), -1) ** 2
+            bound = 2 * np.sqrt(size.sum() * 2.0 ** -22 / 3) + U.UNIT[dtype] * np.linalg.norm(ref[0])
+            off = np.linalg.norm(got - ref[0])
+            print(f"cancel {dtype} {dim} {tokens} {rows}: off by {off / np.linalg.norm(ref[0]):.2g} of the output, {off / bound:.2f} of what is allowed", flush=True)
+            assert off <= bound
 
 
 # ------------------------------------------------------------------------------------------- rotary positions
