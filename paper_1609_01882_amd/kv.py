@@ -142,7 +142,8 @@ class KvCache:
         if k.dim() != 3 or v.dtype != k.dtype or v.shape != k.shape:
             raise PscError(f"k, v: expected [rows, {self.kv_heads}, {self.head_dim}] of one type, got {k.dtype} {list(k.shape)} and {v.dtype} {list(v.shape)}")
         n = k.shape[0]
-        _ints(rows=n)
+        if n >> 31:
+            _ints(rows=n)
         if rotary is not None:
             return self._append_rotary(c, batch, slots, k, v, offsets, first, positions, weights, rotary, q, q_out)
         if q is not None or q_out is not None:
@@ -243,7 +244,8 @@ class KvCache:
             max_rows = n // max(batch, 1)
         elif max_rows is None:
             max_rows = n
-        _ints(rows=n, max_rows=max_rows, window=window, sinks=sinks)
+        if (n | max_rows | window | sinks) >> 31:   # (negative ones too: the call says what is wrong with them)
+            _ints(rows=n, max_rows=max_rows, window=window, sinks=sinks)
         if q.requires_grad and torch.is_grad_enabled():
             raise PscError("q: attention over a memory in 4 bits has no gradient; detach q, or call under torch.no_grad()")
         if _duals._current_level >= 0:
