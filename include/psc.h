@@ -488,8 +488,11 @@ int psc_kv_attention(const psc_kv_cache *cache, int dtype, const void *q_dev, in
  * Both heads of a pair hold the same tokens in the same slots: positions_dev is read for the even one.  weights_out_dev:
  * both heads of a pair receive the sum of both maps' probabilities, so that psc_kv_evict cuts them alike where
  * they began alike.  A map that comes out NaN adds nothing to the weights; its output head is NaN.  Rows that see
- * nothing come out 0, whatever lam, norm and eps are.  Everything else as for psc_kv_attention, the precision of a map's
- * products too. */
+ * nothing come out 0, whatever lam, norm and eps are.  Heads are in the order [pair][map][group]; projections that give them
+ * as [pair][group][map] have their rows permuted once.  Everything else as for psc_kv_attention, the precision of a map's
+ * products too: of out before the norm, each probability's 2^-11 (float32 rows: 2^-22) counts for both maps, however little their
+ * difference leaves, and the norm divides that by the difference's root mean square.  Long memories with a row or two beside a
+ * sequence of hundreds of rows are faster in a call of their own. */
 size_t psc_kv_difference_workspace_bytes(const psc_kv_cache *cache, int dtype, int nrows, int max_rows, int q_heads,
                                          int window, int sinks, int has_positions, int has_weights);
 int psc_kv_difference(const psc_kv_cache *cache, int dtype, const void *q_dev, int64_t q_row_stride,

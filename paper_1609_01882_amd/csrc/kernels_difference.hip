@@ -7,7 +7,15 @@
 // What it is bound by.  A few rows: reading the memory, 4.8 TB/s (8 sequences of 40 to 100 thousand tokens x 8 heads x 128, 618 MB in 128 us;
 // 146 with the codes through registers and one wave to a SIMD).  Many rows: vector instructions and the way from one product's
 // operands to the next product: 2048 rows of 32 query heads over 16384 tokens 925 to 1050 us by card, 740 to 840 TFLOP/s (through registers
-// 1768; every wave with expansions of its own 1178).
+// 1768; every wave with expansions of its own 1178).  float32 rows, whose scores take three products and whose values two, have one wave to a SIMD
+// and expand for themselves: the same rows 2374 us.
+//
+// Bits.  Scores, sums and the difference are 32 bits.  The probabilities of 16-bit rows go into the second product as float16 (11 bits: one product,
+// where two terms would take two; float32 rows have two, 22 bits).  That error is a share of each map, not of what the maps leave of
+// each other: where they cancel to 2 % of themselves, outputs are 0.7 % off, and the head's norm makes it no smaller.
+//
+// Registers.  Two waves to a SIMD have 256 each, and some kernels need more: with 64 coordinates and 32 rows to a wave 132 to 240 bytes of a lane lie in
+// scratch, with 128 coordinates 36 to 52 (none in the rows kernel over a memory in order).
 #include <algorithm>
 #include <type_traits>
 
@@ -995,15 +1003,15 @@ constexpr int64_t kLeastBlocks = 8, kFewBlocks = 32;
 // Rows of a wave, in sixteens, at most.
 constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || dim == 128 ? 1 : 2; }
 
-// Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel): two to a compute unit.  8 heads x 128, us with rows of their
-// own and without: 512 rows x 4 over 8000 tokens (512 workgroups) 444 and 485, 2048 over 8000 (512) 509 and 578, 8192 of 8192 (2048) 1102 and 1320;
+// Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel): two to a compute unit, as many as run at
+// a time.  With just so many it gains or loses little, with half as many again it loses 5 %.  8 heads x 128, us with rows of their own and without: 512 rows x 4 over 8000 tokens (512 workgroups) 444 and 485, 2048 over 8000 (512) 509 and 578, 8192 of 8192 (2048) 1102 and 1320;
 // 2048 of 2048 (512) 140 and 138, 3000 over 8000 (752) 830 and 790; 1024 over 8000 (256) 385 and 315, 256 x 4 over 8000 (256) 382 and 287.
 constexpr int64_t kRowGroups = 512;
 
 // 64 coordinates: where workgroups with rows of their own would be fewer, what they see is cut into parts, as many workgroups as those, if there are
 // kRowUnits units and kRowBlocks blocks to a part at least.  4 heads x 64, float16, 8 query heads to each, us so cut and with waves that share out the
 // tokens, joins with both: 624 rows over 6209 tokens 138 and 193, in any order 170 and 246; 3 x 300 over 3000 (21 blocks to a part) 99 and 127, 400 over
-// 6000 (18) 103 and 137, 900 over 3000 (21) 128 and 122, 1200 over 1900 (14) 105 and 90; 100 over 40000 (14 units) 136 and 140, 40 over 60000 (6 units) 103 and 97.
+// 6000 (18) 103 and 137, 900 over 3000 (21) 128 and 122 (lost: more rows and short memories), 1200 over 1900 (14) 105 and 90; 100 over 40000 (14 units) 136 and 140, 40 over 60000 (6 units) 103 and 97.
 // (128 coordinates, a part's sums twice as long: 256 rows over 8000 120 and 112, over 30000 292 and 310; 1024 over 4000 203 and 167: never taken.)
 constexpr int64_t kRowUnits = 16, kRowBlocks = 16;
 
@@ -1066,7 +1074,10 @@ KvPlan plan_kv_difference(const KvView &c, int dtype, int group, int64_t nrows, 
     int64_t blocks = blocks_of_rows(16 * p.row_tiles);
     const int most = 64 * most_row_tiles(dtype, c.dim);
     const int64_t groups = (m + most - 1) / most;
-    // (by the rows that there are, not by the most that a sequence may have: single tokens beside a prompt do not fill workgroups)
+    // (By the rows that there are, not by the most that a sequence may have: single tokens beside a prompt do not fill workgroups.  Whether units are
+    // cut into parts does go by the most, for all sequences: long memories with a row or two beside a sequence with many rows are not cut.  31
+    // tokens over 8 to 98 thousand, 8 heads x 128: 359 us in a call of their own; with a chunk over 16 thousand, of 2048 rows 1991 us where that
+    // takes 926 alone, of 512 rows 6625 where that takes 336, of 300 rows 1158 where that takes 256.)
     p.own_rows = dtype != PSC_F32 && nrows * group * pairs >= kRowGroups * most && m > most / 2;
     if (p.own_rows) p.row_groups = groups;
     int64_t units = p.row_groups * c.batch * pairs;

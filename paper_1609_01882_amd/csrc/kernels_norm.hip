@@ -3,8 +3,10 @@
 //   h = residual_scale x + block_scale u      z = rms(h) * before
 // A row lies in the registers of `lanes` lanes, 8 consecutive coordinates (or twice 8) to each: 8 to 64 lanes of a wave for narrow rows,
 // a workgroup for wide ones.  Each input is read once and each output written once; everything between is 32-bit floats.
-// Bound by HBM: 16384 x 4096 bfloat16 with a gate, forward 139 us, backward 226 (4.8 TB/s).  A few rows: the start and the way through the
-// instructions (6 rows 4.5 and 9.5 us).
+// Bound by HBM: 16384 x 4096 bfloat16 with a gate, forward 139 us, backward 226 to 235 (4.6 to 4.8 TB/s).  A few rows: the start and the way through
+// the instructions (6 rows 4.5 and 9.5 us).  Rows wider than 8192 have 1024 lanes and so 128 registers each, which do not do for the backward pass:
+// 316 to 492 bytes of a lane lie in scratch (forward 68 to 140), and weights are read again for every row.  4096 x 12288 and x 16384, forward
+// 126 and 143 us (4.0 and 4.7 TB/s), backward 591 and 649 (1.4 and 1.7), where 4096 x 8192 takes 74 and 136.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -190,9 +192,8 @@ struct Columns {
     __device__ int count(int v) const { return v < NV - 1 ? 8 : max(0, min(8, width - at(v))); }
 };
 
-// The weights of both norms: a workgroup's rows share them in LDS (in registers they would cost a third of the waves: 195 us forward
-// instead of 156), where a lane's eight
-// lie in two planes, 16 bytes beside the next lane's.  The widest rows' do not fit and are read again for every row.
+// The weights of both norms: a workgroup's rows share them in LDS (in registers they would cost a third of the waves: at the step that took 156
+// us forward, 195), where a lane's eight lie in two planes, 16 bytes beside the next lane's.  The widest rows' do not fit and are read again for every row.
 template <int TB, int NV, bool kLds>
 struct NormWeights {
     float4 *lds;
@@ -374,8 +375,8 @@ __global__ __launch_bounds__(kThreads) void residual_norm_kernel(ResidualNorm p,
     }
 }
 
-// Sums over a workgroup's rows, a place of each lane's own in LDS (registers would leave room for half the waves: 570 us backward
-// instead of 272), in planes of 16 bytes to a lane.
+// Sums over a workgroup's rows, a place of each lane's own in LDS (registers would leave room for half the waves: at the step that took 272 us
+// backward, 570), in planes of 16 bytes to a lane.
 template <int NV>
 struct RowSums {
     float4 *lds;

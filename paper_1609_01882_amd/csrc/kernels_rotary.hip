@@ -9,7 +9,8 @@
 // cosines for several heads.
 //
 // Bound by HBM: 16384 rows of 32 heads x 128 bfloat16 in 54 us, 5.0 TB/s (67 with rows, not heads, beside each other in a wave); 27 thousand rows
-// of 32 query heads and 8 kv heads x 128 float16 into the memory in 133 us, 4.5 TB/s (159 without the loads ahead).
+// of 32 query heads and 8 kv heads x 128 float16 into the memory in 121 us, 5.0 TB/s (when it took 133, 159 without the loads ahead).  Dimensions
+// or places that the wide kernel does not take: two-byte accesses, 24 of 96 coordinates of 16384 rows x 32 heads bfloat16 in 80 us, 2.5 TB/s.
 #include "kv_device.h"
 
 namespace psc {

@@ -210,7 +210,9 @@ class KvCache:
         2j * g + i and (2j + 1) * g + i, with `norm` [2 head_dim] (float32) divided by the root of its mean square plus
         `eps` and multiplied by `norm`; then by `factor`.  `lam` (float32): [q_heads / 2], or [n, q_heads / 2] for each row.
         `positions` of a pair's heads are alike (the even one's are read); both receive both maps' weights.  head_dim is
-        64 or 128, kv_heads even.  All else as for `attend`; nothing flows back."""
+        64 or 128, kv_heads even.  16-bit rows' probabilities are rounded to 11 bits in both maps, however little the difference leaves of
+        them (float32 rows: 22).  All else as for `attend`; nothing flows back.  Single tokens over long memories are faster in a call of their own than
+        beside a sequence of hundreds of rows."""
         heads = q.shape[1] if q.dim() == 3 else 0
         if self.kv_heads % 2 or self.head_dim > 128 or heads < 1 or heads % self.kv_heads:
             raise PscError(f"differential attention takes pairs of kv heads of 64 or 128 and a multiple of {self.kv_heads} query heads, got {heads} over "

@@ -254,7 +254,7 @@ def residual_norm(x, y=None, *, gate=None, activation="none", after=None, before
         h = residual_scale * x + block_scale * u        z = rms(h) * before
     `after`, `before` [width] (None: no such norm; without `before` z is None), `gate` (None: none) of y's rows, or with
     fewer rows [rows', width] of which each serves rows / rows' consecutive ones, through `activation` ("none", "sigmoid",
-    "silu").  x or y may be None.  h has x's type (float32, or y's), z and the gate y's.  Without y and with residual_scale 1 h is x.
+    "silu").  x or y may be None.  h has x's type (float32, or y's), z and the gate y's (without y: x's).  Without y and with residual_scale 1 h is x.
     Differentiable in all tensors, backwards and once (tensors that carry a tangent are refused)."""
     if _duals._current_level >= 0:
         _no_tangents(x, y, gate, after, before)
