@@ -1004,8 +1004,10 @@ constexpr int64_t kLeastBlocks = 8, kFewBlocks = 32;
 constexpr int most_row_tiles(int dtype, int dim) { return dtype == PSC_F32 || dim == 128 ? 1 : 2; }
 
 // Workgroups from which on a wave's rows are its own (kv_difference_rows_kernel): two to a compute unit, as many as run at
-// a time.  With just so many it gains or loses little, with half as many again it loses 5 %.  8 heads x 128, us with rows of their own and without: 512 rows x 4 over 8000 tokens (512 workgroups) 444 and 485, 2048 over 8000 (512) 509 and 578, 8192 of 8192 (2048) 1102 and 1320;
-// 2048 of 2048 (512) 140 and 138, 3000 over 8000 (752) 830 and 790; 1024 over 8000 (256) 385 and 315, 256 x 4 over 8000 (256) 382 and 287.
+// a time.  With just so many it gains 8 to 12 % or loses 1, with half as many again it lost 5 %, with four times as many it gains 17 %.  8 heads x
+// 128, us with rows of their own and without: 512 rows x 4 over 8000 tokens (512 workgroups) 444 and 485, 2048 over 8000 (512) 509 and 578, 8192 of
+// 8192 (2048) 1102 and 1320; 2048 of 2048 (512) 140 and 138, 3000 over 8000 (752) 830 and 790; 1024 over 8000 (256) 385 and 315, 256 x 4 over 8000
+// (256) 382 and 287.
 constexpr int64_t kRowGroups = 512;
 
 // 64 coordinates: where workgroups with rows of their own would be fewer, what they see is cut into parts, as many workgroups as those, if there are
